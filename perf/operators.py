@@ -192,8 +192,8 @@ def _prepare_nets(case, seed):
         s["grad_out"] = torch.randn((G, P, case["outputs"]), generator=g, device="cuda") / P
     if own:
         from paper_2608_27612_amd import emr
-        subs = [(2.0 * i / max(1, case["inputs"]) - 1, -1.0, emr.DIR_OUT) for i in range(case["inputs"])]
-        subs += [(2.0 * i / max(1, case["outputs"]) - 1, 1.0, emr.DIR_IN) for i in range(case["outputs"])]
+        subs = [(2.0 * i / max(1, case["inputs"]) - 1, -1.0, emr.EMR_DIR_OUT) for i in range(case["inputs"])]
+        subs += [(2.0 * i / max(1, case["outputs"]) - 1, 1.0, emr.EMR_DIR_IN) for i in range(case["outputs"])]
         s["net"] = emr.emr_load_networks(subs, nets["node_offset"], nets["in_offset"], nets["src"],
                                          nets["w"])
         if case["op"] == "back":
