@@ -513,6 +513,69 @@ void emr_free_networks(emr_networks* net);
  * memory after the work already on `stream`; returns when the copy is done. */
 emr_status emr_copy_to_host(void* host, const void* device, int64_t bytes, void* stream);
 
+/* ------------------------------------------------------------------ choices
+ * What follows a network's outputs, or a generation's fitness: drawing an index from rows of scores with
+ * given random numbers, and the loss of such draws with its gradient. A network with several outputs
+ * answers with one of them; the parents of the next generation are drawn by fitness (top_k: only
+ * the k fittest). */
+
+/* Types of scores. */
+enum { EMR_F32 = 0, EMR_BF16 = 1, EMR_F16 = 2 };
+
+/* Rows of scores (device, caller-owned): row r is the n (1 .. 2^31 - 1) scores from x + r * stride on
+ * (entries of the type; 0: every row is the same one). A score that must not be drawn is -inf. */
+typedef struct {
+  const void* x;
+  int32_t type;   /* EMR_F32, EMR_BF16, EMR_F16 */
+  int64_t rows;   /* 0 .. 2^31 - 1 */
+  int64_t n;
+  int64_t stride;
+} emr_scores;
+
+/* How a row's scores are drawn from; a row_ pointer (device, [rows]) that is not NULL replaces the
+ * value before it row by row. */
+typedef struct {
+  float temperature;            /* at least 0; below the least normal float: the first maximum */
+  const float* row_temperature; /* (a NaN or a negative one counts as 0) */
+  int32_t top_k;                /* 0: all */
+  const int32_t* row_top_k;     /* (a negative one counts as 0) */
+  float top_p;                  /* in (0, 1]; 1: all */
+  const float* row_top_p;       /* (a NaN counts as 1) */
+  float min_p;                  /* in [0, 1]; 0: all */
+  const float* row_min_p;       /* (a NaN counts as 0) */
+} emr_sampling;
+
+/*
+ * index[r * draws + d] (device, int32) receives the entry of row r that u[r * draws + d] (device, in
+ * [0, 1)) draws, and logp (device or NULL) its log-probability among the entries left.
+ *   - A NaN score counts as -inf, one above the largest float as that. With the row's maximum m, entry
+ *     i weighs q_i = floor(2^31 exp((x_i - m) * (1 / temperature))) in fp32, a whole number, so the sums
+ *     below are exact and the draws the same on every run and every division of the work; an entry
+ *     below 2^-31 of the largest weighs 0.
+ *   - top_k leaves the k largest scores; top_p, of those, the ones before which (by falling score) less
+ *     than top_p of their sum lies; min_p, of those, the ones with q_i >= 2^31 min_p. Equal scores rank
+ *     by index.
+ *   - With S the sum of the weights left, the draw is the first index at which their running sum by
+ *     index exceeds floor(u S) (in doubles; u outside [0, 1) counts as the nearest end).
+ * A row without a score above -inf gives index -1 and log-probability -inf. Enqueued on `stream`.
+ * EMR_E_INVAL, EMR_E_LIMIT (more than 2^31 - 1 rows or scores), EMR_E_DEVICE.
+ */
+emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const float* u, int64_t draws,
+                      int32_t* index, float* logp, void* stream);
+
+/*
+ * The loss of one index per row (device, [rows]): loss[r] = -scale[r] log softmax(x / temperature)[index[r]]
+ * (device, [rows], or NULL), and grad (device, rows of n entries of the scores' type, grad_stride entries
+ * apart, or NULL) its gradient, scale[r] / temperature (softmax(x / temperature) - 1 at index[r]).
+ * scale: device, [rows] (an advantage, a weight, a mean's factor), or NULL for 1. Computed in fp32,
+ * the gradient rounded once. A row whose index lies outside [0, n), or whose scores are all -inf, has no
+ * answer: its loss and gradient are 0. grad may be the scores' own memory. Enqueued on `stream`.
+ * EMR_E_INVAL, EMR_E_LIMIT, EMR_E_DEVICE.
+ */
+emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const float* scale,
+                           float temperature, float* loss, void* grad, int64_t grad_stride,
+                           void* stream);
+
 /*
  * Raw CPPN outputs (debug and parity): out_dev[r * N(D) + p] = CPPN output of pair r at grid
  * position p (device, caller-owned, n_pairs * N(D) floats). Same arithmetic as emr_discover.

@@ -32,9 +32,10 @@ ABI_FUNCTIONS = [
     "emr_band_values", "emr_band_filter", "emr_record_file_open",
     "emr_record_file_sink", "emr_record_file_close", "emr_build_networks", "emr_networks_info",
     "emr_networks_phase", "emr_activate", "emr_xor_fitness", "emr_free_networks",
-    "emr_copy_to_host",
+    "emr_copy_to_host", "emr_sample", "emr_answer_loss",
 ]
 EMR_CONN_FORWARD, EMR_CONN_BACKWARD, EMR_CONN_LATERAL, EMR_CONN_SELF, EMR_CONN_ALL = 1, 2, 4, 8, 15
+EMR_F32, EMR_BF16, EMR_F16 = 0, 1, 2
 EMR_NOALLOC_SCRATCH_BYTES = 32 << 20
 EMR_JIT_OFF, EMR_JIT_AUTO, EMR_JIT_ALWAYS = 0, 1, 2
 
@@ -94,6 +95,18 @@ class emr_network_phase(C.Structure):
                 ("w4", C.c_void_p), ("pair_offset", C.c_void_p), ("records", C.c_int64),
                 ("conn_cell", C.c_void_p), ("conn_w", C.c_void_p), ("conn_offset", C.c_void_p),
                 ("connections", C.c_int64)]
+
+
+class emr_scores(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("type", C.c_int32), ("rows", C.c_int64), ("n", C.c_int64),
+                ("stride", C.c_int64)]
+
+
+class emr_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("row_temperature", C.c_void_p),
+                ("top_k", C.c_int32), ("row_top_k", C.c_void_p),
+                ("top_p", C.c_float), ("row_top_p", C.c_void_p),
+                ("min_p", C.c_float), ("row_min_p", C.c_void_p)]
 
 
 _lib = None
@@ -156,6 +169,8 @@ def lib():
             "emr_xor_fitness": (I32, [P, I32, I32, P, P]),
             "emr_free_networks": (None, [P]),
             "emr_copy_to_host": (I32, [P, P, I64, P]),
+            "emr_sample": (I32, [P, P, P, I64, P, P, P]),
+            "emr_answer_loss": (I32, [P, P, P, F32, P, P, I64, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -1011,3 +1026,87 @@ def emr_build_networks(pop: Population, substrate, depth: int, theta: float, typ
                                     C.c_float(theta), type_mask, C.c_float(w_min), iterations,
                                     C.byref(h), _stream_ptr(stream)))
     return Networks(h)
+
+
+# ----------------------------------------------------------------------------- choices
+
+def _on_device(name, t, dtype=None, shape=None):
+    """t, checked: a device tensor of the dtype and shape asked for."""
+    import torch
+    if not torch.is_tensor(t) or not t.is_cuda:
+        raise ValueError("%s: a device tensor is needed" % name)
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: %s is needed, not %s" % (name, dtype, t.dtype))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _on(stream):
+    """The stream that a call's copies and results are made on: the call's own."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _scores(x):
+    """emr_scores of a device tensor [rows, n] (a copy where its last dimension is strided), and the
+    tensor that holds them."""
+    import torch
+    types = {torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16}
+    if not torch.is_tensor(x) or not x.is_cuda or x.dim() != 2 or x.dtype not in types:
+        raise ValueError("scores: a device tensor [rows, n] of float32, bfloat16 or float16 is needed")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        x = x.contiguous()
+    return emr_scores(x.data_ptr(), types[x.dtype], x.shape[0], x.shape[1], x.stride(0)), x
+
+
+def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: bool = True, stream=None):
+    """Draws by the random numbers u ([rows, draws], float32) from rows of scores ([rows, n]); see
+    emr_sample in include/emr.h. temperature, top_k, top_p and min_p are numbers, or device tensors with
+    one for each row (float32; top_k int32). Returns index (int32 [rows, draws]) and their
+    log-probabilities (float32, or None without logp), not synchronized."""
+    import torch
+    with _on(stream):
+        st, x = _scores(scores)
+        rows = x.shape[0]
+        _on_device("u", u, torch.float32)
+        if u.dim() != 2 or u.shape[0] != rows:
+            raise ValueError("u: shape (%d, draws) is needed, not %s" % (rows, tuple(u.shape)))
+        u = u.contiguous()
+        value, held = {}, []
+        for name, v, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+            if torch.is_tensor(v):
+                v = _on_device(name, v, dtype, (rows,)).contiguous()
+                held.append(v)
+                value[name], value["row_" + name] = 0, v.data_ptr()
+            else:
+                value[name], value["row_" + name] = v, 0
+        rule = emr_sampling(**value)
+        index = torch.empty(u.shape, dtype=torch.int32, device=x.device)
+        lp = torch.empty(u.shape, dtype=torch.float32, device=x.device) if logp else None
+        _check(lib().emr_sample(C.byref(st), C.byref(rule), C.c_void_p(u.data_ptr()), u.shape[1],
+                                C.c_void_p(index.data_ptr()),
+                                C.c_void_p(lp.data_ptr() if logp else 0), _stream_ptr(stream)))
+        return index, lp
+
+
+def emr_answer_loss(scores, index, scale=None, temperature: float = 1.0, stream=None):
+    """The loss of one index per row of scores ([rows, n]) and its gradient; see emr_answer_loss in
+    include/emr.h. index: int32 [rows]; scale: float32 [rows] or None. Returns loss (float32 [rows]) and
+    grad ([rows, n], of the scores' type), not synchronized."""
+    import torch
+    with _on(stream):
+        st, x = _scores(scores)
+        rows = x.shape[0]
+        index = _on_device("index", index, torch.int32, (rows,)).contiguous()
+        if scale is not None:
+            scale = _on_device("scale", scale, torch.float32, (rows,)).contiguous()
+        loss = torch.empty(rows, dtype=torch.float32, device=x.device)
+        grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        _check(lib().emr_answer_loss(C.byref(st), C.c_void_p(index.data_ptr()),
+                                     C.c_void_p(0 if scale is None else scale.data_ptr()),
+                                     C.c_float(temperature), C.c_void_p(loss.data_ptr()),
+                                     C.c_void_p(grad.data_ptr()), x.shape[1], _stream_ptr(stream)))
+        return loss, grad
