@@ -509,6 +509,52 @@ emr_status emr_xor_fitness(const emr_networks* net, int32_t bias_input, int32_t 
 
 void emr_free_networks(emr_networks* net);
 
+/* Networks from host arrays in the layout of emr_network_info (read during the call): kept ones, or
+ * ones from elsewhere. A genome's first n_substrate nodes are the substrate's sources; node i's
+ * incoming edges are in_offset[i] .. in_offset[i+1] - 1, from nodes in_src of its own genome, none into
+ * an input node. node_cell (or NULL: 0) and depth (0: none) are what emr_networks_info then reports; the
+ * handle has no phases and no bitmaps (known NULL, known_words 0). Synchronizes with `stream`.
+ * EMR_E_INVAL, EMR_E_LIMIT (more than 2^32 - 2 nodes), EMR_E_NOMEM, EMR_E_DEVICE. */
+emr_status emr_load_networks(const emr_source* substrate, int32_t n_substrate, int32_t depth,
+                             int32_t n_genomes, const int64_t* node_offset, const uint32_t* node_cell,
+                             const int64_t* in_offset, const uint32_t* in_src, const float* in_w,
+                             emr_networks** out, void* stream);
+
+/* The weights of every edge (device, [edges], in the order of in_w) for the calls after this one on
+ * `stream`. Enqueued. */
+emr_status emr_networks_set_weights(const emr_networks* net, const float* w, void* stream);
+
+/*
+ * Learning the weights. emr_activate_keep is emr_activate with the patterns on the device (inputs,
+ * [n_patterns][n_inputs], caller-owned) and the same outputs, bit for bit, that also keeps every step's
+ * states in 8 bits; emr_activate_backward takes them to the derivatives of a loss by the weights
+ * (grad_w, device, [edges]) and, where grad_inputs (device, [n_genomes][n_patterns][n_inputs]) is not
+ * NULL, by each genome's copy of the patterns, from those by the outputs (grad_outputs, device,
+ * [n_genomes][n_patterns][n_outputs]).
+ *   - kept (device, caller-owned, emr_kept_bytes of it, aligned to 16 bytes): code c = rint(255 s) stands
+ *     for the state c / 255, an error of at most 1 / 510 against 4 bytes for the float. Codes are
+ *     [steps - 1][blocks][nodes][b], b patterns beside each other: b = 4, 8 or 16 for up to 4, up to 8 or
+ *     more patterns, blocks = ceil(n_patterns / b); the states after step t lie at t - 1; input
+ *     nodes' codes are 0, those past n_patterns undefined. The states after the last step are not
+ *     kept: only the outputs' are used, and outputs holds those unrounded.
+ *   - The gradient is the one of the activation with each state replaced by c / 255 in both places where it
+ *     occurs (the product with a weight's derivative, and s (1 - s)), in fp32; every sum has a fixed
+ *     order, so a handle's gradients are the same bits on every call.
+ *   - A weight that `steps` steps do not let reach an output has derivative 0. A node that no derivative
+ *     reaches adds nothing, whatever its states.
+ * Enqueued on `stream`, but for the first backward call of a handle, which lays the edges out by source
+ * (allocations, so not under capture). Calls on one handle must be ordered on one stream, as emr_activate's.
+ * EMR_E_INVAL, EMR_E_CAPACITY (kept_bytes too small), EMR_E_LIMIT, EMR_E_NOMEM, EMR_E_DEVICE.
+ */
+emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes);
+emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32_t n_patterns,
+                             int32_t steps, float* outputs, uint8_t* kept, int64_t kept_bytes,
+                             void* stream);
+emr_status emr_activate_backward(const emr_networks* net, const float* inputs, int32_t n_patterns,
+                                 int32_t steps, const float* outputs, const uint8_t* kept,
+                                 int64_t kept_bytes, const float* grad_outputs, float* grad_w,
+                                 float* grad_inputs, void* stream);
+
 /* Copies `bytes` of device memory (such as the buffers the info calls above point to) to host
  * memory after the work already on `stream`; returns when the copy is done. */
 emr_status emr_copy_to_host(void* host, const void* device, int64_t bytes, void* stream);

@@ -1,5 +1,5 @@
 // Arguments of the kernels that draw from rows of scores and score the draws (choice.hip), shared with
-// their host entry points (choice.cpp).
+// their host entry points (networks.cpp).
 //
 // Weights. A row's entry i with score x_i weighs q_i = floor(2^31 exp((x_i - m) / T)), m the row's
 // maximum: a whole number of at most 31 bits and one, so that every sum of weights is a 64-bit

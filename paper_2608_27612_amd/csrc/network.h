@@ -1,4 +1,4 @@
-// Arguments of the network kernels (network.hip), shared with their host driver (networks.cpp).
+// Arguments of the network kernels (network.hip, learn.hip), shared with their host driver (networks.cpp).
 //
 // Numbering. Before pruning, genome g has raw nodes 0 .. n_sub - 1 (its substrate sources, in
 // substrate order) and n_sub + i for the i-th set bit of its hidden-cell bitmap (ascending grid
@@ -184,6 +184,18 @@ inline constexpr uint32_t net_run_lds(uint32_t n, uint32_t q) { return n * (32u 
 constexpr int kNetRanges = 8;                 // classes of genomes in a launch, at most
 constexpr uint32_t kNetStageFloats = 256;     // patterns small enough for the kernarg
 
+// States kept in 8 bits for the gradients: code c stands for c / 255. After step t (1 .. steps - 1) the
+// states are plane t - 1 of codes [plane][block][node][4 q], a block's 4 q patterns beside each other;
+// input nodes' codes are 0. q: as many groups of four patterns as there are, up to 4.
+struct NetKept {
+  uint8_t* codes;  // or NULL: nothing is kept
+  uint32_t q, blocks;
+  uint32_t planes;  // steps - 1
+};
+inline constexpr uint32_t net_kept_q(uint32_t patterns) {
+  return patterns <= 4u ? 1u : (patterns <= 8u ? 2u : 4u);
+}
+
 // Patterns passed by value to the device buffer the kernels read.
 struct NetStageArgs {
   float* dst;
@@ -208,6 +220,7 @@ struct NetRunArgs {
   uint32_t n_inputs, n_outputs, n_patterns;
   uint32_t steps;
   uint32_t lds_bytes;          // the launch's dynamic LDS
+  NetKept kept;
   // class r: genomes order[first[r]] .. (count[r] of them), blocks[r] blocks of 4 q[r] patterns
   uint32_t first[kNetRanges], count[kNetRanges], blocks[kNetRanges], q[kNetRanges];
 };
@@ -233,6 +246,7 @@ struct NetStateArgs {
   uint32_t n_inputs;
   uint32_t n_patterns;
   uint32_t pblocks;
+  NetKept kept;             // (the input nodes' codes)
   float v[kNetStageFloats];
 };
 
@@ -247,6 +261,8 @@ struct NetStepArgs {
   float* nxt;
   int64_t nodes;
   uint32_t pblocks;
+  NetKept kept;
+  uint32_t plane;           // the step's, when codes are kept
 };
 
 struct NetOutArgs {
@@ -260,6 +276,44 @@ struct NetOutArgs {
   int64_t nodes;
   uint32_t n_outputs;
   uint32_t n_patterns;
+};
+
+// Gradients. The edges a second time, grouped by their source.
+struct NetTurnArgs {
+  const int64_t* in_offset;  // [nodes + 1]
+  const uint32_t* in_src;    // [edges]
+  uint32_t* key;             // [edges] source
+  uint64_t* val;             // [edges] edge | destination << 32
+  uint32_t* dst;             // [edges] destination
+  const uint32_t* skey;      // sorted by source, each group in edge order
+  int64_t* out_offset;       // [nodes + 1]
+  int64_t nodes, edges;
+};
+
+// The stepwise kernels: derivatives by the node sums ("gz") as [pblocks][nodes] float4.
+struct NetBackArgs {
+  const int64_t* node_offset;
+  const int32_t* node_in;
+  const int32_t* out_node;     // [n_outputs]
+  const int64_t* in_offset;
+  const uint32_t* in_src;
+  const float* in_w;
+  const uint32_t* dst;         // [edges]
+  const int64_t* out_offset;   // [nodes + 1]
+  const uint64_t* out_edge;    // [edges] edge | destination << 32
+  const float* patterns;       // [n_patterns * n_inputs]
+  const float* outputs;        // [n_genomes * n_patterns * n_outputs]
+  const float* grad_outputs;   // the same
+  const float* gz;             // derivatives after the step
+  float* gz_before;            // before it
+  float* grad_w;               // [edges]
+  float* grad_inputs;          // [n_genomes * n_patterns * n_inputs] or NULL
+  NetKept kept;
+  int64_t nodes, edges;
+  uint32_t n_genomes, n_inputs, n_outputs, n_patterns;
+  uint32_t pblocks;
+  uint32_t step;               // 1 .. steps: the step whose derivatives gz holds
+  uint32_t last;               // whether it is the first one looked at: gradients are set, not added to
 };
 
 }  // namespace emr

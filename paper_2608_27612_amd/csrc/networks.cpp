@@ -1,4 +1,5 @@
-// Networks built from a population's discovered substrates, and their activation (the networks the
+// Networks built from a population's discovered substrates, their activation, the gradients of their
+// weights, and draws from their outputs' scores with their loss (the networks the
 // experiments evaluate, Section 5: XOR over its four patterns, with the hidden-to-hidden
 // connection type of Section 4's configurations).
 //
@@ -25,6 +26,7 @@
 #include <vector>
 
 #include "../../include/emr.h"
+#include "choice.h"
 #include "network.h"
 
 namespace emr {
@@ -284,12 +286,16 @@ struct emr_networks {
   int64_t words = 0;
   std::vector<emr_source> substrate;
   std::vector<int32_t> slots;  // in_slot[n_sub], then out_slot[n_sub]
+  std::vector<int32_t> out_node;  // [n_out] substrate index of output o
   std::vector<std::unique_ptr<Phase>> phases;
   Dev known;
   Dev node_offset, node_cell, node_in, in_offset, in_src, in_w, d_slots;
   Dev d_out_node;  // [n_out] substrate index of output o
   int64_t nodes = 0, edges = 0;
   Dev state, patterns;
+  // gradients: the edges by source (made by the first call), and the derivatives' two halves
+  Dev edge_dst, out_offset, out_edge, back;
+  bool turned = false;
   // genomes in the order of the activation launches (order_genomes): their loads and node counts, the
   // sums over those before each, and the most nodes of those before each in its class
   Dev order;
@@ -318,7 +324,8 @@ struct emr_networks {
     if (pin) (void)hipHostFree(pin);
     for (auto& ph : phases) ph->release_idle();
     for (Dev* d : {&known, &node_offset, &node_cell, &node_in, &in_offset, &in_src, &in_w,
-                   &d_slots, &d_out_node, &state, &patterns, &order})
+                   &d_slots, &d_out_node, &state, &patterns, &edge_dst, &out_offset, &out_edge,
+                   &back, &order})
       d->reset_idle();
   }
 };
@@ -863,14 +870,28 @@ RunCut best_cut(const emr_networks& N, int64_t pblocks, const uint32_t* q_of, in
   return best;
 }
 
-emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_patterns,
-                       int32_t steps, float* outputs, float* fitness, const float* targets,
-                       hipStream_t s) {
-  emr_networks& M = const_cast<emr_networks&>(*N);
+emr_status check_device(const emr_networks* N) {
   int dev = 0;
   NET_HIP(hipGetDevice(&dev));
   if (dev != N->device)
     return failf(EMR_E_INVAL, "networks: built on device %d, current device is %d", N->device, dev);
+  return EMR_OK;
+}
+
+// The end of the work queued on `s`, which the handle's buffers outlive.
+emr_status mark_done(emr_networks& M, hipStream_t s) {
+  if (!M.done) NET_HIP(hipEventCreateWithFlags(&M.done, hipEventDisableTiming));
+  NET_HIP(hipEventRecord(M.done, s));
+  M.done_pending = true;
+  return EMR_OK;
+}
+
+// patterns: on the host, or (with `kept`, whose codes may be NULL) on the device.
+emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_patterns,
+                       int32_t steps, float* outputs, float* fitness, const float* targets,
+                       hipStream_t s, const emr::NetKept* kept = nullptr) {
+  emr_networks& M = const_cast<emr_networks&>(*N);
+  NET_TRY(check_device(N));
   const int64_t pblocks = (n_patterns + 3) / 4;
   if (pblocks * (N->nodes ? N->nodes : 1) > ((int64_t)1 << 40))
     return failf(EMR_E_LIMIT, "networks: too many nodes x patterns");
@@ -901,8 +922,8 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
     list.count[0] = list.total;
   }
   // (few patterns of stepwise kernels alone are the initial state's arguments: a launch fewer)
-  const bool by_value = list.order == nullptr && n_pat <= emr::kNetStageFloats;
-  if (!by_value)
+  const bool by_value = !kept && list.order == nullptr && n_pat <= emr::kNetStageFloats;
+  if (!by_value && !kept)
     NET_TRY(stage_patterns(M, patterns, n_pat, targets, targets ? (size_t)n_patterns : 0, s));
   emr::NetRunArgs ra{};
   ra.order = N->order.as<uint32_t>();
@@ -911,7 +932,9 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
   ra.in_offset = N->in_offset.as<int64_t>();
   ra.in_src = N->in_src.as<uint32_t>();
   ra.in_w = N->in_w.as<float>();
-  ra.patterns = M.patterns.as<float>();
+  const float* dev_patterns = kept ? patterns : M.patterns.as<float>();
+  ra.patterns = dev_patterns;
+  if (kept) ra.kept = *kept;
   ra.targets = targets ? M.patterns.as<float>() + n_pat : nullptr;
   ra.out_node = N->d_out_node.as<int32_t>();
   ra.outputs = outputs;
@@ -964,8 +987,9 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
         left -= n;
       }
       emr::NetStateArgs sa{list, N->node_offset.as<int64_t>(), N->node_in.as<int32_t>(),
-                           by_value ? nullptr : M.patterns.as<float>(), buf[0], N->nodes,
-                           (uint32_t)N->n_in, (uint32_t)n_patterns, (uint32_t)pblocks, {}};
+                           by_value ? nullptr : dev_patterns, buf[0], N->nodes,
+                           (uint32_t)N->n_in, (uint32_t)n_patterns, (uint32_t)pblocks,
+                           kept ? *kept : emr::NetKept{}, {}};
       if (by_value) std::memcpy(sa.v, patterns, n_pat * 4);
       NET_HIP(emr_launch_net(9, &sa, s));
       int cur = 0;
@@ -973,7 +997,7 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
         emr::NetStepArgs st{list, N->node_offset.as<int64_t>(), N->node_in.as<int32_t>(),
                             N->in_offset.as<int64_t>(), N->in_src.as<uint32_t>(),
                             N->in_w.as<float>(), buf[cur], buf[cur ^ 1], N->nodes,
-                            (uint32_t)pblocks};
+                            (uint32_t)pblocks, kept ? *kept : emr::NetKept{}, (uint32_t)t};
         NET_HIP(emr_launch_net(10, &st, s));
       }
       emr::NetOutArgs oa{};
@@ -990,24 +1014,120 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
       NET_HIP(emr_launch_net(11, &oa, s));
     }
   }
-  if (!M.done) NET_HIP(hipEventCreateWithFlags(&M.done, hipEventDisableTiming));
-  NET_HIP(hipEventRecord(M.done, s));
-  M.done_pending = true;
+  return mark_done(M, s);
+}
+
+// Bytes of the codes that `steps` steps on n_patterns patterns keep, and their layout.
+emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps, uint8_t* codes,
+                       emr::NetKept* K, int64_t* bytes) {
+  if (n_patterns < 1 || n_patterns > kMaxPatterns)
+    return failf(EMR_E_INVAL, "networks: n_patterns %d outside [1, %d]", n_patterns, kMaxPatterns);
+  if (steps < 0 || steps > kMaxSteps)
+    return failf(EMR_E_INVAL, "networks: steps %d outside [0, %d]", steps, kMaxSteps);
+  K->q = emr::net_kept_q((uint32_t)n_patterns);
+  K->blocks = ((uint32_t)n_patterns + 4 * K->q - 1) / (4 * K->q);
+  K->planes = steps > 0 ? (uint32_t)steps - 1 : 0;
+  K->codes = codes;
+  const double all = (double)K->planes * K->blocks * 4.0 * K->q * (double)N->nodes;
+  if (all > 9e15) return failf(EMR_E_LIMIT, "networks: too many steps x nodes x patterns to keep");
+  *bytes = (int64_t)K->planes * K->blocks * N->nodes * (4 * K->q);
   return EMR_OK;
 }
 
+// The edges by source, on the first call's stream.
+emr_status turn_edges(emr_networks& N, hipStream_t s) {
+  if (N.turned) return EMR_OK;
+  if (N.edges > (int64_t)UINT32_MAX) return failf(EMR_E_LIMIT, "networks: too many edges");
+  Dev key, skey, val, tmp;
+  const size_t e = (size_t)N.edges;
+  NET_TRY(alloc(N.edge_dst, e * 4, "edge destinations", s));
+  NET_TRY(alloc(N.out_offset, ((size_t)N.nodes + 1) * 8, "outgoing edge offsets", s));
+  NET_TRY(alloc(N.out_edge, e * 8, "outgoing edges", s));
+  NET_TRY(alloc(key, e * 4, "edge keys", s));
+  NET_TRY(alloc(skey, e * 4, "edge keys", s));
+  NET_TRY(alloc(val, e * 8, "edge values", s));
+  emr::NetTurnArgs a{N.in_offset.as<int64_t>(), N.in_src.as<uint32_t>(), key.as<uint32_t>(),
+                     val.as<uint64_t>(), N.edge_dst.as<uint32_t>(), skey.as<uint32_t>(),
+                     N.out_offset.as<int64_t>(), N.nodes, N.edges};
+  if (e > 0) {
+    NET_HIP(emr_launch_net(20, &a, s));
+    int bits = 1;
+    while (bits < 32 && ((uint64_t)1 << bits) < (uint64_t)N.nodes) ++bits;
+    size_t tb = 0;
+    NET_HIP(emr_net_sort(nullptr, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
+                         N.out_edge.as<uint64_t>(), (uint32_t)e, bits, s));
+    NET_TRY(alloc(tmp, tb, "sort storage", s));
+    NET_HIP(emr_net_sort(tmp.p, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
+                         N.out_edge.as<uint64_t>(), (uint32_t)e, bits, s));
+  }
+  NET_HIP(emr_launch_net(21, &a, s));
+  N.turned = true;
+  return EMR_OK;
+}
+
+emr_status run_backward(emr_networks& M, emr::NetBackArgs& A, int32_t steps, hipStream_t s) {
+  if (steps == 0) {  // the outputs are their initial states: nothing moves them
+    NET_HIP(emr_launch_net(25, &A, s));
+    return mark_done(M, s);
+  }
+  const size_t half = (size_t)A.pblocks * (size_t)(M.nodes ? M.nodes : 1) * 16;
+  if (!M.back.p || M.back.bytes < 2 * half) NET_TRY(alloc(M.back, 2 * half, "derivatives", s));
+  float* buf[2] = {M.back.as<float>(), reinterpret_cast<float*>(M.back.as<char>() + half)};
+  A.gz_before = buf[0];
+  NET_HIP(emr_launch_net(22, &A, s));
+  int cur = 0;
+  for (int32_t t = steps; t >= 1; --t, cur ^= 1) {
+    A.gz = buf[cur];
+    A.gz_before = buf[cur ^ 1];
+    A.step = (uint32_t)t;
+    A.last = t == steps ? 1u : 0u;
+    NET_HIP(emr_launch_net(23, &A, s));
+    NET_HIP(emr_launch_net(24, &A, s));
+  }
+  return mark_done(M, s);
+}
+
+// The handle's substrate: its inputs and outputs numbered in substrate order.
+emr_status set_substrate(emr_networks& N, const emr_source* substrate, int32_t n_substrate,
+                         int32_t depth) {
+  if (n_substrate < 1 || n_substrate > kMaxSubstrate)
+    return failf(EMR_E_INVAL, "networks: n_substrate %d outside [1, %d]", n_substrate,
+                 kMaxSubstrate);
+  N.n_sub = n_substrate;
+  N.depth = depth;
+  N.substrate.assign(substrate, substrate + n_substrate);
+  N.slots.assign((size_t)2 * n_substrate, -1);
+  for (int32_t j = 0; j < n_substrate; ++j) {
+    const emr_source& q = substrate[j];
+    if (q.dir != EMR_DIR_OUT && q.dir != EMR_DIR_IN)
+      return failf(EMR_E_INVAL, "networks: substrate source %d has direction %d", j, q.dir);
+    if (!std::isfinite(q.x) || !std::isfinite(q.y))
+      return failf(EMR_E_INVAL, "networks: substrate source %d is not finite", j);
+    if (q.dir == EMR_DIR_OUT) N.slots[j] = N.n_in++;
+    else N.slots[(size_t)n_substrate + j] = N.n_out++;
+  }
+  if (N.n_in == 0 || N.n_out == 0)
+    return failf(EMR_E_INVAL, "networks: the substrate needs an input and an output");
+  N.out_node.resize((size_t)N.n_out);
+  for (int32_t j = 0; j < n_substrate; ++j)
+    if (N.slots[(size_t)n_substrate + j] >= 0)
+      N.out_node[(size_t)N.slots[(size_t)n_substrate + j]] = j;
+  return EMR_OK;
+}
+
+emr_status upload_substrate(emr_networks& N, hipStream_t s) {
+  NET_TRY(alloc(N.d_slots, N.slots.size() * 4, "substrate slots", s));
+  NET_TRY(to_device(N.d_slots.p, N.slots.data(), N.slots.size() * 4, s));
+  NET_TRY(alloc(N.d_out_node, N.out_node.size() * 4, "output nodes", s));
+  return to_device(N.d_out_node.p, N.out_node.data(), N.out_node.size() * 4, s);
+}
+
 // Every phase and the assembly; synchronizes with the stream at the end.
-emr_status build_all(Build& B, int32_t n_substrate, int32_t iterations) {
+emr_status build_all(Build& B, int32_t iterations) {
   emr_networks& N = *B.net;
   NET_TRY(alloc(N.known, (size_t)N.n_genomes * (size_t)N.words * 4, "hidden-cell bitmaps", B.s));
   NET_HIP(hipMemsetAsync(N.known.p, 0, N.known.bytes, B.s));
-  NET_TRY(alloc(N.d_slots, N.slots.size() * 4, "substrate slots", B.s));
-  NET_TRY(to_device(N.d_slots.p, N.slots.data(), N.slots.size() * 4, B.s));
-  std::vector<int32_t> out_node((size_t)N.n_out);
-  for (int32_t j = 0; j < n_substrate; ++j)
-    if (N.slots[(size_t)n_substrate + j] >= 0) out_node[(size_t)N.slots[(size_t)n_substrate + j]] = j;
-  NET_TRY(alloc(N.d_out_node, out_node.size() * 4, "output nodes", B.s));
-  NET_TRY(to_device(N.d_out_node.p, out_node.data(), out_node.size() * 4, B.s));
+  NET_TRY(upload_substrate(N, B.s));
 
   N.phases.push_back(std::make_unique<Phase>());
   N.phases[0]->sources = N.substrate;
@@ -1027,6 +1147,32 @@ emr_status build_all(Build& B, int32_t n_substrate, int32_t iterations) {
   return EMR_OK;
 }
 
+static_assert(EMR_F32 == emr::kTypeF32 && EMR_BF16 == emr::kTypeBf16 && EMR_F16 == emr::kTypeF16, "");
+
+int64_t type_size(int32_t type) { return type == EMR_F32 ? 4 : 2; }
+
+emr_status check_scores(const char* who, const emr_scores* S) {
+  if (!S) return failf(EMR_E_INVAL, "%s: scores is NULL", who);
+  if (S->type != EMR_F32 && S->type != EMR_BF16 && S->type != EMR_F16)
+    return failf(EMR_E_INVAL, "%s: score type %d", who, S->type);
+  if (S->rows < 0 || S->n < 1)
+    return failf(EMR_E_INVAL, "%s: %lld rows of %lld scores", who, (long long)S->rows,
+                 (long long)S->n);
+  if (S->rows > INT32_MAX || S->n > INT32_MAX)
+    return failf(EMR_E_LIMIT, "%s: %lld rows of %lld scores (at most 2^31 - 1 each)", who,
+                 (long long)S->rows, (long long)S->n);
+  if (S->stride < 0 || S->stride > INT64_MAX / 4 / (S->rows > 0 ? S->rows : 1))
+    return failf(EMR_E_INVAL, "%s: row stride %lld", who, (long long)S->stride);
+  if (S->rows > 0 && (!S->x || (uintptr_t)S->x % (uintptr_t)type_size(S->type) != 0))
+    return failf(EMR_E_INVAL, "%s: scores NULL or not aligned to their type", who);
+  return EMR_OK;
+}
+
+// Whether groups of four entries of every row are aligned to their size.
+int32_t aligned4(const void* p, int64_t stride, int32_t type) {
+  return (uintptr_t)p % (uintptr_t)(4 * type_size(type)) == 0 && stride % 4 == 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1037,9 +1183,6 @@ emr_status emr_build_networks(const emr_population* pop, const emr_source* subst
   if (!out) return failf(EMR_E_INVAL, "networks: out is NULL");
   *out = nullptr;
   if (!pop || !substrate) return failf(EMR_E_INVAL, "networks: NULL population or substrate");
-  if (n_substrate < 1 || n_substrate > kMaxSubstrate)
-    return failf(EMR_E_INVAL, "networks: n_substrate %d outside [1, %d]", n_substrate,
-                 kMaxSubstrate);
   if (depth < 1 || depth > EMR_MAX_DEPTH)
     return failf(EMR_E_INVAL, "networks: depth %d outside [1, %d]", depth, EMR_MAX_DEPTH);
   if (type_mask < 1 || type_mask > EMR_CONN_ALL)
@@ -1051,27 +1194,13 @@ emr_status emr_build_networks(const emr_population* pop, const emr_source* subst
     return failf(EMR_E_INVAL, "networks: theta and w_min must not be NaN");
   auto net = std::make_unique<emr_networks>();
   emr_networks& N = *net;
-  N.n_sub = n_substrate;
-  N.depth = depth;
-  N.substrate.assign(substrate, substrate + n_substrate);
-  N.slots.assign((size_t)2 * n_substrate, -1);
-  for (int32_t j = 0; j < n_substrate; ++j) {
-    const emr_source& q = substrate[j];
-    if (q.dir != EMR_DIR_OUT && q.dir != EMR_DIR_IN)
-      return failf(EMR_E_INVAL, "networks: substrate source %d has direction %d", j, q.dir);
-    if (!std::isfinite(q.x) || !std::isfinite(q.y))
-      return failf(EMR_E_INVAL, "networks: substrate source %d is not finite", j);
-    if (q.dir == EMR_DIR_OUT) N.slots[j] = N.n_in++;
-    else N.slots[(size_t)n_substrate + j] = N.n_out++;
-  }
-  if (N.n_in == 0 || N.n_out == 0)
-    return failf(EMR_E_INVAL, "networks: the substrate needs an input and an output");
+  NET_TRY(set_substrate(N, substrate, n_substrate, depth));
   NET_TRY(emr_population_info(pop, &N.n_genomes, nullptr, nullptr, nullptr));
   if (N.n_genomes < 1) return failf(EMR_E_INVAL, "networks: empty population");
   NET_HIP(hipGetDevice(&N.device));
   NET_TRY(emr_cell_words(depth, &N.words));
   Build B{pop, &N, theta, type_mask, w_min, (hipStream_t)stream};
-  const emr_status st = build_all(B, n_substrate, iterations);
+  const emr_status st = build_all(B, iterations);
   // after a failure, nothing queued may still use the buffers the handle gives back
   if (st != EMR_OK) {
     (void)hipStreamSynchronize(B.s);
@@ -1152,6 +1281,241 @@ emr_status emr_xor_fitness(const emr_networks* net, int32_t bias_input, int32_t 
     for (int j = 0; j < net->n_in; ++j) pat[(size_t)p * net->n_in + j] = j == bias_input ? 1.f : ab[p][c++];
   }
   return run_forward(net, pat.data(), 4, steps, nullptr, fitness, target, (hipStream_t)stream);
+}
+
+emr_status emr_load_networks(const emr_source* substrate, int32_t n_substrate, int32_t depth,
+                             int32_t n_genomes, const int64_t* node_offset, const uint32_t* node_cell,
+                             const int64_t* in_offset, const uint32_t* in_src, const float* in_w,
+                             emr_networks** out, void* stream) try {
+  if (!out) return failf(EMR_E_INVAL, "networks: out is NULL");
+  *out = nullptr;
+  if (!substrate || !node_offset || !in_offset)
+    return failf(EMR_E_INVAL, "networks: NULL argument");
+  if (depth < 0 || depth > EMR_MAX_DEPTH)
+    return failf(EMR_E_INVAL, "networks: depth %d outside [0, %d]", depth, EMR_MAX_DEPTH);
+  if (n_genomes < 1) return failf(EMR_E_INVAL, "networks: %d genomes", n_genomes);
+  auto net = std::make_unique<emr_networks>();
+  emr_networks& N = *net;
+  NET_TRY(set_substrate(N, substrate, n_substrate, depth));
+  N.n_genomes = n_genomes;
+  const size_t G = (size_t)n_genomes;
+  if (node_offset[0] != 0) return failf(EMR_E_INVAL, "networks: node_offset[0] is not 0");
+  for (size_t g = 0; g < G; ++g)
+    if (node_offset[g + 1] < node_offset[g] || node_offset[g + 1] - node_offset[g] < n_substrate)
+      return failf(EMR_E_INVAL, "networks: genome %zu has fewer nodes than the substrate", g);
+  N.nodes = node_offset[G];
+  if (N.nodes > (int64_t)UINT32_MAX - 1)
+    return failf(EMR_E_LIMIT, "networks: %lld nodes", (long long)N.nodes);
+  if (in_offset[0] != 0) return failf(EMR_E_INVAL, "networks: in_offset[0] is not 0");
+  N.edges = in_offset[N.nodes];
+  if (N.edges < 0 || (N.edges > 0 && (!in_src || !in_w)))
+    return failf(EMR_E_INVAL, "networks: in_src or in_w is NULL");
+  std::vector<int32_t> node_in((size_t)N.nodes, -1);
+  std::vector<uint32_t> cells((size_t)N.nodes, 0);
+  std::vector<int64_t> edge_off(G + 1);
+  for (size_t g = 0; g < G; ++g) {
+    const int64_t a = node_offset[g], b = node_offset[g + 1];
+    for (int32_t j = 0; j < n_substrate; ++j) {
+      node_in[(size_t)(a + j)] = N.slots[(size_t)j];
+      cells[(size_t)(a + j)] = EMR_SUBSTRATE_NODE;
+    }
+    for (int64_t i = a; i < b; ++i) {
+      if (in_offset[i + 1] < in_offset[i] || in_offset[i + 1] > N.edges)
+        return failf(EMR_E_INVAL, "networks: in_offset falls at node %lld", (long long)i);
+      if (node_in[(size_t)i] >= 0 && in_offset[i + 1] != in_offset[i])
+        return failf(EMR_E_INVAL, "networks: input node %lld has incoming edges", (long long)i);
+      if (node_cell && i - a >= n_substrate) cells[(size_t)i] = node_cell[i];
+      for (int64_t e = in_offset[i]; e < in_offset[i + 1]; ++e)
+        if ((int64_t)in_src[e] < a || (int64_t)in_src[e] >= b)
+          return failf(EMR_E_INVAL, "networks: edge %lld leaves its genome", (long long)e);
+    }
+    edge_off[g] = in_offset[a];
+  }
+  edge_off[G] = N.edges;
+  NET_HIP(hipGetDevice(&N.device));
+  hipStream_t s = (hipStream_t)stream;
+  const emr_status st = [&]() -> emr_status {
+    NET_TRY(upload_substrate(N, s));
+    const struct { Dev* d; const void* src; size_t bytes; const char* what; } up[] = {
+        {&N.node_offset, node_offset, (G + 1) * 8, "node offsets"},
+        {&N.node_cell, cells.data(), cells.size() * 4, "network nodes"},
+        {&N.node_in, node_in.data(), node_in.size() * 4, "network input numbers"},
+        {&N.in_offset, in_offset, ((size_t)N.nodes + 1) * 8, "network edge offsets"},
+        {&N.in_src, in_src, (size_t)N.edges * 4, "network edges"},
+        {&N.in_w, in_w, (size_t)N.edges * 4, "network edges"}};
+    for (const auto& u : up) {
+      NET_TRY(alloc(*u.d, u.bytes, u.what, s));
+      NET_TRY(to_device(u.d->p, u.src, u.bytes, s));
+    }
+    NET_TRY(order_genomes(N, node_offset, edge_off.data(), s));
+    NET_HIP(hipStreamSynchronize(s));
+    return EMR_OK;
+  }();
+  if (st != EMR_OK) {
+    (void)hipStreamSynchronize(s);
+    return st;
+  }
+  *out = net.release();
+  return EMR_OK;
+} catch (const std::bad_alloc&) {
+  return failf(EMR_E_NOMEM, "networks: out of host memory");
+}
+
+emr_status emr_networks_set_weights(const emr_networks* net, const float* w, void* stream) {
+  if (!net || (!w && net->edges > 0)) return failf(EMR_E_INVAL, "networks: NULL argument");
+  NET_TRY(check_device(net));
+  emr_networks& M = const_cast<emr_networks&>(*net);
+  hipStream_t s = (hipStream_t)stream;
+  if (net->edges > 0)
+    NET_HIP(hipMemcpyAsync(M.in_w.p, w, (size_t)net->edges * 4, hipMemcpyDeviceToDevice, s));
+  return mark_done(M, s);
+}
+
+emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes) {
+  if (!net || !bytes) return failf(EMR_E_INVAL, "networks: NULL argument");
+  emr::NetKept K{};
+  return kept_layout(net, n_patterns, steps, nullptr, &K, bytes);
+}
+
+emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32_t n_patterns,
+                             int32_t steps, float* outputs, uint8_t* kept, int64_t kept_bytes,
+                             void* stream) {
+  if (!net || !inputs || !outputs) return failf(EMR_E_INVAL, "networks: NULL argument");
+  emr::NetKept K{};
+  int64_t need = 0;
+  NET_TRY(kept_layout(net, n_patterns, steps, kept, &K, &need));
+  if (need > 0 && (!kept || (uintptr_t)kept % 16 != 0))
+    return failf(EMR_E_INVAL, "networks: kept is NULL or not aligned to 16 bytes");
+  if (kept_bytes < need)
+    return failf(EMR_E_CAPACITY, "networks: kept holds %lld bytes of %lld", (long long)kept_bytes,
+                 (long long)need);
+  if (need == 0) K.codes = nullptr;
+  return run_forward(net, inputs, n_patterns, steps, outputs, nullptr, nullptr, (hipStream_t)stream,
+                     &K);
+}
+
+emr_status emr_activate_backward(const emr_networks* net, const float* inputs, int32_t n_patterns,
+                                 int32_t steps, const float* outputs, const uint8_t* kept,
+                                 int64_t kept_bytes, const float* grad_outputs, float* grad_w,
+                                 float* grad_inputs, void* stream) try {
+  if (!net || !inputs || !outputs || !grad_outputs || !grad_w)
+    return failf(EMR_E_INVAL, "networks: NULL argument");
+  emr::NetBackArgs A{};
+  int64_t need = 0;
+  NET_TRY(kept_layout(net, n_patterns, steps, const_cast<uint8_t*>(kept), &A.kept, &need));
+  if (need > 0 && (!kept || (uintptr_t)kept % 16 != 0))
+    return failf(EMR_E_INVAL, "networks: kept is NULL or not aligned to 16 bytes");
+  if (kept_bytes < need)
+    return failf(EMR_E_CAPACITY, "networks: kept holds %lld bytes of %lld", (long long)kept_bytes,
+                 (long long)need);
+  NET_TRY(check_device(net));
+  emr_networks& M = const_cast<emr_networks&>(*net);
+  hipStream_t s = (hipStream_t)stream;
+  A.pblocks = ((uint32_t)n_patterns + 3) / 4;
+  if ((int64_t)A.pblocks * (net->nodes ? net->nodes : 1) > ((int64_t)1 << 40))
+    return failf(EMR_E_LIMIT, "networks: too many nodes x patterns");
+  NET_TRY(turn_edges(M, s));
+  A.node_offset = net->node_offset.as<int64_t>();
+  A.node_in = net->node_in.as<int32_t>();
+  A.out_node = net->d_out_node.as<int32_t>();
+  A.in_offset = net->in_offset.as<int64_t>();
+  A.in_src = net->in_src.as<uint32_t>();
+  A.in_w = net->in_w.as<float>();
+  A.dst = net->edge_dst.as<uint32_t>();
+  A.out_offset = net->out_offset.as<int64_t>();
+  A.out_edge = net->out_edge.as<uint64_t>();
+  A.patterns = inputs;
+  A.outputs = outputs;
+  A.grad_outputs = grad_outputs;
+  A.grad_w = grad_w;
+  A.grad_inputs = grad_inputs;
+  A.nodes = net->nodes;
+  A.edges = net->edges;
+  A.n_genomes = (uint32_t)net->n_genomes;
+  A.n_inputs = (uint32_t)net->n_in;
+  A.n_outputs = (uint32_t)net->n_out;
+  A.n_patterns = (uint32_t)n_patterns;
+  return run_backward(M, A, steps, s);
+} catch (const std::bad_alloc&) {
+  return failf(EMR_E_NOMEM, "networks: out of host memory");
+}
+
+emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const float* u, int64_t draws,
+                      int32_t* index, float* logp, void* stream) {
+  const emr_status st = check_scores("sample", scores);
+  if (st != EMR_OK) return st;
+  if (!rule) return failf(EMR_E_INVAL, "sample: rule is NULL");
+  if (!rule->row_temperature && !(rule->temperature >= 0.0f))
+    return failf(EMR_E_INVAL, "sample: temperature %g is not at least 0", (double)rule->temperature);
+  if (!rule->row_top_k && rule->top_k < 0)
+    return failf(EMR_E_INVAL, "sample: top_k %d is negative", rule->top_k);
+  if (!rule->row_top_p && !(rule->top_p > 0.0f && rule->top_p <= 1.0f))
+    return failf(EMR_E_INVAL, "sample: top_p %g outside (0, 1]", (double)rule->top_p);
+  if (!rule->row_min_p && !(rule->min_p >= 0.0f && rule->min_p <= 1.0f))
+    return failf(EMR_E_INVAL, "sample: min_p %g outside [0, 1]", (double)rule->min_p);
+  if (draws < 0 || draws > INT64_MAX / 8 / (scores->rows > 0 ? scores->rows : 1))
+    return failf(EMR_E_INVAL, "sample: %lld draws", (long long)draws);
+  if (scores->rows == 0 || draws == 0) return EMR_OK;
+  if (!u || !index) return failf(EMR_E_INVAL, "sample: u or index is NULL");
+  emr::SampleArgs a{};
+  a.x = scores->x;
+  a.stride = scores->stride;
+  a.rows = scores->rows;
+  a.n = (uint32_t)scores->n;
+  a.type = scores->type;
+  a.vec = aligned4(scores->x, scores->stride, scores->type);
+  a.t = rule->temperature;
+  a.p = rule->top_p;
+  a.min_p = rule->min_p;
+  a.k = rule->top_k;
+  a.row_t = rule->row_temperature;
+  a.row_k = rule->row_top_k;
+  a.row_p = rule->row_top_p;
+  a.row_min_p = rule->row_min_p;
+  a.u = u;
+  a.draws = draws;
+  a.index = index;
+  a.logp = logp;
+  const uint32_t groups = (a.n + emr::kDrawPart - 1) / emr::kDrawPart;
+  a.part = (groups + emr::kDrawSegs - 1) / emr::kDrawSegs * emr::kDrawPart;
+  const hipError_t e = emr_launch_net(30, &a, (hipStream_t)stream);
+  if (e != hipSuccess) return failf(EMR_E_DEVICE, "sample: %s", hipGetErrorString(e));
+  return EMR_OK;
+}
+
+emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const float* scale,
+                           float temperature, float* loss, void* grad, int64_t grad_stride,
+                           void* stream) {
+  const emr_status st = check_scores("loss", scores);
+  if (st != EMR_OK) return st;
+  if (!(temperature >= 1.17549435e-38f && std::isfinite(temperature)))
+    return failf(EMR_E_INVAL, "loss: temperature %g is not a positive normal number",
+                 (double)temperature);
+  if (scores->rows == 0) return EMR_OK;
+  if (!loss && !grad) return failf(EMR_E_INVAL, "loss: neither loss nor grad is asked for");
+  if (grad && (grad_stride < scores->n || grad_stride > INT64_MAX / 4 / (scores->rows + 1)))
+    return failf(EMR_E_INVAL, "loss: grad's row stride %lld is below %lld scores",
+                 (long long)grad_stride, (long long)scores->n);
+  if (grad && (uintptr_t)grad % (uintptr_t)type_size(scores->type) != 0)
+    return failf(EMR_E_INVAL, "loss: grad is not aligned to its type");
+  if (!index) return failf(EMR_E_INVAL, "loss: index is NULL");
+  emr::LossArgs a{};
+  a.x = scores->x;
+  a.stride = scores->stride;
+  a.rows = scores->rows;
+  a.n = (uint32_t)scores->n;
+  a.type = scores->type;
+  a.vec = aligned4(scores->x, scores->stride, scores->type) &&
+          (!grad || aligned4(grad, grad_stride, scores->type));
+  a.inv_t = 1.0f / temperature;
+  a.index = index;
+  a.scale = scale;
+  a.loss = loss;
+  a.grad = grad;
+  a.grad_stride = grad_stride;
+  const hipError_t e = emr_launch_net(31, &a, (hipStream_t)stream);
+  if (e != hipSuccess) return failf(EMR_E_DEVICE, "loss: %s", hipGetErrorString(e));
+  return EMR_OK;
 }
 
 emr_status emr_copy_to_host(void* host, const void* device, int64_t bytes, void* stream) {

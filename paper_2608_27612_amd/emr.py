@@ -32,7 +32,8 @@ ABI_FUNCTIONS = [
     "emr_band_values", "emr_band_filter", "emr_record_file_open",
     "emr_record_file_sink", "emr_record_file_close", "emr_build_networks", "emr_networks_info",
     "emr_networks_phase", "emr_activate", "emr_xor_fitness", "emr_free_networks",
-    "emr_copy_to_host", "emr_sample", "emr_answer_loss",
+    "emr_copy_to_host", "emr_sample", "emr_answer_loss", "emr_load_networks",
+    "emr_networks_set_weights", "emr_kept_bytes", "emr_activate_keep", "emr_activate_backward",
 ]
 EMR_CONN_FORWARD, EMR_CONN_BACKWARD, EMR_CONN_LATERAL, EMR_CONN_SELF, EMR_CONN_ALL = 1, 2, 4, 8, 15
 EMR_F32, EMR_BF16, EMR_F16 = 0, 1, 2
@@ -169,6 +170,11 @@ def lib():
             "emr_xor_fitness": (I32, [P, I32, I32, P, P]),
             "emr_free_networks": (None, [P]),
             "emr_copy_to_host": (I32, [P, P, I64, P]),
+            "emr_load_networks": (I32, [P, I32, I32, I32, P, P, P, P, P, P, P]),
+            "emr_networks_set_weights": (I32, [P, P, P]),
+            "emr_kept_bytes": (I32, [P, I32, I32, P]),
+            "emr_activate_keep": (I32, [P, P, I32, I32, P, P, I64, P]),
+            "emr_activate_backward": (I32, [P, P, I32, I32, P, P, I64, P, P, P, P]),
             "emr_sample": (I32, [P, P, P, I64, P, P, P]),
             "emr_answer_loss": (I32, [P, P, P, F32, P, P, I64, P]),
         }
@@ -1014,6 +1020,127 @@ class Networks:
         _check(lib().emr_xor_fitness(self.handle, -1 if bias_input is None else int(bias_input),
                                      steps, C.c_void_p(out.data_ptr()), _stream_ptr(stream)))
         return out
+
+    def set_weights(self, w, stream=None):
+        """The weight of every edge (a float32 device tensor in the order of in_w) for later calls."""
+        import torch
+        with _on(stream):
+            w = _on_device("w", w, torch.float32, (self.info().edges,)).contiguous()
+            _check(lib().emr_networks_set_weights(self.handle, C.c_void_p(w.data_ptr()),
+                                                  _stream_ptr(stream)))
+
+    def weights(self, stream=None):
+        """A copy of the edges' weights (numpy, in the order of in_w)."""
+        i = self.info()
+        return _dev_to_host(i.in_w, i.edges, np.float32, stream)
+
+    def _patterns(self, inputs, info):
+        import torch
+        _on_device("inputs", inputs, torch.float32)
+        if inputs.dim() != 2 or inputs.shape[1] != info.n_inputs:
+            raise ValueError("inputs: shape (patterns, %d) is needed, not %s"
+                             % (info.n_inputs, tuple(inputs.shape)))
+        return inputs.contiguous()
+
+    def activate_keep(self, inputs, steps: int, stream=None):
+        """Outputs (float32 device tensor [n_genomes, n_patterns, n_outputs]) of emr_activate_keep for
+        `inputs` (float32 device tensor [n_patterns, n_inputs]), and the Kept states; not synchronized."""
+        import torch
+        with _on(stream):
+            i = self.info()
+            x = self._patterns(inputs, i)
+            P = x.shape[0]
+            n = C.c_int64()
+            _check(lib().emr_kept_bytes(self.handle, P, steps, C.byref(n)))
+            out = torch.empty((i.n_genomes, P, i.n_outputs), dtype=torch.float32, device=x.device)
+            b = _kept_width(P)
+            codes = torch.empty((max(steps - 1, 0), -(-P // b), i.nodes, b), dtype=torch.uint8,
+                                device=x.device)
+            assert codes.numel() == n.value
+            _check(lib().emr_activate_keep(self.handle, C.c_void_p(x.data_ptr()), P, steps,
+                                           C.c_void_p(out.data_ptr()), C.c_void_p(codes.data_ptr()),
+                                           n.value, _stream_ptr(stream)))
+            return out, Kept(codes, P)
+
+    def activate_backward(self, inputs, steps: int, outputs, kept, grad_outputs, grad_inputs: bool = False,
+                          stream=None):
+        """Derivatives by the weights (float32 device tensor [edges], in the order of in_w) and, with
+        grad_inputs, by each genome's patterns ([n_genomes, n_patterns, n_inputs], else None), from
+        activate_keep's inputs, outputs and Kept and the derivatives by the outputs; see
+        emr_activate_backward in include/emr.h. Not synchronized."""
+        import torch
+        with _on(stream):
+            i = self.info()
+            x = self._patterns(inputs, i)
+            P = x.shape[0]
+            shape = (i.n_genomes, P, i.n_outputs)
+            outputs = _on_device("outputs", outputs, torch.float32, shape).contiguous()
+            grad_outputs = _on_device("grad_outputs", grad_outputs, torch.float32, shape).contiguous()
+            b = _kept_width(P)
+            codes = _on_device("kept", kept.codes, torch.uint8,
+                               (max(steps - 1, 0), -(-P // b), i.nodes, b)).contiguous()
+            grad_w = torch.empty(i.edges, dtype=torch.float32, device=x.device)
+            grad_x = torch.empty((i.n_genomes, P, i.n_inputs), dtype=torch.float32,
+                                 device=x.device) if grad_inputs else None
+            # (a network without edges has no memory for them: any address will do)
+            _check(lib().emr_activate_backward(
+                self.handle, C.c_void_p(x.data_ptr()), P, steps, C.c_void_p(outputs.data_ptr()),
+                C.c_void_p(codes.data_ptr()), codes.numel(), C.c_void_p(grad_outputs.data_ptr()),
+                C.c_void_p(grad_w.data_ptr() or x.data_ptr()),
+                C.c_void_p(0 if grad_x is None else grad_x.data_ptr()), _stream_ptr(stream)))
+            return grad_w, grad_x
+
+
+def _kept_width(patterns: int) -> int:
+    return 4 if patterns <= 4 else 8 if patterns <= 8 else 16
+
+
+class Kept:
+    """The states that Networks.activate_keep keeps: codes (uint8 device tensor [steps - 1, blocks, nodes,
+    b]), of which c stands for the state c / 255."""
+
+    def __init__(self, codes, patterns: int):
+        self.codes, self.patterns = codes, patterns
+
+    def values(self, dtype=None):
+        """The states, [steps - 1, nodes, patterns] (a strided view)."""
+        import torch
+        t, blocks, nodes, b = self.codes.shape
+        out = torch.empty((t, nodes, blocks, b), dtype=dtype or torch.float32, device=self.codes.device)
+        torch.mul(self.codes.transpose(1, 2), 1.0 / 255.0, out=out)
+        return out.view(t, nodes, blocks * b)[:, :, :self.patterns]
+
+
+def kept_from_codes(codes) -> Kept:
+    """Kept of codes (uint8 device tensor [steps - 1, nodes, patterns])."""
+    import torch
+    t, nodes, P = codes.shape
+    b = _kept_width(P)
+    full = torch.zeros((t, nodes, -(-P // b) * b), dtype=torch.uint8, device=codes.device)
+    full[:, :, :P] = codes
+    return Kept(full.view(t, nodes, -1, b).transpose(1, 2).contiguous(), P)
+
+
+def emr_load_networks(substrate, node_offset, in_offset, in_src, in_w, node_cell=None, depth: int = 0,
+                      stream=None) -> Networks:
+    """Networks from host arrays (see emr_load_networks in include/emr.h; synchronizing). substrate: the
+    shared sources, inputs outgoing, outputs incoming, as records or a list of (x, y, dir)."""
+    src = _sources([dict(zip(("x", "y", "dir"), q)) if isinstance(q, tuple) else q for q in substrate]
+                   if isinstance(substrate, list) else substrate)
+    a = [np.ascontiguousarray(node_offset, np.int64), np.ascontiguousarray(in_offset, np.int64),
+         np.ascontiguousarray(in_src, np.uint32), np.ascontiguousarray(in_w, np.float32)]
+    if len(a[0]) < 1 or len(a[1]) != a[0][-1] + 1 or not len(a[2]) == len(a[3]) == a[1][-1]:
+        raise ValueError("networks: arrays of different lengths")
+    cells = None
+    if node_cell is not None:
+        cells = np.ascontiguousarray(node_cell, np.uint32)
+        if len(cells) != a[0][-1]:
+            raise ValueError("networks: arrays of different lengths")
+    h = C.c_void_p()
+    _check(lib().emr_load_networks(src.ctypes.data, len(src), depth, len(a[0]) - 1, a[0].ctypes.data,
+                                   None if cells is None else cells.ctypes.data, a[1].ctypes.data,
+                                   a[2].ctypes.data, a[3].ctypes.data, C.byref(h), _stream_ptr(stream)))
+    return Networks(h)
 
 
 def emr_build_networks(pop: Population, substrate, depth: int, theta: float, type_mask: int,
