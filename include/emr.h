@@ -526,9 +526,9 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
 
 /*
  * Learning the weights. emr_activate_keep is emr_activate with the patterns on the device (inputs,
- * [n_patterns][n_inputs], caller-owned) and the same outputs, bit for bit, that also keeps every step's
- * states in 8 bits; emr_activate_backward takes them to the derivatives of a loss by the weights
- * (grad_w, device, [edges]) and, where grad_inputs (device, [n_genomes][n_patterns][n_inputs]) is not
+ * [n_patterns][n_inputs], caller-owned) that also keeps every step's states in 8 bits (its sums, in fp32
+ * as well, run in another order: the outputs differ from emr_activate's by their rounding);
+ * emr_activate_backward takes them to the derivatives of a loss by the weights (grad_w, device, [edges]) and, where grad_inputs (device, [n_genomes][n_patterns][n_inputs]) is not
  * NULL, by each genome's copy of the patterns, from those by the outputs (grad_outputs, device,
  * [n_genomes][n_patterns][n_outputs]).
  *   - kept (device, caller-owned, emr_kept_bytes of it, aligned to 16 bytes): code c = rint(255 s) stands
@@ -542,8 +542,10 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  *     order, so a handle's gradients are the same bits on every call.
  *   - A weight that `steps` steps do not let reach an output has derivative 0. A node that no derivative
  *     reaches adds nothing, whatever its states.
- * Enqueued on `stream`, but for the first backward call of a handle, which lays the edges out by source
- * (allocations, so not under capture). Calls on one handle must be ordered on one stream, as emr_activate's.
+ * Enqueued on `stream`, but for a handle's first call of the two, and its first on a number of patterns (of
+ * the last 64 such numbers), which lay out edges and work and wait for the stream: not under capture. A call
+ * on more patterns than before may replace buffers that a captured call uses: capture after it. Calls on
+ * one handle must be ordered on one stream, as emr_activate's.
  * EMR_E_INVAL, EMR_E_CAPACITY (kept_bytes too small), EMR_E_LIMIT, EMR_E_NOMEM, EMR_E_DEVICE.
  */
 emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes);

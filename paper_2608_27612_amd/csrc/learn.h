@@ -1,0 +1,166 @@
+// Arguments of the learning kernels (learn.hip), shared with their host driver (networks.cpp).
+//
+// Rows. A genome's edges are laid out four times, by destination ("in") and by source ("out"), the ones
+// from input nodes apart from the others ("inp", "hid"): an input holds still over the steps, so its edges
+// count once where the others count in every step. A row is a node with its edges of one kind. Rows
+// lie in slices of sixteen places:
+//   - a light slice holds sixteen rows, the edge k of its row r at base + 16 k + r, so that the
+//     lanes of a wave, a row each, read sixteen edges side by side; rows come in falling order of
+//     edges, which leaves few places empty;
+//   - a heavy slice holds one row of many edges (more than kLightEdges; the output nodes of "in" always),
+//     its edge k at base + k: sixteen lanes share it and add their sums at the end.
+// An empty place has the weight 0 and, as the other node, the one past the genome's last, whose values
+// are zeros.
+#pragma once
+#include <stdint.h>
+
+#include "network.h"
+
+namespace emr {
+
+// Gradients. The edges a second time, grouped by their source.
+struct NetTurnArgs {
+  const int64_t* in_offset;  // [nodes + 1]
+  const uint32_t* in_src;    // [edges]
+  uint32_t* key;             // [edges] source
+  uint64_t* val;             // [edges] edge | destination << 32
+  uint32_t* dst;             // [edges] destination
+  const uint32_t* skey;      // sorted by source, each group in edge order
+  int64_t* out_offset;       // [nodes + 1]
+  int64_t nodes, edges;
+};
+
+// A genome that does not fit a workgroup: a launch per step, derivatives by the node sums ("gz") as
+// [pblocks][its nodes] float4.
+struct NetBackArgs {
+  uint32_t genome;
+  int64_t node0, size;         // its nodes
+  int64_t edge0, edge1;        // its edges
+  const int32_t* node_in;
+  const int32_t* out_node;     // [n_outputs]
+  const int64_t* in_offset;
+  const uint32_t* in_src;
+  const float* in_w;
+  const uint32_t* dst;         // [edges]
+  const int64_t* out_offset;   // [nodes + 1]
+  const uint64_t* out_edge;    // [edges] edge | destination << 32
+  const float* patterns;       // [n_patterns * n_inputs]
+  const float* outputs;        // [n_genomes * n_patterns * n_outputs]
+  const float* grad_outputs;   // the same
+  const float* gz;             // derivatives after the step
+  float* gz_before;            // before it
+  float* grad_w;               // [edges]
+  float* grad_inputs;          // [n_genomes * n_patterns * n_inputs] or NULL
+  NetKept kept;
+  int64_t nodes;               // of all genomes
+  uint32_t n_inputs, n_outputs, n_patterns;
+  uint32_t pblocks;
+  uint32_t step;               // 1 .. steps: the step whose derivatives gz holds
+  uint32_t last;               // whether it is the first one looked at: gradients are set, not added to
+};
+
+constexpr uint32_t kLightEdges = 64;
+constexpr int kInHid = 0, kInInp = 1, kOutHid = 2, kOutInp = 3, kSets = 4;
+constexpr uint32_t kNoEdge = 0xFFFFFFFFu;
+
+struct LearnSlice {
+  uint32_t base;   // first place, from the genome's on
+  uint32_t len;    // sixteens of places
+  uint32_t first;  // (out) the sixteens that reach output nodes, which come first in a row
+  uint32_t heavy;
+};
+
+// One of the four layouts; a genome's places start at place[g], its slices at slice[g].
+struct LearnSet {
+  uint2* ent;          // other node (local) | weight bits
+  uint32_t* edge;      // edge number, or kNoEdge
+  LearnSlice* slices;
+  uint16_t* rows;      // [slice * 16] local nodes (heavy: the same one), kNoRow: none
+  uint32_t* n_slices;  // [n_genomes]
+  uint32_t* n_places;  // [n_genomes]
+};
+constexpr uint32_t kNoRow = 0xFFFFu;
+
+// Nodes that fit a workgroup: three arrays of at least four patterns of floats, and one node more.
+constexpr uint32_t kLearnLds = 160u * 1024u;
+inline constexpr uint32_t learn_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 48u * groups; }
+constexpr uint32_t kLearnNodes = kLearnLds / 48u - 1u;
+
+// Places and slices of one of a genome's layouts, at most: a heavy row or an output leaves up to fifteen
+// places empty; falling rows of at most min(kLightEdges, e) edges leave sixteen times that.
+inline constexpr int64_t learn_places(int64_t e, int64_t n_out) {
+  return (e + e / 4 + 15 * n_out + 16 * (e < (int64_t)kLightEdges ? e : (int64_t)kLightEdges) + 31) / 16 * 16;
+}
+inline constexpr int64_t learn_slices(int64_t n, int64_t e, int64_t n_out) {
+  return n / 16 + 2 + e / kLightEdges + n_out;
+}
+
+struct LearnLayoutArgs {
+  LearnSet set[kSets];
+  const uint32_t* genomes;     // [count]
+  const int64_t* place;        // [n_genomes]
+  const int64_t* slice;        // [n_genomes]
+  const int64_t* node_offset;
+  const int32_t* node_in;
+  const int32_t* out_node;
+  const int64_t* in_offset;
+  const uint32_t* in_src;
+  const float* in_w;
+  const int64_t* out_offset;
+  const uint64_t* out_edge;    // [edges] edge | destination << 32
+  uint32_t count, n_outputs, n_sub;
+};
+
+// The weights of laid out places, after the edges' changed.
+struct LearnWeightsArgs {
+  LearnSet set[kSets];
+  const uint32_t* genomes;
+  const int64_t* place;
+  const float* in_w;
+  uint32_t count;
+};
+
+// A workgroup's share: patterns blocks b0 .. b1 - 1 of 4 `groups` patterns of one genome. The weights'
+// derivatives of its share are summed at partial + part (places of kOutHid, then of kOutInp).
+struct LearnItem {
+  uint32_t genome, b0, b1, groups;
+  int64_t part;
+  uint32_t alone;     // the genome has no other item: its derivatives go to grad_w directly
+  uint32_t pad;
+};
+
+// The genomes of more than one item.
+struct LearnJoin {
+  uint32_t genome, items;
+  int64_t part, stride;  // its items' partial sums
+};
+
+struct LearnFillArgs {
+  float* p;
+  int64_t n;
+};
+
+struct LearnArgs {
+  LearnSet set[kSets];
+  const LearnItem* items;
+  const LearnJoin* joins;
+  const int64_t* place;
+  const int64_t* slice;
+  const int64_t* node_offset;
+  const int32_t* node_in;
+  const int32_t* out_node;
+  const float* patterns;       // [n_patterns * n_inputs]
+  float* outputs;              // [n_genomes * n_patterns * n_outputs] (keep: written)
+  const float* grad_outputs;
+  float* partial;
+  float* grad_w;
+  float* grad_inputs;          // or NULL
+  NetKept kept;
+  int64_t nodes;
+  uint32_t n_inputs, n_outputs, n_patterns, n_sub;
+  uint32_t steps;
+  uint32_t first_item, n_items, n_joins;
+  uint32_t threads, lds_bytes;
+};
+
+}  // namespace emr

@@ -12,7 +12,7 @@
 #include <stdint.h>
 
 #include "emr_internal.h"
-#include "network.h"
+#include "learn.h"
 
 namespace emr {
 namespace {
@@ -91,27 +91,26 @@ __device__ __forceinline__ float4 state_before(const NetBackArgs& A, int64_t nod
 // The derivatives by the output nodes' sums in the last step (the others are cleared before).
 __global__ void __launch_bounds__(kNetThreads) k_back_outputs(NetBackArgs A) {
   float* gz = A.gz_before;
-  const int64_t per = (int64_t)A.n_patterns * A.n_outputs, all = per * A.n_genomes;
-  for (int64_t r = grid_thread(); r < all; r += grid_threads()) {
-    const int64_t g = r / per;
-    const uint32_t p = (uint32_t)(r % per / A.n_outputs), o = (uint32_t)(r % A.n_outputs);
-    const int64_t node = A.node_offset[g] + A.out_node[o];
-    const float v = A.outputs[r];
-    gz[((int64_t)(p / 4u) * A.nodes + node) * 4 + p % 4u] = A.grad_outputs[r] * v * (1.0f - v);
+  const int64_t per = (int64_t)A.n_patterns * A.n_outputs;
+  for (int64_t r = grid_thread(); r < per; r += grid_threads()) {
+    const uint32_t p = (uint32_t)(r / A.n_outputs), o = (uint32_t)(r % A.n_outputs);
+    const int64_t at = A.genome * per + r;
+    const float v = A.outputs[at];
+    gz[((int64_t)(p / 4u) * A.size + A.out_node[o]) * 4 + p % 4u] = A.grad_outputs[at] * v * (1.0f - v);
   }
 }
-__global__ void __launch_bounds__(kNetThreads) k_back_clear(float* p, int64_t n) {
-  for (int64_t i = grid_thread(); i < n; i += grid_threads()) p[i] = 0.0f;
+__global__ void __launch_bounds__(kNetThreads) k_back_clear(LearnFillArgs A) {
+  for (int64_t i = grid_thread(); i < A.n; i += grid_threads()) A.p[i] = 0.0f;
 }
 
 // The weights' derivatives in one step: a thread for an edge.
 __global__ void __launch_bounds__(kNetThreads) k_back_edges(NetBackArgs A) {
   const float4* gz = reinterpret_cast<const float4*>(A.gz);
-  for (int64_t e = grid_thread(); e < A.edges; e += grid_threads()) {
+  for (int64_t e = A.edge0 + grid_thread(); e < A.edge1; e += grid_threads()) {
     const int64_t src = A.in_src[e], dst = A.dst[e];
     float sum = 0.0f;
     for (uint32_t pb = 0; pb < A.pblocks; ++pb) {
-      const float4 d = gz[(int64_t)pb * A.nodes + dst], s = state_before(A, src, pb);
+      const float4 d = gz[(int64_t)pb * A.size + dst - A.node0], s = state_before(A, src, pb);
       sum = fmaf(d.x, s.x, fmaf(d.y, s.y, fmaf(d.z, s.z, fmaf(d.w, s.w, sum))));
     }
     A.grad_w[e] = A.last ? sum : A.grad_w[e] + sum;
@@ -123,7 +122,8 @@ __global__ void __launch_bounds__(kNetThreads) k_back_nodes(NetBackArgs A) {
   const float4* gz = reinterpret_cast<const float4*>(A.gz);
   float4* before = reinterpret_cast<float4*>(A.gz_before);
   const uint32_t lane = threadIdx.x % kWave;
-  for (int64_t j = grid_thread() / kWave; j < A.nodes; j += grid_threads() / kWave) {
+  for (int64_t i = grid_thread() / kWave; i < A.size; i += grid_threads() / kWave) {
+    const int64_t j = A.node0 + i;
     const int32_t slot = A.node_in[j];
     const int64_t e0 = A.out_offset[j], e1 = A.out_offset[j + 1];
     for (uint32_t pb = blockIdx.z; pb < A.pblocks; pb += gridDim.z) {
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kNetThreads) k_back_nodes(NetBackArgs A) {
       for (int64_t k = e0 + lane; k < e1; k += kWave) {
         const uint64_t v = A.out_edge[k];
         const float w = A.in_w[(uint32_t)v];
-        const float4 x = gz[(int64_t)pb * A.nodes + (int64_t)(v >> 32)];
+        const float4 x = gz[(int64_t)pb * A.size + (int64_t)(v >> 32) - A.node0];
         d.x = fmaf(w, x.x, d.x);
         d.y = fmaf(w, x.y, d.y);
         d.z = fmaf(w, x.z, d.z);
@@ -146,25 +146,548 @@ __global__ void __launch_bounds__(kNetThreads) k_back_nodes(NetBackArgs A) {
         d.w += __shfl_xor(d.w, o, kWave);
       }
       if (slot >= 0) {
-        int64_t lo = 0, hi = A.n_genomes;  // the node's genome
-        while (hi - lo > 1) {
-          const int64_t mid = (lo + hi) / 2;
-          if (A.node_offset[mid] <= j) lo = mid;
-          else hi = mid;
-        }
         const uint32_t p = 4u * pb + lane;
         if (lane < 4u && p < A.n_patterns) {
-          float* g = A.grad_inputs + (lo * A.n_patterns + p) * A.n_inputs + (uint32_t)slot;
+          float* g = A.grad_inputs + ((int64_t)A.genome * A.n_patterns + p) * A.n_inputs + (uint32_t)slot;
           const float v = lane == 0 ? d.x : (lane == 1 ? d.y : (lane == 2 ? d.z : d.w));
           *g = A.last ? v : *g + v;
         }
       } else if (lane == 0 && A.step > 1) {
         const uint32_t c = code4(A.kept, A.nodes, A.step - 2, pb, j);
-        before[(int64_t)pb * A.nodes + j] =
+        before[(int64_t)pb * A.size + i] =
             make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
                         d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
       }
     }
+  }
+}
+
+// ----------------------------------------------------------------------------- layouts
+
+// Exclusive prefix sum over the workgroup (every thread must call it); *total receives the sum.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* part, uint32_t* total) {
+  const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
+  uint32_t x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t y = (uint32_t)__shfl_up((int)x, (unsigned)o, kWave);
+    if (lane >= (uint32_t)o) x += y;
+  }
+  if (lane == kWave - 1) part[wv] = x;
+  __syncthreads();
+  uint32_t before = 0, tot = 0;
+  for (uint32_t i = 0; i < blockDim.x / kWave; ++i) {
+    before += i < wv ? part[i] : 0u;
+    tot += part[i];
+  }
+  __syncthreads();
+  *total = tot;
+  return before + x - v;
+}
+
+constexpr int kLayoutThreads = 512;
+constexpr uint32_t kAbsent = 0xFFFFFFFFu;
+
+// One of a genome's four layouts (blockIdx.y).
+__global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs A) {
+  __shared__ uint32_t key[kLearnNodes];    // edges of a row (bit 31: an output's, always heavy), or kAbsent
+  __shared__ uint16_t rank[kLearnNodes];   // a row's place in the order
+  __shared__ uint32_t part[kLayoutThreads / kWave];
+  __shared__ uint32_t heavy, rows, places;
+  const uint32_t g = A.genomes[blockIdx.x];
+  const int which = (int)blockIdx.y;
+  const LearnSet S = A.set[which];
+  const bool by_in = which == kInHid || which == kInInp;
+  const bool inputs = which == kInInp || which == kOutInp;
+  const int64_t n0 = A.node_offset[g];
+  const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
+  if (n > kLearnNodes) return;  // (host-checked)
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  constexpr uint32_t waves = kLayoutThreads / kWave;
+  uint2* ent = S.ent + A.place[g];
+  uint32_t* edge = S.edge + A.place[g];
+  LearnSlice* slices = S.slices + A.slice[g];
+  uint16_t* row_of = S.rows + 16 * A.slice[g];
+  if (threadIdx.x == 0) heavy = rows = 0;
+  __syncthreads();
+  for (uint32_t i = wave; i < n; i += waves) {
+    const int64_t node = n0 + i;
+    const bool is_input = A.node_in[node] >= 0;
+    uint32_t d = 0;
+    if (by_in) {
+      if (!is_input)
+        for (int64_t e = A.in_offset[node]; e < A.in_offset[node + 1]; e += kWave) {
+          const int64_t k = e + lane;
+          const bool mine = k < A.in_offset[node + 1] && (A.node_in[A.in_src[k]] >= 0) == inputs;
+          d += (uint32_t)__popcll(__ballot(mine));
+        }
+    } else if (is_input == inputs) {
+      d = (uint32_t)(A.out_offset[node + 1] - A.out_offset[node]);
+    }
+    if (lane == 0) {
+      const bool in = by_in ? !is_input && (!inputs || d > 0) : is_input == inputs;
+      key[i] = in ? d : kAbsent;
+    }
+  }
+  __syncthreads();
+  if (which == kInHid) {
+    for (uint32_t o = threadIdx.x; o < A.n_outputs; o += kLayoutThreads)
+      key[A.out_node[o]] |= 0x80000000u;
+    __syncthreads();
+  }
+  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
+    const uint32_t k = key[i];
+    if (k == kAbsent) continue;
+    uint32_t r = 0;
+    for (uint32_t j = 0; j < n; ++j) {
+      const uint32_t o = key[j];
+      r += o != kAbsent && (o > k || (o == k && j < i)) ? 1u : 0u;
+    }
+    rank[i] = (uint16_t)r;
+    atomicAdd(&rows, 1u);
+    if (k > kLightEdges) atomicAdd(&heavy, 1u);
+  }
+  __syncthreads();
+  const uint32_t nh = heavy, ns = nh + (rows - nh + 15u) / 16u;
+  // the slices' lengths, then their bases
+  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
+    const uint32_t k = key[i];
+    if (k == kAbsent) continue;
+    const uint32_t r = rank[i];
+    if (r < nh) {
+      slices[r] = {0, ((k & 0x7FFFFFFFu) + 15u) / 16u, 0, 1};
+      for (uint32_t j = 0; j < 16; ++j) row_of[16u * r + j] = (uint16_t)i;
+    } else {
+      const uint32_t s = nh + (r - nh) / 16u;
+      if ((r - nh) % 16u == 0) slices[s] = {0, k, 0, 0};
+      row_of[16u * s + (r - nh) % 16u] = (uint16_t)i;
+    }
+  }
+  for (uint32_t r = rows + threadIdx.x; r < nh + 16u * (ns - nh); r += kLayoutThreads)
+    row_of[16u * (nh + (r - nh) / 16u) + (r - nh) % 16u] = (uint16_t)kNoRow;
+  __threadfence_block();
+  __syncthreads();
+  uint32_t base = 0;
+  for (uint32_t s0 = 0; s0 < ns; s0 += kLayoutThreads) {
+    const uint32_t s = s0 + threadIdx.x;
+    uint32_t total;
+    const uint32_t at = block_scan(s < ns ? 16u * slices[s].len : 0u, part, &total);
+    if (s < ns) slices[s].base = base + at;
+    base += total;
+  }
+  if (threadIdx.x == 0) {
+    places = base;
+    S.n_slices[g] = ns;
+    S.n_places[g] = base;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < places; i += kLayoutThreads) {
+    ent[i] = make_uint2(n, 0u);
+    edge[i] = kNoEdge;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (uint32_t i = wave; i < n; i += waves) {
+    if (key[i] == kAbsent) continue;
+    const int64_t node = n0 + i;
+    const uint32_t r = rank[i];
+    const bool is_heavy = r < nh;
+    const uint32_t s = is_heavy ? r : nh + (r - nh) / 16u;
+    const uint32_t b = slices[s].base + (is_heavy ? 0u : (r - nh) % 16u), step = is_heavy ? 1u : 16u;
+    const int64_t* off = by_in ? A.in_offset : A.out_offset;
+    uint32_t done = 0, outs = 0;
+    for (int64_t e = off[node]; e < off[node + 1]; e += kWave) {
+      const int64_t k = e + lane;
+      const bool in = k < off[node + 1];
+      uint32_t other = 0, id = 0;
+      bool mine = in;
+      if (in) {
+        if (by_in) {
+          other = A.in_src[k];
+          id = (uint32_t)k;
+          mine = (A.node_in[other] >= 0) == inputs;
+        } else {
+          const uint64_t v = A.out_edge[k];
+          other = (uint32_t)(v >> 32);
+          id = (uint32_t)v;
+        }
+        other -= (uint32_t)n0;
+      }
+      const uint64_t m = __ballot(mine);
+      if (mine) {
+        const uint32_t at = b + step * (done + (uint32_t)__popcll(m & ((1ull << lane) - 1ull)));
+        ent[at] = make_uint2(other, __float_as_uint(A.in_w[id]));
+        edge[at] = id;
+      }
+      done += (uint32_t)__popcll(m);
+      outs += (uint32_t)__popcll(__ballot(mine && other < A.n_sub));
+    }
+    if (lane == 0 && outs > 0) atomicMax(&slices[s].first, is_heavy ? (outs + 15u) / 16u : outs);
+  }
+}
+
+__global__ void __launch_bounds__(kNetThreads) k_learn_weights(LearnWeightsArgs A) {
+  const uint32_t g = A.genomes[blockIdx.y];
+  for (int which = 0; which < kSets; ++which) {
+    const LearnSet S = A.set[which];
+    const uint32_t n = S.n_places[g];
+    for (uint32_t i = blockIdx.x * kNetThreads + threadIdx.x; i < n; i += gridDim.x * kNetThreads) {
+      const uint32_t e = S.edge[A.place[g] + i];
+      if (e != kNoEdge) S.ent[A.place[g] + i].y = __float_as_uint(A.in_w[e]);
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- a genome in LDS
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+                 0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kDppXor2 = 0x4E, kDppXor1 = 0xB1;
+// The sum over a row's LN lanes (of four patterns each).
+template <int LN>
+__device__ __forceinline__ float row_sum(float v) {
+  if constexpr (LN >= 2) v = dpp_add<kDppXor1>(v);
+  if constexpr (LN >= 4) v = dpp_add<kDppXor2>(v);
+  return v;
+}
+__device__ __forceinline__ float dot4(const float4& a, const float4& b) {
+  return fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
+}
+__device__ __forceinline__ void fma4(float4& a, float w, const float4& x) {
+  a.x = fmaf(w, x.x, a.x);
+  a.y = fmaf(w, x.y, a.y);
+  a.z = fmaf(w, x.z, a.z);
+  a.w = fmaf(w, x.w, a.w);
+}
+// The sum over the sixteen places of a heavy slice.
+template <int LN>
+__device__ __forceinline__ void heavy_sum(float4& a) {
+#pragma unroll
+  for (int o = LN; o < 16 * LN; o <<= 1) {
+    a.x += __shfl_xor(a.x, o, kWave);
+    a.y += __shfl_xor(a.y, o, kWave);
+    a.z += __shfl_xor(a.z, o, kWave);
+    a.w += __shfl_xor(a.w, o, kWave);
+  }
+}
+
+// What a lane works on: group q of four patterns of the row at place r of slice s.
+template <int LN>
+struct Place {
+  uint32_t q, r;
+  uint32_t base, len, most;  // of the slice; the longest of the wave's slices
+  uint32_t row;              // kNoRow: none
+  bool heavy, any_heavy;
+  bool writes;               // the lane holds its row's sum
+};
+// FIRST: only the edges that reach output nodes.
+template <int LN, bool FIRST>
+__device__ __forceinline__ Place<LN> place_of(const LearnSlice* slices, const uint16_t* rows, uint32_t at,
+                                              uint32_t ns, uint32_t lane) {
+  constexpr uint32_t per = 4 / LN;  // slices of a wave
+  Place<LN> P;
+  P.q = lane % LN;
+  P.r = lane / LN % 16u;
+  P.most = 0;
+  P.any_heavy = false;
+#pragma unroll
+  for (uint32_t j = 0; j < per; ++j) {  // (the wave's)
+    if (at + j >= ns) break;
+    const uint32_t l = FIRST ? slices[at + j].first : slices[at + j].len;
+    P.most = l > P.most ? l : P.most;
+    P.any_heavy |= slices[at + j].heavy != 0;
+  }
+  const uint32_t s = at + lane / (16u * LN);
+  const bool in = s < ns;
+  const LearnSlice S = slices[in ? s : at];
+  P.base = S.base + P.r;
+  P.len = in ? (FIRST ? S.first : S.len) : 0u;
+  P.heavy = in && S.heavy != 0;
+  P.row = in ? rows[16u * s + P.r] : kNoRow;
+  P.writes = P.row != kNoRow && (!P.heavy || P.r == 0);
+  return P;
+}
+
+// The edge at the k-th place of a lane's row, past its end an empty one.
+__device__ __forceinline__ uint2 edge_at(const uint2* __restrict__ e, uint32_t k, uint32_t len, uint32_t n) {
+  uint32_t x = n, y = 0;
+  if (k < len) {
+    const uint64_t v = *reinterpret_cast<const uint64_t*>(e + 16u * k);
+    x = (uint32_t)v;
+    y = (uint32_t)(v >> 32);
+  }
+  return make_uint2(x, y);
+}
+
+// The weighted sums of a slice's rows over x (the values of the genome's nodes, LN float4 each).
+template <int LN>
+__device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint2* __restrict__ ent,
+                                           const float4* x, uint32_t n) {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const uint2* e = ent + P.base;
+  constexpr int U = 4;
+  uint2 a[U], b[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) a[j] = edge_at(e, (uint32_t)j, P.len, n);
+  for (uint32_t k = 0; k < P.most; k += U) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) b[j] = edge_at(e, k + U + (uint32_t)j, P.len, n);
+#pragma unroll
+    for (int j = 0; j < U; ++j) fma4(acc, __uint_as_float(a[j].y), x[a[j].x * LN + P.q]);
+#pragma unroll
+    for (int j = 0; j < U; ++j) a[j] = b[j];
+  }
+  if (P.any_heavy) {
+    float4 h = acc;
+    heavy_sum<LN>(h);
+    if (P.heavy) acc = h;
+  }
+  return acc;
+}
+
+// The same for derivatives gz, and beside it the derivatives of the edges' weights, gz times the row's
+// own states s summed over the patterns, added to `sum` at the edges' places.
+template <int LN>
+__device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __restrict__ ent,
+                                            const float4* gz, uint32_t n, const float4& s,
+                                            float* __restrict__ sum) {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const uint2* e = ent + P.base;
+  constexpr int U = 4;
+  uint2 a[U], b[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) a[j] = edge_at(e, (uint32_t)j, P.len, n);
+  for (uint32_t k = 0; k < P.most; k += U) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) b[j] = edge_at(e, k + U + (uint32_t)j, P.len, n);
+    // each of a row's lanes adds the derivatives of U / LN edges
+    constexpr int own = U / LN;
+    float before[own];
+#pragma unroll
+    for (int c = 0; c < own; ++c) {
+      const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
+      before[c] = kk < P.len ? sum[P.base + 16u * kk] : 0.0f;
+    }
+    float d[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const float4 v = gz[a[j].x * LN + P.q];
+      fma4(acc, __uint_as_float(a[j].y), v);
+      d[j] = row_sum<LN>(dot4(v, s));
+    }
+#pragma unroll
+    for (int c = 0; c < own; ++c) {
+      const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
+      float v = d[c * LN];
+#pragma unroll
+      for (int j = 1; j < LN; ++j) v = P.q == (uint32_t)j ? d[c * LN + j] : v;
+      if (kk < P.len) sum[P.base + 16u * kk] = before[c] + v;
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) a[j] = b[j];
+  }
+  if (P.any_heavy) {
+    float4 h = acc;
+    heavy_sum<LN>(h);
+    if (P.heavy) acc = h;
+  }
+  return acc;
+}
+
+__device__ __forceinline__ float sigmoid_f(float z) { return 1.0f / (1.0f + expf(-z)); }
+__device__ __forceinline__ uint32_t code_of(float s) { return (uint32_t)__float2uint_rn(255.0f * s); }
+// The four codes of a node's state for pattern group pg.
+__device__ __forceinline__ uint32_t* kept_at(const NetKept& K, int64_t nodes, uint32_t plane, uint32_t pg,
+                                             int64_t node) {
+  return reinterpret_cast<uint32_t*>(
+      K.codes + (((int64_t)plane * K.blocks + pg / K.q) * nodes + node) * (4 * K.q) + 4 * (pg % K.q));
+}
+__device__ __forceinline__ float4 pattern4(const LearnArgs& A, int32_t slot, uint32_t pg) {
+  float c[4];
+#pragma unroll
+  for (uint32_t k = 0; k < 4; ++k) {
+    const uint32_t p = 4u * pg + k;
+    c[k] = p < A.n_patterns ? A.patterns[(int64_t)p * A.n_inputs + (uint32_t)slot] : 0.0f;
+  }
+  return make_float4(c[0], c[1], c[2], c[3]);
+}
+
+// All steps of one genome for an item's blocks of 4 LN patterns: states in LDS as two halves that the steps
+// swap and the sums of the input edges, which no step changes. A wave holds a slice of sixteen rows with
+// LN lanes each (or 4 / LN slices).
+template <int LN>
+__device__ __forceinline__ void keep_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
+  const uint32_t g = I.genome;
+  const int64_t n0 = A.node_offset[g];
+  const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
+  if (learn_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  const uint32_t lane = threadIdx.x % kWave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  constexpr uint32_t per = 4 / LN;
+  const LearnSet &H = A.set[kInHid], &E = A.set[kInInp];
+  const uint2 *he = H.ent + A.place[g], *ie = E.ent + A.place[g];
+  const LearnSlice *hs = H.slices + A.slice[g], *is = E.slices + A.slice[g];
+  const uint16_t *hr = H.rows + 16 * A.slice[g], *ir = E.rows + 16 * A.slice[g];
+  const uint32_t hn = H.n_slices[g], in = E.n_slices[g];
+  float4 *cur = lds, *nxt = lds + (n + 1u) * LN, *held = nxt + (n + 1u) * LN;
+  for (uint32_t b = I.b0; b < I.b1; ++b) {
+    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) {
+      const uint32_t node = i / LN;
+      const int32_t slot = node < n ? A.node_in[n0 + node] : -1;
+      const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+      cur[i] = slot >= 0 ? pattern4(A, slot, b * LN + i % LN) : z;
+      nxt[i] = z;
+      held[i] = z;
+      if (slot >= 0)
+        for (uint32_t t = 0; t < A.kept.planes; ++t)
+          *kept_at(A.kept, A.nodes, t, b * LN + i % LN, n0 + node) = 0;
+    }
+    __syncthreads();
+    for (uint32_t at = wave * per; at < in; at += waves * per) {
+      const Place<LN> P = place_of<LN, false>(is, ir, at, in, lane);
+      const float4 z = row_sums<LN>(P, ie, cur, n);
+      if (P.writes) held[P.row * LN + P.q] = z;
+    }
+    __syncthreads();
+    for (uint32_t step = 1; step <= A.steps; ++step) {
+      // the last step: output nodes alone, the first slices
+      const uint32_t end = step == A.steps ? A.n_outputs : hn;
+      for (uint32_t at = wave * per; at < end; at += waves * per) {
+        Place<LN> P = place_of<LN, false>(hs, hr, at, end, lane);
+        if (step == 1) P.most = 0;  // (hidden states are 0: their edges add nothing)
+        float4 z = row_sums<LN>(P, he, cur, n);
+        if (!P.writes) continue;
+        const float4 y = held[P.row * LN + P.q];
+        const float4 s = make_float4(sigmoid_f(z.x + y.x), sigmoid_f(z.y + y.y), sigmoid_f(z.z + y.z),
+                                     sigmoid_f(z.w + y.w));
+        nxt[P.row * LN + P.q] = s;
+        if (step < A.steps)
+          *kept_at(A.kept, A.nodes, step - 1, b * LN + P.q, n0 + P.row) =
+              code_of(s.x) | code_of(s.y) << 8 | code_of(s.z) << 16 | code_of(s.w) << 24;
+      }
+      __syncthreads();
+      float4* x = cur;
+      cur = nxt;
+      nxt = x;
+    }
+    const float* c = reinterpret_cast<const float*>(cur);
+    const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
+    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
+      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+      A.outputs[((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o] =
+          c[(uint32_t)A.out_node[o] * 4u * LN + p];
+    }
+    __syncthreads();
+  }
+}
+
+template <int LN>
+__device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
+  const uint32_t g = I.genome;
+  const int64_t n0 = A.node_offset[g];
+  const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
+  if (learn_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  const uint32_t lane = threadIdx.x % kWave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  constexpr uint32_t per = 4 / LN;
+  const LearnSet &H = A.set[kOutHid], &E = A.set[kOutInp];
+  const uint2 *he = H.ent + A.place[g], *ie = E.ent + A.place[g];
+  const LearnSlice *hs = H.slices + A.slice[g], *is = E.slices + A.slice[g];
+  const uint16_t *hr = H.rows + 16 * A.slice[g], *ir = E.rows + 16 * A.slice[g];
+  const uint32_t hn = H.n_slices[g], in = E.n_slices[g], hp = H.n_places[g], ip = E.n_places[g];
+  float *hsum = A.partial + I.part, *isum = hsum + hp;
+  float4 *cur = lds, *nxt = lds + (n + 1u) * LN, *all = nxt + (n + 1u) * LN;
+  for (uint32_t i = threadIdx.x; i < hp + ip; i += blockDim.x) hsum[i] = 0.0f;
+  for (uint32_t b = I.b0; b < I.b1; ++b) {
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) cur[i] = nxt[i] = all[i] = zero;
+    __threadfence_block();
+    __syncthreads();
+    const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
+    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
+      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+      const int64_t r = ((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o;
+      const float v = A.outputs[r], d = A.grad_outputs[r] * v * (1.0f - v);
+      const uint32_t at = (uint32_t)A.out_node[o] * 4u * LN + p;
+      reinterpret_cast<float*>(cur)[at] = d;
+      reinterpret_cast<float*>(all)[at] = d;
+    }
+    __syncthreads();
+    for (uint32_t step = A.steps; step >= 2; --step) {
+      const bool last = step == A.steps;  // derivatives at the output nodes alone
+      for (uint32_t at = wave * per; at < hn; at += waves * per) {
+        const Place<LN> P = last ? place_of<LN, true>(hs, hr, at, hn, lane)
+                                 : place_of<LN, false>(hs, hr, at, hn, lane);
+        const uint32_t c =
+            P.row != kNoRow ? *kept_at(A.kept, A.nodes, step - 2, b * LN + P.q, n0 + P.row) : 0u;
+        const float4 d = row_grads<LN>(P, he, cur, n, states(c), hsum);
+        if (!P.writes) continue;
+        const float4 v = make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
+                                     d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
+        const uint32_t i = P.row * LN + P.q;
+        nxt[i] = v;
+        const float4 a = all[i];
+        all[i] = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
+      }
+      __syncthreads();
+      float4* x = cur;
+      cur = nxt;
+      nxt = x;
+    }
+    for (uint32_t at = wave * per; at < in; at += waves * per) {
+      const Place<LN> P = place_of<LN, false>(is, ir, at, in, lane);
+      const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
+      const float4 x = slot >= 0 ? pattern4(A, slot, b * LN + P.q) : zero;
+      const float4 d = row_grads<LN>(P, ie, all, n, x, isum);
+      if (!A.grad_inputs || !P.writes) continue;
+      const float v[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t p = p0 + 4u * P.q + k;
+        if (p < A.n_patterns)
+          A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[k];
+      }
+    }
+    __syncthreads();
+  }
+  if (!I.alone) return;
+  __threadfence_block();
+  __syncthreads();
+  const uint32_t *hi = H.edge + A.place[g], *ii = E.edge + A.place[g];
+  for (uint32_t i = threadIdx.x; i < hp; i += blockDim.x)
+    if (hi[i] != kNoEdge) A.grad_w[hi[i]] = hsum[i];
+  for (uint32_t i = threadIdx.x; i < ip; i += blockDim.x)
+    if (ii[i] != kNoEdge) A.grad_w[ii[i]] = isum[i];
+}
+
+template <bool BACK>
+__global__ void __launch_bounds__(1024, 4) k_learn(LearnArgs A) {
+  extern __shared__ float4 learn_lds_mem[];
+  const LearnItem I = A.items[A.first_item + blockIdx.x];
+  switch (I.groups) {
+    case 1: BACK ? back_item<1>(A, I, learn_lds_mem) : keep_item<1>(A, I, learn_lds_mem); break;
+    case 2: BACK ? back_item<2>(A, I, learn_lds_mem) : keep_item<2>(A, I, learn_lds_mem); break;
+    default: BACK ? back_item<4>(A, I, learn_lds_mem) : keep_item<4>(A, I, learn_lds_mem); break;
+  }
+}
+
+// The items' sums of genomes with more than one, in the items' order.
+__global__ void __launch_bounds__(kNetThreads) k_learn_join(LearnArgs A) {
+  const LearnJoin J = A.joins[blockIdx.y];
+  const LearnSet &H = A.set[kOutHid], &E = A.set[kOutInp];
+  const uint32_t hp = H.n_places[J.genome], all = hp + E.n_places[J.genome];
+  const uint32_t *hi = H.edge + A.place[J.genome], *ii = E.edge + A.place[J.genome];
+  for (uint32_t i = blockIdx.x * kNetThreads + threadIdx.x; i < all; i += gridDim.x * kNetThreads) {
+    const uint32_t e = i < hp ? hi[i] : ii[i - hp];
+    if (e == kNoEdge) continue;
+    const float* p = A.partial + J.part + i;
+    float sum = 0.0f;
+    for (uint32_t k = 0; k < J.items; ++k) sum += p[k * J.stride];
+    A.grad_w[e] = sum;
   }
 }
 
@@ -176,45 +699,87 @@ uint32_t stride_blocks(int64_t n) {
 }  // namespace
 }  // namespace emr
 
-// Steps: 0 the edges' keys by source, 1 their offsets (after the sort), 2 the derivatives by the outputs'
-// sums into gz_before (the other half behind it cleared), 3 one step's weight derivatives, 4 one step
-// backwards, 5 no derivatives at all.
+// Steps: 0 the edges' keys by source, 1 their offsets (after the sort), 2 a layout, 3 its weights; all steps
+// of the genomes in LDS: 4 activation, 5 gradients, 6 their joined sums; a larger genome: 7 the derivatives by
+// the outputs' sums into gz_before (the other half behind it cleared), 8 one step's weight derivatives, 9 one
+// step backwards; 10 zeros.
 extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s) {
   using namespace emr;
   const dim3 blk(kNetThreads);
-  if (step < 2) {
-    const auto& A = *static_cast<const NetTurnArgs*>(args);
-    if (step == 0)
-      hipLaunchKernelGGL(k_turn_keys, dim3(stride_blocks(A.nodes * kWave)), blk, 0, s, A);
-    else
-      hipLaunchKernelGGL(k_turn_offsets, dim3(stride_blocks(A.nodes + 1)), blk, 0, s, A);
-    return hipGetLastError();
-  }
-  const auto& A = *static_cast<const NetBackArgs*>(args);
   switch (step) {
-    case 2: {
-      const int64_t n = 8 * (int64_t)A.pblocks * A.nodes;  // (both halves: input nodes stay 0)
-      hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(n)), blk, 0, s,
-                         A.gz_before, n);
-      hipLaunchKernelGGL(k_back_outputs,
-                         dim3(stride_blocks((int64_t)A.n_genomes * A.n_patterns * A.n_outputs)), blk, 0,
-                         s, A);
+    case 0: {
+      const auto& A = *static_cast<const NetTurnArgs*>(args);
+      hipLaunchKernelGGL(k_turn_keys, dim3(stride_blocks(A.nodes * kWave)), blk, 0, s, A);
       break;
     }
-    case 3:
-      if (A.edges <= 0) return hipSuccess;
-      hipLaunchKernelGGL(k_back_edges, dim3(stride_blocks(A.edges)), blk, 0, s, A);
+    case 1: {
+      const auto& A = *static_cast<const NetTurnArgs*>(args);
+      hipLaunchKernelGGL(k_turn_offsets, dim3(stride_blocks(A.nodes + 1)), blk, 0, s, A);
       break;
+    }
+    case 2: {
+      const auto& A = *static_cast<const LearnLayoutArgs*>(args);
+      if (A.count == 0) return hipSuccess;
+      hipLaunchKernelGGL(k_learn_layout, dim3(A.count, kSets), dim3(kLayoutThreads), 0, s, A);
+      break;
+    }
+    case 3: {
+      const auto& A = *static_cast<const LearnWeightsArgs*>(args);
+      for (uint32_t a = 0; a < A.count; a += 65535u) {
+        LearnWeightsArgs B = A;
+        B.genomes = A.genomes + a;
+        hipLaunchKernelGGL(k_learn_weights, dim3(16, A.count - a < 65535u ? A.count - a : 65535u), blk, 0, s,
+                           B);
+      }
+      break;
+    }
     case 4:
-      hipLaunchKernelGGL(k_back_nodes, dim3(stride_blocks(A.nodes * kWave), 1, A.pblocks < 64u ? A.pblocks : 64u),
-                         blk, 0, s, A);
-      break;
     case 5: {
-      const int64_t n = (int64_t)A.n_genomes * A.n_patterns * A.n_inputs;
-      if (A.edges > 0)
-        hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(A.edges)), blk, 0, s, A.grad_w, A.edges);
-      if (A.grad_inputs)
-        hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(n)), blk, 0, s, A.grad_inputs, n);
+      const auto& A = *static_cast<const LearnArgs*>(args);
+      if (A.n_items == 0) return hipSuccess;
+      if (A.lds_bytes > kLearnLds || A.threads == 0 || A.threads > 1024u || A.threads % kWave != 0)
+        return hipErrorInvalidValue;
+      if (step == 4)
+        hipLaunchKernelGGL(k_learn<false>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      else
+        hipLaunchKernelGGL(k_learn<true>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      break;
+    }
+    case 6: {
+      const auto& A = *static_cast<const LearnArgs*>(args);
+      for (uint32_t a = 0; a < A.n_joins; a += 65535u) {
+        LearnArgs B = A;
+        B.joins = A.joins + a;
+        hipLaunchKernelGGL(k_learn_join, dim3(32, A.n_joins - a < 65535u ? A.n_joins - a : 65535u), blk, 0, s,
+                           B);
+      }
+      break;
+    }
+    case 7: {
+      const auto& A = *static_cast<const NetBackArgs*>(args);
+      const int64_t n = 8 * (int64_t)A.pblocks * A.size;  // (both halves: input nodes stay 0)
+      hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(n)), blk, 0, s, LearnFillArgs{A.gz_before, n});
+      hipLaunchKernelGGL(k_back_outputs, dim3(stride_blocks((int64_t)A.n_patterns * A.n_outputs)), blk, 0, s,
+                         A);
+      break;
+    }
+    case 8: {
+      const auto& A = *static_cast<const NetBackArgs*>(args);
+      if (A.edge1 <= A.edge0) return hipSuccess;
+      hipLaunchKernelGGL(k_back_edges, dim3(stride_blocks(A.edge1 - A.edge0)), blk, 0, s, A);
+      break;
+    }
+    case 9: {
+      const auto& A = *static_cast<const NetBackArgs*>(args);
+      hipLaunchKernelGGL(k_back_nodes,
+                         dim3(stride_blocks(A.size * kWave), 1, A.pblocks < 64u ? A.pblocks : 64u), blk, 0, s,
+                         A);
+      break;
+    }
+    case 10: {
+      const auto& A = *static_cast<const LearnFillArgs*>(args);
+      if (A.n <= 0) return hipSuccess;
+      hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(A.n)), blk, 0, s, A);
       break;
     }
     default:

@@ -1,4 +1,4 @@
-// Arguments of the network kernels (network.hip, learn.hip), shared with their host driver (networks.cpp).
+// Arguments of the network kernels (network.hip), shared with their host driver (networks.cpp).
 //
 // Numbering. Before pruning, genome g has raw nodes 0 .. n_sub - 1 (its substrate sources, in
 // substrate order) and n_sub + i for the i-th set bit of its hidden-cell bitmap (ascending grid
@@ -220,7 +220,6 @@ struct NetRunArgs {
   uint32_t n_inputs, n_outputs, n_patterns;
   uint32_t steps;
   uint32_t lds_bytes;          // the launch's dynamic LDS
-  NetKept kept;
   // class r: genomes order[first[r]] .. (count[r] of them), blocks[r] blocks of 4 q[r] patterns
   uint32_t first[kNetRanges], count[kNetRanges], blocks[kNetRanges], q[kNetRanges];
 };
@@ -276,44 +275,6 @@ struct NetOutArgs {
   int64_t nodes;
   uint32_t n_outputs;
   uint32_t n_patterns;
-};
-
-// Gradients. The edges a second time, grouped by their source.
-struct NetTurnArgs {
-  const int64_t* in_offset;  // [nodes + 1]
-  const uint32_t* in_src;    // [edges]
-  uint32_t* key;             // [edges] source
-  uint64_t* val;             // [edges] edge | destination << 32
-  uint32_t* dst;             // [edges] destination
-  const uint32_t* skey;      // sorted by source, each group in edge order
-  int64_t* out_offset;       // [nodes + 1]
-  int64_t nodes, edges;
-};
-
-// The stepwise kernels: derivatives by the node sums ("gz") as [pblocks][nodes] float4.
-struct NetBackArgs {
-  const int64_t* node_offset;
-  const int32_t* node_in;
-  const int32_t* out_node;     // [n_outputs]
-  const int64_t* in_offset;
-  const uint32_t* in_src;
-  const float* in_w;
-  const uint32_t* dst;         // [edges]
-  const int64_t* out_offset;   // [nodes + 1]
-  const uint64_t* out_edge;    // [edges] edge | destination << 32
-  const float* patterns;       // [n_patterns * n_inputs]
-  const float* outputs;        // [n_genomes * n_patterns * n_outputs]
-  const float* grad_outputs;   // the same
-  const float* gz;             // derivatives after the step
-  float* gz_before;            // before it
-  float* grad_w;               // [edges]
-  float* grad_inputs;          // [n_genomes * n_patterns * n_inputs] or NULL
-  NetKept kept;
-  int64_t nodes, edges;
-  uint32_t n_genomes, n_inputs, n_outputs, n_patterns;
-  uint32_t pblocks;
-  uint32_t step;               // 1 .. steps: the step whose derivatives gz holds
-  uint32_t last;               // whether it is the first one looked at: gradients are set, not added to
 };
 
 }  // namespace emr

@@ -650,13 +650,6 @@ __device__ __forceinline__ float node_sum(X&& x, const uint32_t* __restrict__ sr
   return z;
 }
 
-// The four codes of a node's state for pattern group pg.
-__device__ __forceinline__ uint8_t* kept_at(const NetKept& K, int64_t nodes, uint32_t plane, uint32_t pg,
-                                            int64_t node) {
-  return K.codes + (((int64_t)plane * K.blocks + pg / K.q) * nodes + node) * (4 * K.q) + 4 * (pg % K.q);
-}
-__device__ __forceinline__ uint8_t state_code(float s) { return (uint8_t)__float2uint_rn(255.0f * s); }
-
 // All steps of one genome for one block of 4 Q patterns. One launch per step over global states
 // gathers 16 bytes per edge and four patterns from L2 (150 networks, 0.51M edges, 1000 patterns, 4
 // steps: 2560 us); here the gathers are LDS reads, the edges are read once per 4 Q patterns and
@@ -665,7 +658,7 @@ __device__ __forceinline__ uint8_t state_code(float s) { return (uint8_t)__float
 // buffers (swapped by each step), one wave per node and step, the edges read from L2. An input
 // node holds its pattern values in both buffers. The node's first edge (bit 31: an input node) is
 // kept in LDS after the states.
-template <int Q, bool KEEP>
+template <int Q>
 __device__ __forceinline__ void net_run(const NetRunArgs& A, uint32_t g, uint32_t block,
                                         float4* lds) {
   const int64_t n0 = A.node_offset[g];
@@ -685,17 +678,12 @@ __device__ __forceinline__ void net_run(const NetRunArgs& A, uint32_t g, uint32_
                  A.node_in[n0 + i / Q], block * Q + i % Q);
     cur[i] = v;
     nxt[i] = v;
-    if (KEEP && A.node_in[n0 + i / Q] >= 0)
-      for (uint32_t t = 0; t < A.kept.planes; ++t)
-        *reinterpret_cast<uint32_t*>(kept_at(A.kept, A.nodes, t, block * Q + i % Q, n0 + i / Q)) = 0;
   }
   for (uint32_t i = threadIdx.x; i <= n; i += kNetRunThreads) {
     const int64_t e = A.in_offset[n0 + i] - e0;
     const uint32_t f = e < 0 ? 0u : (e > (int64_t)edges ? edges : (uint32_t)e);
     first[i] = f | (i < n && A.node_in[n0 + i] >= 0 ? 0x80000000u : 0u);
   }
-  // (a workgroup's groups of patterns lie in one block of codes: Q is no more than a block's)
-  uint8_t* codes = KEEP ? kept_at(A.kept, A.nodes, 0, block * Q, n0) : nullptr;
   __syncthreads();
   for (uint32_t step = 0; step < A.steps; ++step) {
     const float4* mine = cur + lane % Q;  // the lane's patterns
@@ -705,14 +693,9 @@ __device__ __forceinline__ void net_run(const NetRunArgs& A, uint32_t g, uint32_
       const uint32_t l = __builtin_amdgcn_readfirstlane(first[i + 1]) & 0x7FFFFFFFu;
       const float z = node_sum<Q, false>([&](uint32_t s) { return mine[(s - (uint32_t)n0) * Q]; },
                                   A.in_src + e0 + f, A.in_w + e0 + f, l > f ? l - f : 0u, lane);
-      if (lane % 16u < (uint32_t)Q) {
-        const float v = sigmoid_f(z);
-        reinterpret_cast<float*>(nxt + i * Q + lane % 16u)[lane / 16u] = v;
-        if (KEEP && step < A.kept.planes)
-          codes[i * (4u * A.kept.q) + (4u * (lane % 16u) + lane / 16u)] = state_code(v);
-      }
+      if (lane % 16u < (uint32_t)Q)
+        reinterpret_cast<float*>(nxt + i * Q + lane % 16u)[lane / 16u] = sigmoid_f(z);
     }
-    if (KEEP) codes += (int64_t)A.kept.blocks * A.nodes * (4u * A.kept.q);
     __syncthreads();
     float4* s = cur;
     cur = nxt;
@@ -739,8 +722,7 @@ __device__ __forceinline__ void net_run(const NetRunArgs& A, uint32_t g, uint32_
   }
 }
 
-template <bool KEEP>
-__global__ void __launch_bounds__(kNetRunThreads, KEEP ? 4 : 8) k_net_run(NetRunArgs A) {
+__global__ void __launch_bounds__(kNetRunThreads, 8) k_net_run(NetRunArgs A) {
   extern __shared__ float4 net_lds[];
   uint32_t at = blockIdx.x;
 #pragma unroll
@@ -750,15 +732,22 @@ __global__ void __launch_bounds__(kNetRunThreads, KEEP ? 4 : 8) k_net_run(NetRun
       const uint32_t g = A.order[A.first[r] + at / blocks], block = at % blocks;
       if (g >= A.n_genomes) return;
       switch (A.q[r]) {
-        case 1: net_run<1, KEEP>(A, g, block, net_lds); break;
-        case 2: net_run<2, KEEP>(A, g, block, net_lds); break;
-        default: net_run<4, KEEP>(A, g, block, net_lds); break;
+        case 1: net_run<1>(A, g, block, net_lds); break;
+        case 2: net_run<2>(A, g, block, net_lds); break;
+        default: net_run<4>(A, g, block, net_lds); break;
       }
       return;
     }
     at -= all;
   }
 }
+
+// The four codes of a node's state for pattern group pg.
+__device__ __forceinline__ uint8_t* kept_at(const NetKept& K, int64_t nodes, uint32_t plane, uint32_t pg,
+                                            int64_t node) {
+  return K.codes + (((int64_t)plane * K.blocks + pg / K.q) * nodes + node) * (4 * K.q) + 4 * (pg % K.q);
+}
+__device__ __forceinline__ uint8_t state_code(float s) { return (uint8_t)__float2uint_rn(255.0f * s); }
 
 // The k-th genome of a list (k < total).
 __device__ __forceinline__ uint32_t list_genome(const NetList& L, uint32_t k) {
@@ -899,11 +888,11 @@ extern "C" hipError_t emr_launch_choice(int kind, const void* args, hipStream_t 
 // Steps: 0 rank, 1 layout, 2 pairs of a phase, 3 its edges, 4 flags, 5 reach pass, 6 kept counts
 // and their sums, 7 nodes, 8 keys; after the sort, 14 offsets and edges. Activation: 9 initial
 // state, 10 one step, 11 outputs / fitness (stepwise), 12 patterns by value, 13 all steps in LDS. 15
-// copies into buffers of the contents' size. From 20 on, the gradients' (learn.hip), from 30 on, the
+// copies into buffers of the contents' size. From 20 on, the learning ones (learn.hip), from 40 on, the
 // draws' and their loss (choice.hip).
 extern "C" hipError_t emr_launch_net(int step, const void* args, hipStream_t s) {
   using namespace emr;
-  if (step >= 30) return emr_launch_choice(step - 30, args, s);
+  if (step >= 40) return emr_launch_choice(step - 40, args, s);
   if (step >= 20) return emr_launch_learn(step - 20, args, s);
   const dim3 blk(kNetThreads);
   switch (step) {
@@ -1013,10 +1002,7 @@ extern "C" hipError_t emr_launch_net(int step, const void* args, hipStream_t s) 
       }
       if (b == 0) return hipSuccess;
       if (b > 0x7FFFFFFFull || A.lds_bytes > kNetRunLds) return hipErrorInvalidValue;
-      if (A.kept.codes)
-        hipLaunchKernelGGL(k_net_run<true>, dim3((uint32_t)b), dim3(kNetRunThreads), A.lds_bytes, s, A);
-      else
-        hipLaunchKernelGGL(k_net_run<false>, dim3((uint32_t)b), dim3(kNetRunThreads), A.lds_bytes, s, A);
+      hipLaunchKernelGGL(k_net_run, dim3((uint32_t)b), dim3(kNetRunThreads), A.lds_bytes, s, A);
       break;
     }
     case 15: {

@@ -27,6 +27,7 @@
 
 #include "../../include/emr.h"
 #include "choice.h"
+#include "learn.h"
 #include "network.h"
 
 namespace emr {
@@ -293,9 +294,39 @@ struct emr_networks {
   Dev d_out_node;  // [n_out] substrate index of output o
   int64_t nodes = 0, edges = 0;
   Dev state, patterns;
-  // gradients: the edges by source (made by the first call), and the derivatives' two halves
-  Dev edge_dst, out_offset, out_edge, back;
-  bool turned = false;
+  // learning, from its first call on: the edges' layouts of the genomes that fit a workgroup (learn.h), by
+  // genome the first place and slice; the others, whose edges by source lie in out_edge; the items by
+  // number of patterns; partial sums, and a larger genome's derivatives
+  struct Learning {
+    bool laid = false;
+    Dev ent[emr::kSets], edge[emr::kSets], slices[emr::kSets], rows[emr::kSets], n_slices, n_places;
+    Dev place, slice, fits, large, edge_dst, out_offset, out_edge;
+    std::vector<uint32_t> fit, big;
+    struct Run {
+      uint32_t first, count, threads, lds;
+    };
+    struct Plan {
+      int32_t patterns = 0;
+      Dev items, joins;
+      uint32_t n_joins = 0;
+      std::vector<Run> runs;
+      int64_t partial_floats = 0;
+    };
+    std::vector<std::unique_ptr<Plan>> plans;  // by number of patterns, the oldest first
+    Dev partial, back;
+    void release_idle() {
+      for (int k = 0; k < emr::kSets; ++k)
+        for (Dev* d : {&ent[k], &edge[k], &slices[k], &rows[k]}) d->reset_idle();
+      for (Dev* d : {&n_slices, &n_places, &place, &slice, &fits, &large, &edge_dst, &out_offset, &out_edge,
+                     &partial, &back})
+        d->reset_idle();
+      for (auto& p : plans) {
+        p->items.reset_idle();
+        p->joins.reset_idle();
+      }
+    }
+  } learn;
+  std::vector<int64_t> node_off, edge_off;  // [n_genomes + 1] first nodes, first edges
   // genomes in the order of the activation launches (order_genomes): their loads and node counts, the
   // sums over those before each, and the most nodes of those before each in its class
   Dev order;
@@ -324,9 +355,9 @@ struct emr_networks {
     if (pin) (void)hipHostFree(pin);
     for (auto& ph : phases) ph->release_idle();
     for (Dev* d : {&known, &node_offset, &node_cell, &node_in, &in_offset, &in_src, &in_w,
-                   &d_slots, &d_out_node, &state, &patterns, &edge_dst, &out_offset, &out_edge,
-                   &back, &order})
+                   &d_slots, &d_out_node, &state, &patterns, &order})
       d->reset_idle();
+    learn.release_idle();
   }
 };
 
@@ -712,6 +743,8 @@ static_assert(kRunClasses <= emr::kNetRanges && kRunClass[kRunClasses - 2].lds =
 emr_status order_genomes(emr_networks& N, const int64_t* node_off, const int64_t* edge_off,
                          hipStream_t s) {
   const uint32_t G = (uint32_t)N.n_genomes;
+  N.node_off.assign(node_off, node_off + G + 1);
+  N.edge_off.assign(edge_off, edge_off + G + 1);
   std::vector<uint32_t>& order = N.order_host;
   order.resize(G);
   std::vector<uint8_t> cls(G);
@@ -886,10 +919,9 @@ emr_status mark_done(emr_networks& M, hipStream_t s) {
   return EMR_OK;
 }
 
-// patterns: on the host, or (with `kept`, whose codes may be NULL) on the device.
 emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_patterns,
                        int32_t steps, float* outputs, float* fitness, const float* targets,
-                       hipStream_t s, const emr::NetKept* kept = nullptr) {
+                       hipStream_t s) {
   emr_networks& M = const_cast<emr_networks&>(*N);
   NET_TRY(check_device(N));
   const int64_t pblocks = (n_patterns + 3) / 4;
@@ -922,8 +954,8 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
     list.count[0] = list.total;
   }
   // (few patterns of stepwise kernels alone are the initial state's arguments: a launch fewer)
-  const bool by_value = !kept && list.order == nullptr && n_pat <= emr::kNetStageFloats;
-  if (!by_value && !kept)
+  const bool by_value = list.order == nullptr && n_pat <= emr::kNetStageFloats;
+  if (!by_value)
     NET_TRY(stage_patterns(M, patterns, n_pat, targets, targets ? (size_t)n_patterns : 0, s));
   emr::NetRunArgs ra{};
   ra.order = N->order.as<uint32_t>();
@@ -932,9 +964,7 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
   ra.in_offset = N->in_offset.as<int64_t>();
   ra.in_src = N->in_src.as<uint32_t>();
   ra.in_w = N->in_w.as<float>();
-  const float* dev_patterns = kept ? patterns : M.patterns.as<float>();
-  ra.patterns = dev_patterns;
-  if (kept) ra.kept = *kept;
+  ra.patterns = M.patterns.as<float>();
   ra.targets = targets ? M.patterns.as<float>() + n_pat : nullptr;
   ra.out_node = N->d_out_node.as<int32_t>();
   ra.outputs = outputs;
@@ -987,9 +1017,8 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
         left -= n;
       }
       emr::NetStateArgs sa{list, N->node_offset.as<int64_t>(), N->node_in.as<int32_t>(),
-                           by_value ? nullptr : dev_patterns, buf[0], N->nodes,
-                           (uint32_t)N->n_in, (uint32_t)n_patterns, (uint32_t)pblocks,
-                           kept ? *kept : emr::NetKept{}, {}};
+                           by_value ? nullptr : M.patterns.as<float>(), buf[0], N->nodes,
+                           (uint32_t)N->n_in, (uint32_t)n_patterns, (uint32_t)pblocks, {}, {}};
       if (by_value) std::memcpy(sa.v, patterns, n_pat * 4);
       NET_HIP(emr_launch_net(9, &sa, s));
       int cur = 0;
@@ -997,7 +1026,7 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
         emr::NetStepArgs st{list, N->node_offset.as<int64_t>(), N->node_in.as<int32_t>(),
                             N->in_offset.as<int64_t>(), N->in_src.as<uint32_t>(),
                             N->in_w.as<float>(), buf[cur], buf[cur ^ 1], N->nodes,
-                            (uint32_t)pblocks, kept ? *kept : emr::NetKept{}, (uint32_t)t};
+                            (uint32_t)pblocks, {}, 0};
         NET_HIP(emr_launch_net(10, &st, s));
       }
       emr::NetOutArgs oa{};
@@ -1034,57 +1063,342 @@ emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps,
   return EMR_OK;
 }
 
-// The edges by source, on the first call's stream.
-emr_status turn_edges(emr_networks& N, hipStream_t s) {
-  if (N.turned) return EMR_OK;
-  if (N.edges > (int64_t)UINT32_MAX) return failf(EMR_E_LIMIT, "networks: too many edges");
-  Dev key, skey, val, tmp;
-  const size_t e = (size_t)N.edges;
-  NET_TRY(alloc(N.edge_dst, e * 4, "edge destinations", s));
-  NET_TRY(alloc(N.out_offset, ((size_t)N.nodes + 1) * 8, "outgoing edge offsets", s));
-  NET_TRY(alloc(N.out_edge, e * 8, "outgoing edges", s));
-  NET_TRY(alloc(key, e * 4, "edge keys", s));
-  NET_TRY(alloc(skey, e * 4, "edge keys", s));
-  NET_TRY(alloc(val, e * 8, "edge values", s));
-  emr::NetTurnArgs a{N.in_offset.as<int64_t>(), N.in_src.as<uint32_t>(), key.as<uint32_t>(),
-                     val.as<uint64_t>(), N.edge_dst.as<uint32_t>(), skey.as<uint32_t>(),
-                     N.out_offset.as<int64_t>(), N.nodes, N.edges};
-  if (e > 0) {
-    NET_HIP(emr_launch_net(20, &a, s));
-    int bits = 1;
-    while (bits < 32 && ((uint64_t)1 << bits) < (uint64_t)N.nodes) ++bits;
-    size_t tb = 0;
-    NET_HIP(emr_net_sort(nullptr, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
-                         N.out_edge.as<uint64_t>(), (uint32_t)e, bits, s));
-    NET_TRY(alloc(tmp, tb, "sort storage", s));
-    NET_HIP(emr_net_sort(tmp.p, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
-                         N.out_edge.as<uint64_t>(), (uint32_t)e, bits, s));
+// Items of a call over all genomes, about: twice what the chip holds at a time, so that their ends fall
+// together.
+constexpr double kLearnItems = 1024.0;
+constexpr size_t kLearnPlans = 64;  // numbers of patterns whose items a handle keeps
+
+void learn_sets(emr_networks& N, emr::LearnSet* out) {
+  auto& L = N.learn;
+  for (int k = 0; k < emr::kSets; ++k)
+    out[k] = {L.ent[k].as<uint2>(), L.edge[k].as<uint32_t>(), L.slices[k].as<emr::LearnSlice>(),
+              L.rows[k].as<uint16_t>(), L.n_slices.as<uint32_t>() + (size_t)k * N.n_genomes,
+              L.n_places.as<uint32_t>() + (size_t)k * N.n_genomes};
+}
+
+// The edges by source and the layouts of the genomes that fit a workgroup, on the first learning call's
+// stream.
+emr_status lay_out(emr_networks& N, hipStream_t s) {
+  auto& L = N.learn;
+  const size_t G = (size_t)N.n_genomes, E = (size_t)N.edges;
+  if (!L.laid) {
+    if (N.edges > (int64_t)UINT32_MAX - 1) return failf(EMR_E_LIMIT, "networks: too many edges");
+    L.fit.clear();
+    L.big.clear();
+    std::vector<int64_t> place(G, 0), slice(G, 0);
+    int64_t places = 0, slices = 0;
+    for (uint32_t g : N.order_host) {
+      const int64_t n = N.node_off[g + 1] - N.node_off[g], e = N.edge_off[g + 1] - N.edge_off[g];
+      place[g] = places;
+      slice[g] = slices;
+      if (n > (int64_t)emr::kLearnNodes || emr::learn_places(e, N.n_out) > INT32_MAX) {
+        L.big.push_back(g);
+        continue;
+      }
+      L.fit.push_back(g);
+      places += emr::learn_places(e, N.n_out);
+      slices += emr::learn_slices(n, e, N.n_out);
+    }
+    Dev key, skey, val, tmp;
+    NET_TRY(alloc(L.edge_dst, E * 4, "edge destinations", s));
+    NET_TRY(alloc(L.out_offset, ((size_t)N.nodes + 1) * 8, "outgoing edge offsets", s));
+    NET_TRY(alloc(L.out_edge, E * 8, "outgoing edges", s));
+    NET_TRY(alloc(key, E * 4, "edge keys", s));
+    NET_TRY(alloc(skey, E * 4, "edge keys", s));
+    NET_TRY(alloc(val, E * 8, "edge values", s));
+    emr::NetTurnArgs a{N.in_offset.as<int64_t>(), N.in_src.as<uint32_t>(), key.as<uint32_t>(),
+                       val.as<uint64_t>(), L.edge_dst.as<uint32_t>(), skey.as<uint32_t>(),
+                       L.out_offset.as<int64_t>(), N.nodes, N.edges};
+    if (E > 0) {
+      NET_HIP(emr_launch_net(20, &a, s));
+      int bits = 1;
+      while (bits < 32 && ((uint64_t)1 << bits) < (uint64_t)N.nodes) ++bits;
+      size_t tb = 0;
+      NET_HIP(emr_net_sort(nullptr, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
+                           L.out_edge.as<uint64_t>(), (uint32_t)E, bits, s));
+      NET_TRY(alloc(tmp, tb, "sort storage", s));
+      NET_HIP(emr_net_sort(tmp.p, &tb, key.as<uint32_t>(), skey.as<uint32_t>(), val.as<uint64_t>(),
+                           L.out_edge.as<uint64_t>(), (uint32_t)E, bits, s));
+    }
+    NET_HIP(emr_launch_net(21, &a, s));
+    NET_TRY(alloc(L.n_slices, emr::kSets * G * 4, "slice counts", s));
+    NET_TRY(alloc(L.n_places, emr::kSets * G * 4, "place counts", s));
+    for (int k = 0; k < emr::kSets; ++k) {
+      NET_TRY(alloc(L.ent[k], (size_t)places * 8, "laid out edges", s));
+      NET_TRY(alloc(L.edge[k], (size_t)places * 4, "laid out edge numbers", s));
+      NET_TRY(alloc(L.slices[k], (size_t)slices * sizeof(emr::LearnSlice), "slices", s));
+      NET_TRY(alloc(L.rows[k], (size_t)slices * 32, "rows", s));
+    }
+    const struct { Dev* d; const void* src; size_t bytes; } up[] = {
+        {&L.place, place.data(), G * 8}, {&L.slice, slice.data(), G * 8},
+        {&L.fits, L.fit.data(), L.fit.size() * 4}, {&L.large, L.big.data(), L.big.size() * 4}};
+    for (const auto& u : up) {
+      NET_TRY(alloc(*u.d, u.bytes, "learning tables", s));
+      NET_TRY(to_device(u.d->p, u.src, u.bytes, s));
+    }
+    emr::LearnLayoutArgs la{};
+    learn_sets(N, la.set);
+    la.genomes = L.fits.as<uint32_t>();
+    la.place = L.place.as<int64_t>();
+    la.slice = L.slice.as<int64_t>();
+    la.node_offset = N.node_offset.as<int64_t>();
+    la.node_in = N.node_in.as<int32_t>();
+    la.out_node = N.d_out_node.as<int32_t>();
+    la.in_offset = N.in_offset.as<int64_t>();
+    la.in_src = N.in_src.as<uint32_t>();
+    la.in_w = N.in_w.as<float>();
+    la.out_offset = L.out_offset.as<int64_t>();
+    la.out_edge = L.out_edge.as<uint64_t>();
+    la.count = (uint32_t)L.fit.size();
+    la.n_outputs = (uint32_t)N.n_out;
+    la.n_sub = (uint32_t)N.n_sub;
+    NET_HIP(emr_launch_net(22, &la, s));
+    NET_HIP(hipStreamSynchronize(s));  // (the tables above are the host's)
+    L.laid = true;
   }
-  NET_HIP(emr_launch_net(21, &a, s));
-  N.turned = true;
   return EMR_OK;
 }
 
-emr_status run_backward(emr_networks& M, emr::NetBackArgs& A, int32_t steps, hipStream_t s) {
+// The layouts' copies of the weights, after those changed.
+emr_status lay_weights(emr_networks& N, hipStream_t s) {
+  auto& L = N.learn;
+  if (!L.laid) return EMR_OK;
+  emr::LearnWeightsArgs wa{};
+  learn_sets(N, wa.set);
+  wa.genomes = L.fits.as<uint32_t>();
+  wa.place = L.place.as<int64_t>();
+  wa.in_w = N.in_w.as<float>();
+  wa.count = (uint32_t)L.fit.size();
+  NET_HIP(emr_launch_net(23, &wa, s));
+  return EMR_OK;
+}
+
+// The workgroups' shares of a call on this number of patterns: each genome's blocks in as many items as its
+// load asks for, the heaviest genomes first, in runs of one shape.
+emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learning::Plan** out,
+                      hipStream_t s) {
+  auto& L = N.learn;
+  for (auto& p : L.plans)
+    if (p->patterns == n_patterns) {
+      *out = p.get();
+      return EMR_OK;
+    }
+  auto plan = std::make_unique<emr_networks::Learning::Plan>();
+  plan->patterns = n_patterns;
+  struct Shape {
+    uint32_t groups, lds, blocks;
+  };
+  auto nodes = [&](uint32_t g) { return N.node_off[g + 1] - N.node_off[g]; };
+  auto edges = [&](uint32_t g) { return N.edge_off[g + 1] - N.edge_off[g]; };
+  auto shape = [&](uint32_t g) {
+    Shape S{n_patterns <= 4 ? 1u : (n_patterns <= 8 ? 2u : 4u), 0, 0};
+    while (S.groups > 1 && emr::learn_lds((uint32_t)nodes(g), S.groups) > emr::kLearnLds) S.groups /= 2;
+    S.lds = emr::learn_lds((uint32_t)nodes(g), S.groups);
+    S.blocks = ((uint32_t)n_patterns + 4 * S.groups - 1) / (4 * S.groups);
+    return S;
+  };
+  auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
+  double total = 0.0;
+  for (uint32_t g : L.fit) total += load(g) * shape(g).blocks;
+  // large workgroups alone on a compute unit, in pairs, and small ones
+  constexpr struct { uint32_t lds, threads; } kRuns[] = {
+      {emr::kLearnLds, 1024}, {emr::kLearnLds / 2, 1024}, {emr::kLearnLds / 4, 256}};
+  auto run_of = [&](uint32_t lds) { return lds > kRuns[1].lds ? 0 : (lds > kRuns[2].lds ? 1 : 2); };
+  std::vector<emr::LearnItem> items;
+  std::vector<emr::LearnJoin> joins;
+  int64_t part = 0;
+  for (int r = 0; r < 3; ++r) {
+    std::vector<std::pair<double, uint32_t>> by;
+    uint32_t lds = 0;
+    for (uint32_t g : L.fit) {
+      const Shape S = shape(g);
+      if (run_of(S.lds) != r) continue;
+      by.emplace_back(-load(g) * S.blocks, g);
+      lds = std::max(lds, S.lds);
+    }
+    std::stable_sort(by.begin(), by.end());
+    const uint32_t first = (uint32_t)items.size();
+    for (const auto& b : by) {
+      const uint32_t g = b.second;
+      const Shape S = shape(g);
+      const uint32_t n = (uint32_t)std::min<double>(
+          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnItems / std::max(total, 1.0))));
+      const int64_t stride = 2 * emr::learn_places(edges(g), N.n_out);
+      if (n > 1) joins.push_back({g, n, part, stride});
+      for (uint32_t k = 0; k < n; ++k, part += stride)
+        items.push_back({g, (uint32_t)((uint64_t)S.blocks * k / n), (uint32_t)((uint64_t)S.blocks * (k + 1) / n),
+                         S.groups, part, n == 1 ? 1u : 0u, 0});
+    }
+    if (items.size() > first)
+      plan->runs.push_back({first, (uint32_t)items.size() - first, kRuns[r].threads, lds});
+  }
+  if (items.size() > 0x7FFFFFFF) return failf(EMR_E_LIMIT, "networks: too many genomes x patterns");
+  NET_TRY(alloc(plan->items, items.size() * sizeof(emr::LearnItem), "learning items", s));
+  NET_TRY(to_device(plan->items.p, items.data(), items.size() * sizeof(emr::LearnItem), s));
+  NET_TRY(alloc(plan->joins, joins.size() * sizeof(emr::LearnJoin), "learning joins", s));
+  NET_TRY(to_device(plan->joins.p, joins.data(), joins.size() * sizeof(emr::LearnJoin), s));
+  NET_HIP(hipStreamSynchronize(s));  // (the tables above are the host's)
+  plan->n_joins = (uint32_t)joins.size();
+  plan->partial_floats = part;
+  if (L.plans.size() >= kLearnPlans) L.plans.erase(L.plans.begin());
+  L.plans.push_back(std::move(plan));
+  *out = L.plans.back().get();
+  return EMR_OK;
+}
+
+// Every learning call's arguments, its layouts and items made.
+emr_status learn_args(emr_networks& N, const float* inputs, int32_t n_patterns, int32_t steps,
+                      float* outputs, const emr::NetKept& K, emr::LearnArgs* A,
+                      emr_networks::Learning::Plan** plan, hipStream_t s) {
+  NET_TRY(check_device(&N));
+  if ((int64_t)((n_patterns + 15) / 16) * (N.nodes ? N.nodes : 1) > ((int64_t)1 << 38))
+    return failf(EMR_E_LIMIT, "networks: too many nodes x patterns");
+  NET_TRY(lay_out(N, s));
+  NET_TRY(plan_items(N, n_patterns, plan, s));
+  learn_sets(N, A->set);
+  A->items = (*plan)->items.as<emr::LearnItem>();
+  A->joins = (*plan)->joins.as<emr::LearnJoin>();
+  A->n_joins = (*plan)->n_joins;
+  A->place = N.learn.place.as<int64_t>();
+  A->slice = N.learn.slice.as<int64_t>();
+  A->node_offset = N.node_offset.as<int64_t>();
+  A->node_in = N.node_in.as<int32_t>();
+  A->out_node = N.d_out_node.as<int32_t>();
+  A->patterns = inputs;
+  A->outputs = outputs;
+  A->kept = K;
+  A->nodes = N.nodes;
+  A->n_inputs = (uint32_t)N.n_in;
+  A->n_outputs = (uint32_t)N.n_out;
+  A->n_patterns = (uint32_t)n_patterns;
+  A->n_sub = (uint32_t)N.n_sub;
+  A->steps = (uint32_t)steps;
+  return EMR_OK;
+}
+
+// The items' launches (step: 24 activation, 25 gradients).
+emr_status run_items(const emr_networks::Learning::Plan& plan, emr::LearnArgs& A, int step, hipStream_t s) {
+  for (const auto& r : plan.runs) {
+    A.first_item = r.first;
+    A.n_items = r.count;
+    A.threads = r.threads;
+    A.lds_bytes = r.lds;
+    NET_HIP(emr_launch_net(step, &A, s));
+  }
+  return EMR_OK;
+}
+
+emr_status run_keep(emr_networks& N, const float* inputs, int32_t n_patterns, int32_t steps,
+                    float* outputs, const emr::NetKept& K, hipStream_t s) {
+  emr::LearnArgs A{};
+  emr_networks::Learning::Plan* plan;
+  NET_TRY(learn_args(N, inputs, n_patterns, steps, outputs, K, &A, &plan, s));
+  NET_TRY(run_items(*plan, A, 24, s));
+  const auto& big = N.learn.big;
+  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
+  const size_t half = (size_t)pblocks * (size_t)N.nodes * 16;
+  if (!big.empty() && N.state.bytes < 2 * half) NET_TRY(alloc(N.state, 2 * half, "node states", s));
+  float* buf[2] = {N.state.as<float>(), reinterpret_cast<float*>(N.state.as<char>() + half)};
+  for (size_t done = 0; done < big.size(); done += 65535) {  // (a launch covers at most 65535 genomes)
+    emr::NetList list{};
+    list.order = N.learn.large.as<uint32_t>() + done;
+    list.n_genomes = (uint32_t)N.n_genomes;
+    list.count[0] = list.total = (uint32_t)std::min<size_t>(big.size() - done, 65535);
+    for (uint32_t k = 0; k < list.total; ++k)
+      list.max_nodes = std::max(list.max_nodes,
+                                (uint32_t)(N.node_off[big[done + k] + 1] - N.node_off[big[done + k]]));
+    emr::NetStateArgs sa{list, N.node_offset.as<int64_t>(), N.node_in.as<int32_t>(), inputs, buf[0], N.nodes,
+                         (uint32_t)N.n_in, (uint32_t)n_patterns, pblocks, K, {}};
+    NET_HIP(emr_launch_net(9, &sa, s));
+    int cur = 0;
+    for (int32_t t = 0; t < steps; ++t, cur ^= 1) {
+      emr::NetStepArgs st{list, N.node_offset.as<int64_t>(), N.node_in.as<int32_t>(),
+                          N.in_offset.as<int64_t>(), N.in_src.as<uint32_t>(), N.in_w.as<float>(), buf[cur],
+                          buf[cur ^ 1], N.nodes, pblocks, K, (uint32_t)t};
+      NET_HIP(emr_launch_net(10, &st, s));
+    }
+    emr::NetOutArgs oa{};
+    oa.list = list;
+    oa.node_offset = N.node_offset.as<int64_t>();
+    oa.out_node = N.d_out_node.as<int32_t>();
+    oa.state = buf[cur];
+    oa.outputs = outputs;
+    oa.nodes = N.nodes;
+    oa.n_outputs = (uint32_t)N.n_out;
+    oa.n_patterns = (uint32_t)n_patterns;
+    NET_HIP(emr_launch_net(11, &oa, s));
+  }
+  return mark_done(N, s);
+}
+
+emr_status run_backward(emr_networks& N, const float* inputs, int32_t n_patterns, int32_t steps,
+                        const float* outputs, const emr::NetKept& K, const float* grad_outputs,
+                        float* grad_w, float* grad_inputs, hipStream_t s) {
   if (steps == 0) {  // the outputs are their initial states: nothing moves them
-    NET_HIP(emr_launch_net(25, &A, s));
-    return mark_done(M, s);
+    NET_TRY(check_device(&N));
+    emr::LearnFillArgs f{grad_w, N.edges};
+    NET_HIP(emr_launch_net(30, &f, s));
+    f = {grad_inputs, (int64_t)N.n_genomes * n_patterns * N.n_in};
+    if (grad_inputs) NET_HIP(emr_launch_net(30, &f, s));
+    return mark_done(N, s);
   }
-  const size_t half = (size_t)A.pblocks * (size_t)(M.nodes ? M.nodes : 1) * 16;
-  if (!M.back.p || M.back.bytes < 2 * half) NET_TRY(alloc(M.back, 2 * half, "derivatives", s));
-  float* buf[2] = {M.back.as<float>(), reinterpret_cast<float*>(M.back.as<char>() + half)};
-  A.gz_before = buf[0];
-  NET_HIP(emr_launch_net(22, &A, s));
-  int cur = 0;
-  for (int32_t t = steps; t >= 1; --t, cur ^= 1) {
-    A.gz = buf[cur];
-    A.gz_before = buf[cur ^ 1];
-    A.step = (uint32_t)t;
-    A.last = t == steps ? 1u : 0u;
-    NET_HIP(emr_launch_net(23, &A, s));
-    NET_HIP(emr_launch_net(24, &A, s));
+  emr::LearnArgs A{};
+  emr_networks::Learning::Plan* plan;
+  NET_TRY(learn_args(N, inputs, n_patterns, steps, const_cast<float*>(outputs), K, &A, &plan, s));
+  auto& L = N.learn;
+  const size_t need = (size_t)plan->partial_floats * 4;
+  if (L.partial.bytes < need) NET_TRY(alloc(L.partial, need, "partial derivatives", s));
+  A.partial = L.partial.as<float>();
+  A.grad_outputs = grad_outputs;
+  A.grad_w = grad_w;
+  A.grad_inputs = grad_inputs;
+  NET_TRY(run_items(*plan, A, 25, s));
+  NET_HIP(emr_launch_net(26, &A, s));
+  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
+  size_t half = 0;
+  for (uint32_t g : L.big)
+    half = std::max(half, (size_t)pblocks * (size_t)(N.node_off[g + 1] - N.node_off[g]) * 16);
+  if (L.back.bytes < 2 * half) NET_TRY(alloc(L.back, 2 * half, "derivatives", s));
+  for (uint32_t g : L.big) {
+    emr::NetBackArgs B{};
+    B.genome = g;
+    B.node0 = N.node_off[g];
+    B.size = N.node_off[g + 1] - B.node0;
+    B.edge0 = N.edge_off[g];
+    B.edge1 = N.edge_off[g + 1];
+    B.node_in = A.node_in;
+    B.out_node = A.out_node;
+    B.in_offset = N.in_offset.as<int64_t>();
+    B.in_src = N.in_src.as<uint32_t>();
+    B.in_w = N.in_w.as<float>();
+    B.dst = L.edge_dst.as<uint32_t>();
+    B.out_offset = L.out_offset.as<int64_t>();
+    B.out_edge = L.out_edge.as<uint64_t>();
+    B.patterns = inputs;
+    B.outputs = outputs;
+    B.grad_outputs = grad_outputs;
+    B.grad_w = grad_w;
+    B.grad_inputs = grad_inputs;
+    B.kept = K;
+    B.nodes = N.nodes;
+    B.n_inputs = A.n_inputs;
+    B.n_outputs = A.n_outputs;
+    B.n_patterns = A.n_patterns;
+    B.pblocks = pblocks;
+    float* buf[2] = {L.back.as<float>(), L.back.as<float>() + (size_t)pblocks * (size_t)B.size * 4};
+    B.gz_before = buf[0];
+    NET_HIP(emr_launch_net(27, &B, s));
+    int cur = 0;
+    for (int32_t t = steps; t >= 1; --t, cur ^= 1) {
+      B.gz = buf[cur];
+      B.gz_before = buf[cur ^ 1];
+      B.step = (uint32_t)t;
+      B.last = t == steps ? 1u : 0u;
+      NET_HIP(emr_launch_net(28, &B, s));
+      NET_HIP(emr_launch_net(29, &B, s));
+    }
   }
-  return mark_done(M, s);
+  return mark_done(N, s);
 }
 
 // The handle's substrate: its inputs and outputs numbered in substrate order.
@@ -1368,6 +1682,7 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
   hipStream_t s = (hipStream_t)stream;
   if (net->edges > 0)
     NET_HIP(hipMemcpyAsync(M.in_w.p, w, (size_t)net->edges * 4, hipMemcpyDeviceToDevice, s));
+  NET_TRY(lay_weights(M, s));
   return mark_done(M, s);
 }
 
@@ -1379,7 +1694,7 @@ emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t s
 
 emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32_t n_patterns,
                              int32_t steps, float* outputs, uint8_t* kept, int64_t kept_bytes,
-                             void* stream) {
+                             void* stream) try {
   if (!net || !inputs || !outputs) return failf(EMR_E_INVAL, "networks: NULL argument");
   emr::NetKept K{};
   int64_t need = 0;
@@ -1390,8 +1705,10 @@ emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32
     return failf(EMR_E_CAPACITY, "networks: kept holds %lld bytes of %lld", (long long)kept_bytes,
                  (long long)need);
   if (need == 0) K.codes = nullptr;
-  return run_forward(net, inputs, n_patterns, steps, outputs, nullptr, nullptr, (hipStream_t)stream,
-                     &K);
+  return run_keep(const_cast<emr_networks&>(*net), inputs, n_patterns, steps, outputs, K,
+                  (hipStream_t)stream);
+} catch (const std::bad_alloc&) {
+  return failf(EMR_E_NOMEM, "networks: out of host memory");
 }
 
 emr_status emr_activate_backward(const emr_networks* net, const float* inputs, int32_t n_patterns,
@@ -1400,42 +1717,16 @@ emr_status emr_activate_backward(const emr_networks* net, const float* inputs, i
                                  float* grad_inputs, void* stream) try {
   if (!net || !inputs || !outputs || !grad_outputs || !grad_w)
     return failf(EMR_E_INVAL, "networks: NULL argument");
-  emr::NetBackArgs A{};
+  emr::NetKept K{};
   int64_t need = 0;
-  NET_TRY(kept_layout(net, n_patterns, steps, const_cast<uint8_t*>(kept), &A.kept, &need));
+  NET_TRY(kept_layout(net, n_patterns, steps, const_cast<uint8_t*>(kept), &K, &need));
   if (need > 0 && (!kept || (uintptr_t)kept % 16 != 0))
     return failf(EMR_E_INVAL, "networks: kept is NULL or not aligned to 16 bytes");
   if (kept_bytes < need)
     return failf(EMR_E_CAPACITY, "networks: kept holds %lld bytes of %lld", (long long)kept_bytes,
                  (long long)need);
-  NET_TRY(check_device(net));
-  emr_networks& M = const_cast<emr_networks&>(*net);
-  hipStream_t s = (hipStream_t)stream;
-  A.pblocks = ((uint32_t)n_patterns + 3) / 4;
-  if ((int64_t)A.pblocks * (net->nodes ? net->nodes : 1) > ((int64_t)1 << 40))
-    return failf(EMR_E_LIMIT, "networks: too many nodes x patterns");
-  NET_TRY(turn_edges(M, s));
-  A.node_offset = net->node_offset.as<int64_t>();
-  A.node_in = net->node_in.as<int32_t>();
-  A.out_node = net->d_out_node.as<int32_t>();
-  A.in_offset = net->in_offset.as<int64_t>();
-  A.in_src = net->in_src.as<uint32_t>();
-  A.in_w = net->in_w.as<float>();
-  A.dst = net->edge_dst.as<uint32_t>();
-  A.out_offset = net->out_offset.as<int64_t>();
-  A.out_edge = net->out_edge.as<uint64_t>();
-  A.patterns = inputs;
-  A.outputs = outputs;
-  A.grad_outputs = grad_outputs;
-  A.grad_w = grad_w;
-  A.grad_inputs = grad_inputs;
-  A.nodes = net->nodes;
-  A.edges = net->edges;
-  A.n_genomes = (uint32_t)net->n_genomes;
-  A.n_inputs = (uint32_t)net->n_in;
-  A.n_outputs = (uint32_t)net->n_out;
-  A.n_patterns = (uint32_t)n_patterns;
-  return run_backward(M, A, steps, s);
+  return run_backward(const_cast<emr_networks&>(*net), inputs, n_patterns, steps, outputs, K,
+                      grad_outputs, grad_w, grad_inputs, (hipStream_t)stream);
 } catch (const std::bad_alloc&) {
   return failf(EMR_E_NOMEM, "networks: out of host memory");
 }
@@ -1478,7 +1769,7 @@ emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const 
   a.logp = logp;
   const uint32_t groups = (a.n + emr::kDrawPart - 1) / emr::kDrawPart;
   a.part = (groups + emr::kDrawSegs - 1) / emr::kDrawSegs * emr::kDrawPart;
-  const hipError_t e = emr_launch_net(30, &a, (hipStream_t)stream);
+  const hipError_t e = emr_launch_net(40, &a, (hipStream_t)stream);
   if (e != hipSuccess) return failf(EMR_E_DEVICE, "sample: %s", hipGetErrorString(e));
   return EMR_OK;
 }
@@ -1513,7 +1804,7 @@ emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const
   a.loss = loss;
   a.grad = grad;
   a.grad_stride = grad_stride;
-  const hipError_t e = emr_launch_net(31, &a, (hipStream_t)stream);
+  const hipError_t e = emr_launch_net(41, &a, (hipStream_t)stream);
   if (e != hipSuccess) return failf(EMR_E_DEVICE, "loss: %s", hipGetErrorString(e));
   return EMR_OK;
 }
