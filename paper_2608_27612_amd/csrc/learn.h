@@ -60,6 +60,7 @@ struct NetBackArgs {
 };
 
 constexpr uint32_t kLightEdges = 64;
+constexpr uint32_t kLearnPad = 4;  // a slice's length is a multiple of this
 constexpr int kInHid = 0, kInInp = 1, kOutHid = 2, kOutInp = 3, kSets = 4;
 constexpr uint32_t kNoEdge = 0xFFFFFFFFu;
 
@@ -86,15 +87,18 @@ constexpr uint32_t kLearnLds = 160u * 1024u;
 inline constexpr uint32_t learn_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 48u * groups; }
 constexpr uint32_t kLearnNodes = kLearnLds / 48u - 1u;
 
-// Places and slices of one of a genome's layouts, at most: a heavy row or an output leaves up to fifteen
-// places empty; falling rows of at most min(kLightEdges, e) edges leave sixteen times that.
-inline constexpr int64_t learn_places(int64_t e, int64_t n_out) {
-  return (e + e / 4 + 15 * n_out + 16 * (e < (int64_t)kLightEdges ? e : (int64_t)kLightEdges) + 31) / 16 * 16;
-}
+// Places and slices of one of a genome's layouts, at most: a slice's length is rounded up by up to kLearnPad - 1
+// sixteens; a heavy row or an output leaves up to fifteen places more; falling rows of at most
+// min(kLightEdges, e) edges leave sixteen times that.
 inline constexpr int64_t learn_slices(int64_t n, int64_t e, int64_t n_out) {
   return n / 16 + 2 + e / kLightEdges + n_out;
 }
-
+inline constexpr int64_t learn_places(int64_t n, int64_t e, int64_t n_out) {
+  const int64_t light = e < (int64_t)kLightEdges ? e : (int64_t)kLightEdges;
+  const int64_t used = e < n ? e : n;  // (rows with edges)
+  return (e + 15 * (e / kLightEdges + n_out) + 16 * light +
+          16 * (kLearnPad - 1) * learn_slices(used, e, n_out) + 31) / 16 * 16;
+}
 struct LearnLayoutArgs {
   LearnSet set[kSets];
   const uint32_t* genomes;     // [count]

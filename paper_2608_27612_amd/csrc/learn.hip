@@ -185,6 +185,10 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* part, uint3
   return before + x - v;
 }
 
+__device__ __forceinline__ uint32_t padded(uint32_t len) {
+  return (len + kLearnPad - 1u) / kLearnPad * kLearnPad;
+}
+
 constexpr int kLayoutThreads = 512;
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
 
@@ -255,11 +259,11 @@ __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs
     if (k == kAbsent) continue;
     const uint32_t r = rank[i];
     if (r < nh) {
-      slices[r] = {0, ((k & 0x7FFFFFFFu) + 15u) / 16u, 0, 1};
+      slices[r] = {0, padded(((k & 0x7FFFFFFFu) + 15u) / 16u), 0, 1};
       for (uint32_t j = 0; j < 16; ++j) row_of[16u * r + j] = (uint16_t)i;
     } else {
       const uint32_t s = nh + (r - nh) / 16u;
-      if ((r - nh) % 16u == 0) slices[s] = {0, k, 0, 0};
+      if ((r - nh) % 16u == 0) slices[s] = {0, padded(k), 0, 0};
       row_of[16u * s + (r - nh) % 16u] = (uint16_t)i;
     }
   }
@@ -375,7 +379,7 @@ __device__ __forceinline__ void heavy_sum(float4& a) {
   }
 }
 
-// What a lane works on: group q of four patterns of the row at place r of slice s.
+// What a lane works on: group q of four patterns of the row at place r of a slice.
 template <int LN>
 struct Place {
   uint32_t q, r;
@@ -388,39 +392,51 @@ struct Place {
 template <int LN, bool FIRST>
 __device__ __forceinline__ Place<LN> place_of(const LearnSlice* slices, const uint16_t* rows, uint32_t at,
                                               uint32_t ns, uint32_t lane) {
-  constexpr uint32_t per = 4 / LN;  // slices of a wave
   Place<LN> P;
   P.q = lane % LN;
   P.r = lane / LN % 16u;
-  P.most = 0;
-  P.any_heavy = false;
-#pragma unroll
-  for (uint32_t j = 0; j < per; ++j) {  // (the wave's)
-    if (at + j >= ns) break;
-    const uint32_t l = FIRST ? slices[at + j].first : slices[at + j].len;
-    P.most = l > P.most ? l : P.most;
-    P.any_heavy |= slices[at + j].heavy != 0;
+  auto length = [](const LearnSlice& S) {
+    return FIRST ? (S.first + kLearnPad - 1u) / kLearnPad * kLearnPad : S.len;
+  };
+  if constexpr (LN == 4) {  // the wave's slice
+    const LearnSlice S = slices[at];
+    P.base = S.base;
+    P.len = P.most = length(S);
+    P.heavy = P.any_heavy = S.heavy != 0;
+    P.row = rows[16u * at + P.r];
+  } else {
+    P.most = 0;
+    P.any_heavy = false;
+    for (uint32_t j = 0; j < 4u / LN; ++j) {
+      if (at + j >= ns) break;
+      const uint32_t l = length(slices[at + j]);
+      P.most = l > P.most ? l : P.most;
+      P.any_heavy |= slices[at + j].heavy != 0;
+    }
+    const uint32_t s = at + lane / (16u * LN);
+    const bool in = s < ns;
+    const LearnSlice S = slices[in ? s : at];
+    P.base = S.base;
+    P.len = in ? length(S) : 0u;
+    P.heavy = in && S.heavy != 0;
+    P.row = in ? rows[16u * s + P.r] : kNoRow;
   }
-  const uint32_t s = at + lane / (16u * LN);
-  const bool in = s < ns;
-  const LearnSlice S = slices[in ? s : at];
-  P.base = S.base + P.r;
-  P.len = in ? (FIRST ? S.first : S.len) : 0u;
-  P.heavy = in && S.heavy != 0;
-  P.row = in ? rows[16u * s + P.r] : kNoRow;
   P.writes = P.row != kNoRow && (!P.heavy || P.r == 0);
   return P;
 }
 
-// The edge at the k-th place of a lane's row, past its end an empty one.
-__device__ __forceinline__ uint2 edge_at(const uint2* __restrict__ e, uint32_t k, uint32_t len, uint32_t n) {
-  uint32_t x = n, y = 0;
-  if (k < len) {
-    const uint64_t v = *reinterpret_cast<const uint64_t*>(e + 16u * k);
-    x = (uint32_t)v;
-    y = (uint32_t)(v >> 32);
+// Four edges from the k-th of a lane's row on; a wave whose slices differ in length takes empty ones past
+// its own slice's end (lengths are multiples of four).
+template <int LN>
+__device__ __forceinline__ void edges_at(const uint64_t* __restrict__ e, uint32_t k, const Place<LN>& P,
+                                         uint32_t n, uint64_t (&v)[kLearnPad]) {
+  if (LN == 4 || k < P.len) {
+#pragma unroll
+    for (uint32_t j = 0; j < kLearnPad; ++j) v[j] = e[16u * (k + j) + P.r];
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < kLearnPad; ++j) v[j] = n;
   }
-  return make_uint2(x, y);
 }
 
 // The weighted sums of a slice's rows over x (the values of the genome's nodes, LN float4 each).
@@ -428,18 +444,20 @@ template <int LN>
 __device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint2* __restrict__ ent,
                                            const float4* x, uint32_t n) {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const uint2* e = ent + P.base;
-  constexpr int U = 4;
-  uint2 a[U], b[U];
+  if (P.most > 0) {
+    const uint64_t* e = reinterpret_cast<const uint64_t*>(ent) + P.base;
+    uint64_t a[kLearnPad], b[kLearnPad];
+    edges_at<LN>(e, 0, P, n, a);
+    for (uint32_t k = kLearnPad;; k += kLearnPad) {
+      const bool more = k < P.most;
+      if (more) edges_at<LN>(e, k, P, n, b);
 #pragma unroll
-  for (int j = 0; j < U; ++j) a[j] = edge_at(e, (uint32_t)j, P.len, n);
-  for (uint32_t k = 0; k < P.most; k += U) {
+      for (uint32_t j = 0; j < kLearnPad; ++j)
+        fma4(acc, __uint_as_float((uint32_t)(a[j] >> 32)), x[(uint32_t)a[j] * LN + P.q]);
+      if (!more) break;
 #pragma unroll
-    for (int j = 0; j < U; ++j) b[j] = edge_at(e, k + U + (uint32_t)j, P.len, n);
-#pragma unroll
-    for (int j = 0; j < U; ++j) fma4(acc, __uint_as_float(a[j].y), x[a[j].x * LN + P.q]);
-#pragma unroll
-    for (int j = 0; j < U; ++j) a[j] = b[j];
+      for (uint32_t j = 0; j < kLearnPad; ++j) a[j] = b[j];
+    }
   }
   if (P.any_heavy) {
     float4 h = acc;
@@ -456,39 +474,46 @@ __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __r
                                             const float4* gz, uint32_t n, const float4& s,
                                             float* __restrict__ sum) {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const uint2* e = ent + P.base;
-  constexpr int U = 4;
-  uint2 a[U], b[U];
+  if (P.most > 0) {
+    const uint64_t* e = reinterpret_cast<const uint64_t*>(ent) + P.base;
+    float* mine = sum + P.base;
+    // each of a row's lanes adds the derivatives of one edge in LN
+    constexpr int own = (int)kLearnPad / LN;
+    uint64_t a[kLearnPad], b[kLearnPad];
+    float had[own], next[own];
+    auto sums_at = [&](uint32_t k, float (&v)[own]) {
 #pragma unroll
-  for (int j = 0; j < U; ++j) a[j] = edge_at(e, (uint32_t)j, P.len, n);
-  for (uint32_t k = 0; k < P.most; k += U) {
+      for (int c = 0; c < own; ++c)
+        v[c] = LN == 4 || k < P.len ? mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] : 0.0f;
+    };
+    edges_at<LN>(e, 0, P, n, a);
+    sums_at(0, had);
+    for (uint32_t k = 0;; k += kLearnPad) {
+      const bool more = k + kLearnPad < P.most;
+      if (more) {
+        edges_at<LN>(e, k + kLearnPad, P, n, b);
+        sums_at(k + kLearnPad, next);
+      }
+      float d[kLearnPad];
 #pragma unroll
-    for (int j = 0; j < U; ++j) b[j] = edge_at(e, k + U + (uint32_t)j, P.len, n);
-    // each of a row's lanes adds the derivatives of U / LN edges
-    constexpr int own = U / LN;
-    float before[own];
+      for (uint32_t j = 0; j < kLearnPad; ++j) {
+        const float4 v = gz[(uint32_t)a[j] * LN + P.q];
+        fma4(acc, __uint_as_float((uint32_t)(a[j] >> 32)), v);
+        d[j] = row_sum<LN>(dot4(v, s));
+      }
 #pragma unroll
-    for (int c = 0; c < own; ++c) {
-      const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
-      before[c] = kk < P.len ? sum[P.base + 16u * kk] : 0.0f;
+      for (int c = 0; c < own; ++c) {
+        float v = d[c * LN];
+#pragma unroll
+        for (int j = 1; j < LN; ++j) v = P.q == (uint32_t)j ? d[c * LN + j] : v;
+        if (LN == 4 || k < P.len) mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] = had[c] + v;
+      }
+      if (!more) break;
+#pragma unroll
+      for (uint32_t j = 0; j < kLearnPad; ++j) a[j] = b[j];
+#pragma unroll
+      for (int c = 0; c < own; ++c) had[c] = next[c];
     }
-    float d[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const float4 v = gz[a[j].x * LN + P.q];
-      fma4(acc, __uint_as_float(a[j].y), v);
-      d[j] = row_sum<LN>(dot4(v, s));
-    }
-#pragma unroll
-    for (int c = 0; c < own; ++c) {
-      const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
-      float v = d[c * LN];
-#pragma unroll
-      for (int j = 1; j < LN; ++j) v = P.q == (uint32_t)j ? d[c * LN + j] : v;
-      if (kk < P.len) sum[P.base + 16u * kk] = before[c] + v;
-    }
-#pragma unroll
-    for (int j = 0; j < U; ++j) a[j] = b[j];
   }
   if (P.any_heavy) {
     float4 h = acc;
@@ -686,7 +711,15 @@ __global__ void __launch_bounds__(kNetThreads) k_learn_join(LearnArgs A) {
     if (e == kNoEdge) continue;
     const float* p = A.partial + J.part + i;
     float sum = 0.0f;
-    for (uint32_t k = 0; k < J.items; ++k) sum += p[k * J.stride];
+    uint32_t k = 0;
+    for (; k + 8 <= J.items; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = p[(k + j) * J.stride];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += v[j];
+    }
+    for (; k < J.items; ++k) sum += p[k * J.stride];
     A.grad_w[e] = sum;
   }
 }
@@ -750,7 +783,7 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       for (uint32_t a = 0; a < A.n_joins; a += 65535u) {
         LearnArgs B = A;
         B.joins = A.joins + a;
-        hipLaunchKernelGGL(k_learn_join, dim3(32, A.n_joins - a < 65535u ? A.n_joins - a : 65535u), blk, 0, s,
+        hipLaunchKernelGGL(k_learn_join, dim3(64, A.n_joins - a < 65535u ? A.n_joins - a : 65535u), blk, 0, s,
                            B);
       }
       break;

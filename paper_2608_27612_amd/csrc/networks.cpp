@@ -1063,9 +1063,9 @@ emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps,
   return EMR_OK;
 }
 
-// Items of a call over all genomes, about: twice what the chip holds at a time, so that their ends fall
-// together.
-constexpr double kLearnItems = 1024.0;
+// Waves of a call's items over all genomes, about: sixteen times what the chip holds, so that the items' ends
+// fall together (150 networks on 1000 patterns, gradients: 2.56 ms at 16384, 2.36 at 32768, 2.06 at 65536).
+constexpr double kLearnWaves = 65536.0;
 constexpr size_t kLearnPlans = 64;  // numbers of patterns whose items a handle keeps
 
 void learn_sets(emr_networks& N, emr::LearnSet* out) {
@@ -1091,12 +1091,12 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
       const int64_t n = N.node_off[g + 1] - N.node_off[g], e = N.edge_off[g + 1] - N.edge_off[g];
       place[g] = places;
       slice[g] = slices;
-      if (n > (int64_t)emr::kLearnNodes || emr::learn_places(e, N.n_out) > INT32_MAX) {
+      if (n > (int64_t)emr::kLearnNodes || emr::learn_places(n, e, N.n_out) > INT32_MAX) {
         L.big.push_back(g);
         continue;
       }
       L.fit.push_back(g);
-      places += emr::learn_places(e, N.n_out);
+      places += emr::learn_places(n, e, N.n_out);
       slices += emr::learn_slices(n, e, N.n_out);
     }
     Dev key, skey, val, tmp;
@@ -1222,8 +1222,9 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
       const uint32_t g = b.second;
       const Shape S = shape(g);
       const uint32_t n = (uint32_t)std::min<double>(
-          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnItems / std::max(total, 1.0))));
-      const int64_t stride = 2 * emr::learn_places(edges(g), N.n_out);
+          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnWaves /
+                                                    (std::max(total, 1.0) * (kRuns[r].threads / 64)))));
+      const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
       if (n > 1) joins.push_back({g, n, part, stride});
       for (uint32_t k = 0; k < n; ++k, part += stride)
         items.push_back({g, (uint32_t)((uint64_t)S.blocks * k / n), (uint32_t)((uint64_t)S.blocks * (k + 1) / n),
