@@ -142,56 +142,149 @@ __device__ __forceinline__ uint32_t ties_of(double target, uint64_t before, uint
   return (uint32_t)m;
 }
 
-// A workgroup's memory.
+// ----------------------------------------------------------------------------- short rows
+
+// Rows of up to G scores, G lanes each, a score to a lane. An entry's rank, and the weight before it by
+// rank, come from comparing it with the G others.
+template <int TYPE, int G>
+__global__ void __launch_bounds__(256) k_sample_short(SampleArgs A) {
+  using T = typename Score<TYPE>::T;
+  const uint32_t lane = threadIdx.x % G;
+  const int64_t rows = (int64_t)gridDim.x * (256 / G);
+  for (int64_t r0 = (int64_t)blockIdx.x * (256 / G); r0 < A.rows; r0 += rows) {
+    const int64_t r = r0 + threadIdx.x / G < A.rows ? r0 + threadIdx.x / G : A.rows - 1;
+    const bool mine = r == r0 + threadIdx.x / G;  // (lanes past the rows shadow the last one)
+    const T* row = static_cast<const T*>(A.x) + r * A.stride;
+    const float x = lane < A.n ? clean(Score<TYPE>::get(row[lane])) : -INFINITY;
+    const uint32_t key = lane < A.n ? key_of(x) : 0u;
+    uint32_t top = key;
+#pragma unroll
+    for (int o = G / 2; o >= 1; o >>= 1) {
+      const uint32_t w = (uint32_t)__shfl_xor((int)top, o, G);
+      top = w > top ? w : top;
+    }
+    RowRule R = row_rule(A, r, (uint64_t)top << 32);
+    uint32_t q = x > -INFINITY ? weight_of(x, R) : 0u;
+    if (R.greedy || R.k > 0 || R.p < 1.0) {
+      uint32_t rank = 0;
+      uint64_t above = 0;
+#pragma unroll 8
+      for (int j = 0; j < G; ++j) {
+        const uint32_t kj = (uint32_t)__shfl((int)key, j, G), qj = (uint32_t)__shfl((int)q, j, G);
+        const bool before = kj > key || (kj == key && (uint32_t)j < lane);
+        rank += before ? 1u : 0u;
+        above += before ? qj : 0u;
+      }
+      if (R.greedy) q = rank == 0 && x > -INFINITY ? (uint32_t)kOne : 0u;
+      else if (R.k > 0 && rank >= R.k) q = 0;
+      if (!R.greedy && R.p < 1.0) {
+        uint64_t total = q;
+#pragma unroll
+        for (int o = G / 2; o >= 1; o >>= 1) total += (uint64_t)__shfl_xor((unsigned long long)total, o, G);
+        if (above != 0 && !((double)above < R.p * (double)total)) q = 0;
+      }
+    }
+    if (!R.greedy && q < R.least) q = 0;
+    uint64_t run = q;
+#pragma unroll
+    for (int o = 1; o < G; o <<= 1) {
+      const uint64_t w = (uint64_t)__shfl_up((unsigned long long)run, o, G);
+      if (lane >= (uint32_t)o) run += w;
+    }
+    const uint64_t total = (uint64_t)__shfl((unsigned long long)run, G - 1, G);
+    for (int64_t d0 = 0; d0 < A.draws; d0 += G) {
+      const int64_t d = d0 + lane;
+      const bool draws = d < A.draws;
+      const uint64_t target = total > 0 && draws ? target_of(A.u[r * A.draws + d], total) : 0;
+      uint32_t at = 0;  // entries whose running sum does not exceed the target
+#pragma unroll
+      for (int step = G / 2; step >= 1; step >>= 1)
+        if ((uint64_t)__shfl((unsigned long long)run, (int)(at + step - 1), G) <= target) at += step;
+      const float y = __shfl(x, (int)at, G);
+      if (!draws || !mine) continue;
+      A.index[r * A.draws + d] = total > 0 ? (int32_t)at : -1;
+      if (A.logp)
+        A.logp[r * A.draws + d] = total == 0 ? -INFINITY : (R.greedy ? 0.0f : logp_of(y, R, total));
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- a workgroup for a row
+
+constexpr uint32_t kFew = 64;  // entries that a wave ranks among themselves
+
+// A workgroup's memory: NT threads, bins of scores, and the row's parts.
+template <int NT, int PARTS>
 struct RowShared {
-  uint64_t part[kDrawSegs];        // the parts' sums, then their running sums
-  uint64_t mass[256];
-  uint32_t count[256];
-  uint64_t wave[kDrawThreads / kWave];
-  uint64_t out[2];
+  static constexpr int kBins = 2 * NT;
+  uint64_t part[PARTS];       // the parts' sums, then their running sums
+  uint64_t mass[kBins];       // the bins' weights and entries, then their running sums
+  uint32_t count[kBins];
+  uint64_t wave[NT / kWave];
+  uint32_t wcount[NT / kWave];
+  uint64_t cand[kFew];
+  uint32_t cq[kFew];
+  uint32_t n, bin, lo, hi;
+  uint64_t cut, below;
 };
 
-__device__ __forceinline__ uint64_t block_max(uint64_t v, RowShared& S) {
+template <typename SH, int NT>
+__device__ __forceinline__ uint64_t block_max(uint64_t v, SH& S) {
   v = wave_max(v);
   if (threadIdx.x % kWave == 0) S.wave[threadIdx.x / kWave] = v;
   __syncthreads();
   uint64_t b = 0;
-  for (int i = 0; i < kDrawThreads / kWave; ++i) b = S.wave[i] > b ? S.wave[i] : b;
+#pragma unroll
+  for (int i = 0; i < NT / kWave; ++i) b = S.wave[i] > b ? S.wave[i] : b;
   __syncthreads();
   return b;
 }
 
-// The parts' sums to running sums; returns the total.
-__device__ __forceinline__ uint64_t scan_parts(RowShared& S, uint32_t parts) {
+// PER sums of each thread to running sums over the workgroup; returns the total.
+template <int NT, int PER, typename SH>
+__device__ __forceinline__ uint64_t block_scan(uint64_t (&v)[PER], SH& S) {
   const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
-  constexpr uint32_t per = kDrawSegs / kDrawThreads;
-  uint64_t v[per], sum = 0;
+  uint64_t sum = 0;
 #pragma unroll
-  for (uint32_t j = 0; j < per; ++j) {
-    const uint32_t i = threadIdx.x * per + j;
-    v[j] = i < parts ? S.part[i] : 0;
-    sum += v[j];
-  }
+  for (int j = 0; j < PER; ++j) sum += v[j];
   const uint64_t in = wave_scan(sum, lane);
   if (lane == kWave - 1) S.wave[wv] = in;
   __syncthreads();
   uint64_t run = in - sum, total = 0;
-  for (uint32_t i = 0; i < kDrawThreads / kWave; ++i) {
+#pragma unroll
+  for (uint32_t i = 0; i < NT / kWave; ++i) {
     run += i < wv ? S.wave[i] : 0;
     total += S.wave[i];
   }
+  __syncthreads();
 #pragma unroll
-  for (uint32_t j = 0; j < per; ++j) {
-    run += v[j];
+  for (int j = 0; j < PER; ++j) v[j] = run += v[j];
+  return total;
+}
+
+// The parts' sums to running sums; returns the total.
+template <int NT, int PARTS, typename SH>
+__device__ __forceinline__ uint64_t scan_parts(SH& S, uint32_t parts) {
+  constexpr int per = PARTS / NT;
+  uint64_t v[per];
+#pragma unroll
+  for (int j = 0; j < per; ++j) {
     const uint32_t i = threadIdx.x * per + j;
-    if (i < parts) S.part[i] = run;
+    v[j] = i < parts ? S.part[i] : 0;
+  }
+  const uint64_t total = block_scan<NT, per>(v, S);
+#pragma unroll
+  for (int j = 0; j < per; ++j) {
+    const uint32_t i = threadIdx.x * per + j;
+    if (i < parts) S.part[i] = v[j];
   }
   __syncthreads();
   return total;
 }
 
 // The first part whose running sum exceeds `target`.
-__device__ __forceinline__ uint32_t find_part(const RowShared& S, uint32_t parts, uint64_t target) {
+template <typename SH>
+__device__ __forceinline__ uint32_t find_part(const SH& S, uint32_t parts, uint64_t target) {
   uint32_t lo = 0, hi = parts - 1;
   while (lo < hi) {
     const uint32_t mid = (lo + hi) / 2;
@@ -201,201 +294,424 @@ __device__ __forceinline__ uint32_t find_part(const RowShared& S, uint32_t parts
   return lo;
 }
 
-// f(i, x) for every entry of the row, a wave to a part, four entries to a lane.
-template <int TYPE, typename F>
-__device__ __forceinline__ void each(const SampleArgs& A, const typename Score<TYPE>::T* row, F&& f) {
-  const uint32_t lane = threadIdx.x % kWave;
-  for (uint64_t a = (uint64_t)(threadIdx.x / kWave) * A.part; a < A.n;
-       a += (uint64_t)(kDrawThreads / kWave) * A.part)
-    for (uint32_t i = (uint32_t)a + 4u * lane; i < A.n && i - (uint32_t)a < A.part; i += 4u * kWave) {
-      float v[4];
-      load4<TYPE>(row, i, A.n, A.vec != 0, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f(i + (uint32_t)j, v[j]);
-    }
+// A register's value that the compiler does not follow: what a pass over a row in registers computes from it
+// is not kept for the next pass, which would take more registers than the row.
+template <typename T>
+__device__ __forceinline__ T fresh(T v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
-// The part sums of w(i, x) over the row.
-template <int TYPE, typename F>
-__device__ __forceinline__ void sum_parts(const SampleArgs& A, const typename Score<TYPE>::T* row,
-                                          RowShared& S, F&& w) {
-  const uint32_t lane = threadIdx.x % kWave;
-  for (uint64_t a = (uint64_t)(threadIdx.x / kWave) * A.part; a < A.n;
-       a += (uint64_t)(kDrawThreads / kWave) * A.part) {
-    uint64_t sum = 0;
-    for (uint32_t i = (uint32_t)a + 4u * lane; i < A.n && i - (uint32_t)a < A.part; i += 4u * kWave) {
-      float v[4];
-      load4<TYPE>(row, i, A.n, A.vec != 0, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += w(i + (uint32_t)j, v[j]);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) S.part[a / A.part] = sum;
+// A row's scores, and their weights once the rule is known: in registers as J groups of four to a thread
+// (part k is group k), or (J = 0) read again from memory each time (part k is A.part entries, a wave's).
+template <int TYPE, int NT, int J>
+struct Row {
+  using T = typename Score<TYPE>::T;
+  const SampleArgs& A;
+  const T* row;
+  static constexpr bool kWeights = NT * J <= 2048;  // (more do not fit the registers beside the scores)
+  RowRule R;
+  float x[4 * J + 1];
+  uint32_t q[kWeights ? 4 * J + 1 : 1];
+
+  __device__ Row(const SampleArgs& a, const T* r) : A(a), row(r) {}
+  __device__ uint32_t parts() const {
+    return J > 0 ? (A.n + 3u) / 4u : (A.n + A.part - 1u) / A.part;
   }
-  __syncthreads();
-}
-
-// The entry of part `s` at which the running sum of w first exceeds `target` (a wave; the part
-// holds it).
-template <int TYPE, typename F>
-__device__ __forceinline__ uint32_t find_entry(const SampleArgs& A, const typename Score<TYPE>::T* row,
-                                               uint32_t s, uint64_t before, uint64_t target, F&& w) {
-  const uint32_t lane = threadIdx.x % kWave;
-  const uint32_t a = s * A.part;
-  const uint32_t end = A.n - a < A.part ? A.n : a + A.part;
-  for (uint32_t b = a; b < end; b += 4u * kWave) {
-    float v[4];
-    uint64_t q[4], sum = 0;
-    const uint32_t i = b + 4u * lane;
-    if (i < end) {
-      load4<TYPE>(row, i, A.n, A.vec != 0, v);
-    } else {
-      v[0] = v[1] = v[2] = v[3] = -INFINITY;
-    }
+  // The largest rank.
+  __device__ __forceinline__ uint64_t load() {
+    uint64_t best = 0;
+    auto see = [&](uint32_t i, float v) {
+      const uint64_t k = i < A.n ? rank_of(v, i) : 0;
+      best = k > best ? k : best;
+    };
+    if constexpr (J > 0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      q[j] = i < end ? w(i + (uint32_t)j, v[j]) : 0;
-      sum += q[j];
+      for (int j = 0; j < J; ++j) {
+        const uint32_t i = 4u * ((uint32_t)j * NT + threadIdx.x);
+        float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (i < A.n) load4<TYPE>(row, i, A.n, A.vec != 0, v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[4 * j + c] = v[c];
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) see(4u * ((uint32_t)j * NT + threadIdx.x) + c, x[4 * j + c]);
+    } else {
+      each_score([&](uint32_t i, const float (&v)[4]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) see(i + c, v[c]);
+      });
     }
-    const uint64_t in = before + wave_scan(sum, lane);
-    const uint64_t hit = __ballot(in > target);
-    if (hit != 0) {
-      const int l = __ffsll((unsigned long long)hit) - 1;
-      uint64_t run = in - sum;
+    return best;
+  }
+  // (J = 0) f(i, four scores) from i on
+  template <typename F>
+  __device__ __forceinline__ void each_score(F&& f) {
+    constexpr uint32_t U = 4, step = 4u * NT;
+    uint32_t i = 4u * threadIdx.x;
+    for (; (uint64_t)i + (U - 1) * step < A.n; i += U * step) {
+      float v[U][4];
+#pragma unroll
+      for (uint32_t k = 0; k < U; ++k) load4<TYPE>(row, i + k * step, A.n, A.vec != 0, v[k]);
+#pragma unroll
+      for (uint32_t k = 0; k < U; ++k) f(i + k * step, v[k]);
+    }
+    for (; i < A.n; i += step) {
+      float v[4];
+      load4<TYPE>(row, i, A.n, A.vec != 0, v);
+      f(i, v);
+    }
+  }
+  __device__ __forceinline__ uint32_t weight(float v) const { return v > -INFINITY ? weight_of(v, R) : 0u; }
+  __device__ __forceinline__ void weigh(const RowRule& rule) {
+    R = rule;
+    if constexpr (J > 0 && kWeights) {
+#pragma unroll
+      for (int j = 0; j < 4 * J; ++j) q[j] = weight(x[j]);
+    }
+  }
+  __device__ __forceinline__ uint32_t held(int j) const {
+    if constexpr (kWeights) return fresh(q[j]);
+    else return weight(fresh(x[j]));
+  }
+  // f(i, score, weight) for the entries that weigh anything
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) {
+    if constexpr (J > 0) {
+      const uint32_t i = fresh(4u * threadIdx.x);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if ((uint32_t)j * 4u * NT >= A.n) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t w = held(4 * j + c);
+          if (w != 0) f(i + (uint32_t)(4 * j * NT + c), fresh(x[4 * j + c]), w);
+        }
+      }
+    } else {
+      each_score([&](uint32_t i, const float (&v)[4]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t w = weight(v[c]);
+          if (w != 0) f(i + c, v[c], w);
+        }
+      });
+    }
+  }
+  // The parts' sums of w(i, score, weight).
+  template <typename SH, typename F>
+  __device__ __forceinline__ void sum_parts(SH& S, F&& w) {
+    if constexpr (J > 0) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint32_t k = (uint32_t)j * NT + threadIdx.x;
+        uint64_t sum = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum += w(4u * k + c, fresh(x[4 * j + c]), held(4 * j + c));
+        S.part[k] = sum;
+      }
+    } else {
+      const uint32_t lane = threadIdx.x % kWave;
+      for (uint64_t a = (uint64_t)(threadIdx.x / kWave) * A.part; a < A.n;
+           a += (uint64_t)(NT / kWave) * A.part) {
+        uint64_t sum = 0;
+        for (uint32_t i = (uint32_t)a + 4u * lane; i < A.n && i - (uint32_t)a < A.part; i += 4u * kWave) {
+          float v[4];
+          load4<TYPE>(row, i, A.n, A.vec != 0, v);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) sum += w(i + c, v[c], weight(v[c]));
+        }
+        sum = wave_sum(sum);
+        if (lane == 0) S.part[a / A.part] = sum;
+      }
+    }
+    __syncthreads();
+  }
+  // The entry of part s at which the running sum of w first exceeds `target` (the part holds it): for J = 0
+  // a wave's, else a lane's.
+  template <typename F>
+  __device__ __forceinline__ uint32_t find_entry(uint32_t s, uint64_t before, uint64_t target, F&& w) {
+    if constexpr (J > 0) {
+      float v[4];
+      load4<TYPE>(row, 4u * s, A.n, A.vec != 0, v);
       uint32_t j = 0;
 #pragma unroll
-      for (int c = 0; c < 3; ++c) {
-        run += q[c];
-        if (run <= target) j = (uint32_t)c + 1u;
+      for (uint32_t c = 0; c < 3; ++c) {
+        before += w(4u * s + c, v[c], weight(v[c]));
+        if (before <= target) j = c + 1;
       }
-      return (uint32_t)__shfl((int)(i + j), l, kWave);
-    }
-    before = (uint64_t)__shfl((unsigned long long)in, kWave - 1, kWave);
-  }
-  return end - 1;  // (not reached: the part's sum exceeds the target)
-}
-
-// Among the entries that rank at `from` or above: the score's key that the target-th entry (BY_MASS:
-// the entry at which the sum of weights by rank reaches the target) has, eight bits at a time;
-// *above receives the count (sum) that ranks before that key, *at the entries of that key.
-template <int TYPE, bool BY_MASS>
-__device__ uint32_t select_key(const SampleArgs& A, const typename Score<TYPE>::T* row, const RowRule& R,
-                               RowShared& S, uint64_t from, double target, uint64_t* above) {
-  uint32_t prefix = 0;
-  uint64_t before = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (uint32_t i = threadIdx.x; i < 256u; i += kDrawThreads) {
-      S.count[i] = 0;
-      S.mass[i] = 0;
-    }
-    __syncthreads();
-    each<TYPE>(A, row, [&](uint32_t i, float x) {
-      const uint32_t key = key_of(x);
-      if (shift < 24 && (key >> (shift + 8)) != (prefix >> (shift + 8))) return;
-      if (!(x > -INFINITY) || rank_of(x, i) < from) return;
-      const uint32_t q = weight_of(x, R);
-      if (q == 0) return;
-      const uint32_t d = (key >> shift) & 255u;
-      if (BY_MASS) atomicAdd((unsigned long long*)&S.mass[d], (unsigned long long)q);
-      else atomicAdd(&S.count[d], 1u);
-    });
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t d = 255;
-      uint64_t sum = before;
-      for (;; --d) {
-        const uint64_t here = BY_MASS ? S.mass[d] : (uint64_t)S.count[d];
-        if ((double)(sum + here) >= target || d == 0) break;
-        sum += here;
+      return 4u * s + j;
+    } else {
+      const uint32_t lane = threadIdx.x % kWave;
+      const uint32_t a = s * A.part;
+      const uint32_t end = A.n - a < A.part ? A.n : a + A.part;
+      for (uint32_t b = a; b < end; b += 4u * kWave) {
+        float v[4];
+        uint64_t p[4], sum = 0;
+        const uint32_t i = b + 4u * lane;
+        if (i < end) {
+          load4<TYPE>(row, i, A.n, A.vec != 0, v);
+        } else {
+          v[0] = v[1] = v[2] = v[3] = -INFINITY;
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+          p[c] = i < end ? w(i + c, v[c], weight(v[c])) : 0;
+          sum += p[c];
+        }
+        const uint64_t in = before + wave_scan(sum, lane);
+        const uint64_t hit = __ballot(in > target);
+        if (hit != 0) {
+          const int l = __ffsll((unsigned long long)hit) - 1;
+          uint64_t run = in - sum;
+          uint32_t j = 0;
+#pragma unroll
+          for (uint32_t c = 0; c < 3; ++c) {
+            run += p[c];
+            if (run <= target) j = c + 1;
+          }
+          return (uint32_t)__shfl((int)(i + j), l, kWave);
+        }
+        before = (uint64_t)__shfl((unsigned long long)in, kWave - 1, kWave);
       }
-      S.out[0] = d;
-      S.out[1] = sum;
+      return end - 1;  // (not reached: the part's sum exceeds the target)
     }
-    __syncthreads();
-    prefix |= (uint32_t)S.out[0] << shift;
-    before = S.out[1];
-    __syncthreads();
   }
-  *above = before;
-  return prefix;
-}
+};
 
-// The rank of the m-th entry (from 1, by index) with this key.
-template <int TYPE>
-__device__ uint64_t rank_of_tie(const SampleArgs& A, const typename Score<TYPE>::T* row, RowShared& S,
-                                uint32_t parts, uint32_t key, uint64_t m) {
-  auto is = [&](uint32_t i, float x) { return (uint64_t)(i < A.n && key_of(x) == key ? 1 : 0); };
-  sum_parts<TYPE>(A, row, S, is);
-  scan_parts(S, parts);
-  const uint32_t s = find_part(S, parts, m - 1);
-  const uint32_t i = find_entry<TYPE>(A, row, s, s ? S.part[s - 1] : 0, m - 1, is);
+// The entries that weigh anything, in bins of falling score: entries and weights of each bin, as running sums.
+// BIN(x): a bin below kBins or one past them, rising as x falls.
+template <int NT, typename ROW, typename SH, typename BIN>
+__device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
+  for (uint32_t i = threadIdx.x; i < SH::kBins; i += NT) {
+    S.count[i] = 0;
+    S.mass[i] = 0;
+  }
   __syncthreads();
-  return (uint64_t)key << 32 | (uint32_t)~i;
+  row.each([&](uint32_t i, float x, uint32_t q) {
+    const uint32_t b = bin(i, x);
+    if (b >= (uint32_t)SH::kBins) return;
+    atomicAdd(&S.count[b], 1u);
+    atomicAdd((unsigned long long*)&S.mass[b], (unsigned long long)q);
+  });
+  __syncthreads();
+  const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave, b = 2u * threadIdx.x;
+  uint64_t m[2] = {S.mass[b], S.mass[b + 1]};
+  const uint32_t c0 = S.count[b], c1 = S.count[b + 1];
+  uint32_t c = c0 + c1;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t w = (uint32_t)__shfl_up((int)c, o, kWave);
+    if (lane >= (uint32_t)o) c += w;
+  }
+  if (lane == kWave - 1) S.wcount[wv] = c;
+  block_scan<NT, 2>(m, S);  // (its barriers cover wcount)
+#pragma unroll
+  for (uint32_t i = 0; i < NT / kWave; ++i) c += i < wv ? S.wcount[i] : 0u;
+  S.mass[b] = m[0];
+  S.mass[b + 1] = m[1];
+  S.count[b] = c - c1;
+  S.count[b + 1] = c;
+  __syncthreads();
 }
 
-// A workgroup for a row (blockIdx.x), and for a share of its draws (blockIdx.y).
-template <int TYPE>
-__global__ void __launch_bounds__(kDrawThreads) k_sample_row(SampleArgs A) {
-  using T = typename Score<TYPE>::T;
-  __shared__ RowShared S;
-  const uint32_t lane = threadIdx.x % kWave;
-  const int64_t r = blockIdx.x;
-  const T* row = static_cast<const T*>(A.x) + r * A.stride;
-  const uint32_t parts = (A.n + A.part - 1) / A.part;
-  uint64_t best = 0;
-  each<TYPE>(A, row, [&](uint32_t i, float x) {
-    const uint64_t k = i < A.n ? rank_of(x, i) : 0;
-    best = k > best ? k : best;
+// The bin in which the running count (mass) reaches `target`, or the last one.
+template <bool BY_MASS, int NT, typename SH>
+__device__ __forceinline__ uint32_t reach_bin(SH& S, double target) {
+  if (threadIdx.x == 0) S.bin = SH::kBins - 1;
+  __syncthreads();
+  auto run = [&](uint32_t b) { return BY_MASS ? (double)S.mass[b] : (double)S.count[b]; };
+#pragma unroll
+  for (uint32_t j = 0; j < 2; ++j) {
+    const uint32_t b = 2u * threadIdx.x + j;
+    if (run(b) >= target && (b == 0 || !(run(b - 1) >= target))) S.bin = b;
+  }
+  __syncthreads();
+  const uint32_t b = S.bin;
+  __syncthreads();
+  return b;
+}
+
+// The rank at which the entries ranking at `from` or above reach `target` by count (by weight), counted by
+// falling rank; *below receives the weight at and before it. The bins are filled by `first`; a bin of
+// many entries is divided again, evenly over its scores' bits, until few are left or all are equal.
+template <bool BY_MASS, int NT, int PARTS, typename ROW, typename SH, typename BIN>
+__device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double target, BIN&& first, uint64_t* below) {
+  uint32_t b = reach_bin<BY_MASS, NT>(S, target);
+  uint64_t count = b ? S.count[b - 1] : 0, mass = b ? S.mass[b - 1] : 0;  // before the bin
+  uint32_t inside = S.count[b] - (uint32_t)count;
+  uint32_t lo = 0, hi = 0xFFFFFFFFu, level = 0;  // keys of the bin, from the second level on
+  auto in_bin = [&](uint32_t i, float x) {
+    if (rank_of(x, i) < from) return false;
+    const uint32_t k = key_of(x);
+    return level == 0 ? first(i, x) == b : k >= lo && k <= hi;
+  };
+  while (inside > kFew) {
+    // the bin's least and largest keys
+    if (threadIdx.x == 0) {
+      S.lo = 0xFFFFFFFFu;
+      S.hi = 0;
+    }
+    __syncthreads();
+    uint32_t l = 0xFFFFFFFFu, h = 0;
+    row.each([&](uint32_t i, float x, uint32_t) {
+      if (!in_bin(i, x)) return;
+      const uint32_t k = key_of(x);
+      l = k < l ? k : l;
+      h = k > h ? k : h;
+    });
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      const uint32_t a = (uint32_t)__shfl_xor((int)l, o, kWave), c = (uint32_t)__shfl_xor((int)h, o, kWave);
+      l = a < l ? a : l;
+      h = c > h ? c : h;
+    }
+    if (threadIdx.x % kWave == 0 && l <= h) {
+      atomicMin(&S.lo, l);
+      atomicMax(&S.hi, h);
+    }
+    __syncthreads();
+    lo = S.lo;
+    hi = S.hi;
+    level = 1;
+    __syncthreads();
+    if (lo >= hi) {  // equal scores: the first of them by index
+      const uint32_t q = row.weight(key_score(hi));
+      const uint64_t m = BY_MASS ? ties_of(target, mass, q) : (uint64_t)target - count;
+      auto is = [&](uint32_t i, float x, uint32_t) {
+        return (uint64_t)(i < row.A.n && key_of(x) == hi ? 1 : 0);
+      };
+      row.sum_parts(S, is);
+      scan_parts<NT, PARTS>(S, row.parts());
+      const uint32_t s = find_part(S, row.parts(), m - 1);
+      const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, m - 1, is);
+      __syncthreads();
+      *below = mass + m * q;
+      return (uint64_t)hi << 32 | (uint32_t)~i;
+    }
+    const uint32_t at = lo, width = hi - lo + 1u;  // (0: all 2^32)
+    auto bin = [&](uint32_t i, float x) {
+      const uint32_t k = key_of(x);
+      if (k < lo || k > hi || rank_of(x, i) < from) return (uint32_t)SH::kBins;
+      return SH::kBins - 1u - (uint32_t)((uint64_t)(k - at) * SH::kBins / (width ? width : 1ull << 32));
+    };
+    bin_row<NT>(row, S, bin);
+    b = reach_bin<BY_MASS, NT>(S, BY_MASS ? target - (double)mass : target - (double)count);
+    inside = S.count[b] - (b ? S.count[b - 1] : 0u);
+    if (b) {
+      count += S.count[b - 1];
+      mass += S.mass[b - 1];
+    }
+    // the keys of that bin
+    const uint64_t w = width ? width : 1ull << 32, j = SH::kBins - 1u - b;
+    lo = at + (uint32_t)((j * w + SH::kBins - 1) / SH::kBins);
+    hi = at + (uint32_t)(((j + 1) * w + SH::kBins - 1) / SH::kBins - 1);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) S.n = 0;
+  __syncthreads();
+  row.each([&](uint32_t i, float x, uint32_t q) {
+    if (!in_bin(i, x)) return;
+    const uint32_t at = atomicAdd(&S.n, 1u);
+    if (at < kFew) {
+      S.cand[at] = rank_of(x, i);
+      S.cq[at] = q;
+    }
   });
-  best = block_max(best, S);
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+    const uint32_t n = S.n < kFew ? S.n : kFew;
+    const uint64_t mine = threadIdx.x < n ? S.cand[threadIdx.x] : 0;
+    const uint32_t q = threadIdx.x < n ? S.cq[threadIdx.x] : 0;
+    uint64_t before = mass, rank = count;
+    for (uint32_t j = 0; j < n; ++j) {
+      const bool a = S.cand[j] > mine;
+      before += a ? S.cq[j] : 0u;
+      rank += a ? 1u : 0u;
+    }
+    const bool hit = threadIdx.x < n && (BY_MASS ? (double)before < target && (double)(before + q) >= target
+                                                 : (double)(rank + 1) == target);
+    if (hit) {
+      S.cut = mine;
+      S.below = before + q;
+    }
+  }
+  __syncthreads();
+  *below = S.below;
+  const uint64_t cut = S.cut;
+  __syncthreads();
+  return cut;
+}
+
+// A workgroup for a row (blockIdx.x), and for a share of its draws (blockIdx.y). Memory: the row once
+// (J > 0); else three times, and once more for each refinement of a crowded bin.
+template <int TYPE, int NT, int J>
+__global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
+  using T = typename Score<TYPE>::T;
+  constexpr int PARTS = J > 0 ? J * NT : (int)kDrawSegs;
+  __shared__ RowShared<NT, PARTS> S;
+  constexpr int kBins = 2 * NT;
+  const uint32_t lane = threadIdx.x % kWave;
+  const int64_t r = blockIdx.x, d0 = r * A.draws;
+  Row<TYPE, NT, J> row(A, static_cast<const T*>(A.x) + r * A.stride);
+  const uint64_t best = block_max<decltype(S), NT>(row.load(), S);
   const RowRule R = row_rule(A, r, best);
-  const int64_t d0 = r * A.draws;
   if (!(R.m > -INFINITY) || R.greedy) {
     const bool none = !(R.m > -INFINITY);
-    for (int64_t d = (int64_t)blockIdx.y * kDrawThreads + threadIdx.x; d < A.draws;
-         d += (int64_t)gridDim.y * kDrawThreads) {
+    for (int64_t d = (int64_t)blockIdx.y * NT + threadIdx.x; d < A.draws; d += (int64_t)gridDim.y * NT) {
       A.index[d0 + d] = none ? -1 : (int32_t)R.first;
       if (A.logp) A.logp[d0 + d] = none ? -INFINITY : 0.0f;
     }
     return;
   }
+  row.weigh(R);
   uint64_t from = 0;  // the least rank that is left
-  if (R.k > 0) {
-    uint64_t above;
-    const uint32_t key = select_key<TYPE, false>(A, row, R, S, 0, (double)R.k, &above);
-    // (fewer than k entries weigh anything: the last digits are 0, and all of them stay)
-    if (key != 0) from = rank_of_tie<TYPE>(A, row, S, parts, key, R.k - above);
+  if (R.k > 0 || R.p < 1.0) {
+    // even bins of the exponent: weights fall to 0 at 31 ln 2 = 21.5
+    constexpr float kPer = (float)kBins / 21.5f;
+    auto bin = [&](uint32_t, float x) {
+      const uint32_t b = (uint32_t)((R.m - x) * R.inv * kPer);
+      return b < (uint32_t)kBins ? b : (uint32_t)kBins - 1u;
+    };
+    bin_row<NT>(row, S, bin);
+    uint64_t total = S.mass[kBins - 1];
+    if (R.k > 0 && S.count[kBins - 1] > R.k)
+      from = reach<false, NT, PARTS>(row, S, 0, (double)R.k, bin, &total);
+    if (R.p < 1.0) {
+      if (from != 0)
+        bin_row<NT>(row, S, [&](uint32_t i, float x) {
+          return rank_of(x, i) < from ? (uint32_t)kBins : bin(i, x);
+        });
+      uint64_t below;
+      from = reach<true, NT, PARTS>(row, S, from, fmax(R.p * (double)total, 1.0), bin, &below);
+    }
   }
-  auto kept = [&](uint32_t i, float x) {
-    if (!(x > -INFINITY) || rank_of(x, i) < from) return (uint64_t)0;
-    const uint32_t q = weight_of(x, R);
-    return (uint64_t)(q >= R.least ? q : 0);
+  auto kept = [&](uint32_t i, float x, uint32_t q) {
+    return (uint64_t)(q >= R.least && (from == 0 || rank_of(x, i) >= from) ? q : 0u);
   };
-  if (R.p < 1.0) {
-    const uint32_t least = R.least;
-    sum_parts<TYPE>(A, row, S, [&](uint32_t i, float x) {
-      return x > -INFINITY && rank_of(x, i) >= from ? (uint64_t)weight_of(x, R) : (uint64_t)0;
-    });
-    const uint64_t total = scan_parts(S, parts);
-    const double target = fmax(R.p * (double)total, 1.0);
-    uint64_t above;
-    const uint32_t key = select_key<TYPE, true>(A, row, R, S, from, target, &above);
-    const uint64_t cut =
-        rank_of_tie<TYPE>(A, row, S, parts, key, ties_of(target, above, weight_of(key_score(key), R)));
-    from = cut > from ? cut : from;
-    (void)least;
-  }
-  sum_parts<TYPE>(A, row, S, kept);
-  const uint64_t total = scan_parts(S, parts);
-  const int64_t waves = (int64_t)gridDim.y * (kDrawThreads / kWave);
-  for (int64_t d = (int64_t)blockIdx.y * (kDrawThreads / kWave) + threadIdx.x / kWave; d < A.draws;
-       d += waves) {
-    const uint64_t target = target_of(A.u[d0 + d], total);
-    const uint32_t s = find_part(S, parts, target);
-    const uint32_t i = find_entry<TYPE>(A, row, s, s ? S.part[s - 1] : 0, target, kept);
-    if (lane == 0) {
+  row.sum_parts(S, kept);
+  const uint32_t parts = row.parts();
+  const uint64_t total = scan_parts<NT, PARTS>(S, parts);
+  if constexpr (J > 0) {
+    for (int64_t d = (int64_t)blockIdx.y * NT + threadIdx.x; d < A.draws; d += (int64_t)gridDim.y * NT) {
+      const uint64_t target = target_of(A.u[d0 + d], total);
+      const uint32_t s = find_part(S, parts, target);
+      const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, target, kept);
       A.index[d0 + d] = (int32_t)i;
-      if (A.logp) A.logp[d0 + d] = logp_of(clean(Score<TYPE>::get(row[i])), R, total);
+      if (A.logp) A.logp[d0 + d] = logp_of(clean(Score<TYPE>::get(row.row[i])), R, total);
+    }
+  } else {
+    const int64_t waves = (int64_t)gridDim.y * (NT / kWave);
+    for (int64_t d = (int64_t)blockIdx.y * (NT / kWave) + threadIdx.x / kWave; d < A.draws; d += waves) {
+      const uint64_t target = target_of(A.u[d0 + d], total);
+      const uint32_t s = find_part(S, parts, target);
+      const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, target, kept);
+      if (lane == 0) {
+        A.index[d0 + d] = (int32_t)i;
+        if (A.logp) A.logp[d0 + d] = logp_of(clean(Score<TYPE>::get(row.row[i])), R, total);
+      }
     }
   }
 }
@@ -455,11 +771,30 @@ __global__ void __launch_bounds__(256) k_loss_row(LossArgs A) {
   }
 }
 
+template <int TYPE, int G>
+void launch_short(const SampleArgs& A, hipStream_t s) {
+  const int64_t b = (A.rows + 256 / G - 1) / (256 / G);
+  hipLaunchKernelGGL((k_sample_short<TYPE, G>), dim3((uint32_t)(b < 65536 ? b : 65536)), dim3(256), 0, s, A);
+}
+template <int TYPE, int NT, int J>
+void launch_row(const SampleArgs& A, hipStream_t s) {
+  // (every workgroup of a row finds its limits anew: shares of several draws for each thread, or wave)
+  const int64_t per = J > 0 ? 8 * NT : 4 * NT, y = (A.draws + per - 1) / per;
+  hipLaunchKernelGGL((k_sample_row<TYPE, NT, J>), dim3((uint32_t)A.rows, (uint32_t)(y < 256 ? y : 256)), dim3(NT),
+                     0, s, A);
+}
 template <int TYPE>
 void launch_sample(const SampleArgs& A, hipStream_t s) {
-  const int64_t per = 4096;
-  const uint32_t y = (uint32_t)((A.draws + per - 1) / per < 64 ? (A.draws + per - 1) / per : 64);
-  hipLaunchKernelGGL(k_sample_row<TYPE>, dim3((uint32_t)A.rows, y), dim3(kDrawThreads), 0, s, A);
+  if (A.n <= 8) launch_short<TYPE, 8>(A, s);
+  else if (A.n <= 16) launch_short<TYPE, 16>(A, s);
+  else if (A.n <= 32) launch_short<TYPE, 32>(A, s);
+  else if (A.n <= 64) launch_short<TYPE, 64>(A, s);
+  else if (A.n <= 1024) launch_row<TYPE, 256, 1>(A, s);
+  else if (A.n <= 4096) launch_row<TYPE, 256, 4>(A, s);
+  else if (A.n <= 8192) launch_row<TYPE, 256, 8>(A, s);
+  else if (A.n <= 16384) launch_row<TYPE, 1024, 4>(A, s);
+  else if (A.n <= 32768) launch_row<TYPE, 1024, 8>(A, s);
+  else launch_row<TYPE, 1024, 0>(A, s);
 }
 template <int TYPE>
 void launch_loss(const LossArgs& A, hipStream_t s) {
