@@ -211,7 +211,8 @@ __global__ void __launch_bounds__(256) k_sample_short(SampleArgs A) {
 
 // ----------------------------------------------------------------------------- a workgroup for a row
 
-constexpr uint32_t kFew = 64;  // entries that a wave ranks among themselves
+constexpr uint32_t kFew = 64;     // entries that a wave ranks among themselves
+constexpr uint32_t kList = 2048;  // entries of a row that a list holds
 
 // A workgroup's memory: NT threads, bins of scores, and the row's parts.
 template <int NT, int PARTS>
@@ -222,13 +223,14 @@ struct RowShared {
   uint32_t count[kBins];
   uint64_t wave[NT / kWave];
   uint32_t wcount[NT / kWave];
+  uint64_t list[kList];       // ranks
   uint64_t cand[kFew];
   uint32_t cq[kFew];
-  uint32_t n, bin, lo, hi;
+  uint32_t n, listed, bin, lo, hi;
   uint64_t cut, below;
 };
 
-template <typename SH, int NT>
+template <int NT, typename SH>
 __device__ __forceinline__ uint64_t block_max(uint64_t v, SH& S) {
   v = wave_max(v);
   if (threadIdx.x % kWave == 0) S.wave[threadIdx.x / kWave] = v;
@@ -236,6 +238,18 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v, SH& S) {
   uint64_t b = 0;
 #pragma unroll
   for (int i = 0; i < NT / kWave; ++i) b = S.wave[i] > b ? S.wave[i] : b;
+  __syncthreads();
+  return b;
+}
+template <int NT, typename SH>
+__device__ __forceinline__ float block_max(float v, SH& S) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
+  if (threadIdx.x % kWave == 0) S.wcount[threadIdx.x / kWave] = __float_as_uint(v);
+  __syncthreads();
+  float b = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NT / kWave; ++i) b = fmaxf(b, __uint_as_float(S.wcount[i]));
   __syncthreads();
   return b;
 }
@@ -318,13 +332,9 @@ struct Row {
   __device__ uint32_t parts() const {
     return J > 0 ? (A.n + 3u) / 4u : (A.n + A.part - 1u) / A.part;
   }
-  // The largest rank.
-  __device__ __forceinline__ uint64_t load() {
-    uint64_t best = 0;
-    auto see = [&](uint32_t i, float v) {
-      const uint64_t k = i < A.n ? rank_of(v, i) : 0;
-      best = k > best ? k : best;
-    };
+  // The maximum.
+  __device__ __forceinline__ float load() {
+    float best = -INFINITY;
     if constexpr (J > 0) {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
@@ -335,16 +345,45 @@ struct Row {
         for (int c = 0; c < 4; ++c) x[4 * j + c] = v[c];
       }
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) see(4u * ((uint32_t)j * NT + threadIdx.x) + c, x[4 * j + c]);
+      for (int j = 0; j < 4 * J; ++j) best = fmaxf(best, x[j]);
     } else {
-      each_score([&](uint32_t i, const float (&v)[4]) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) see(i + c, v[c]);
+      each_score([&](uint32_t, const float (&v)[4]) {
+        best = fmaxf(fmaxf(best, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
       });
     }
     return best;
+  }
+  // The largest rank.
+  __device__ __forceinline__ uint64_t first_best() {
+    uint64_t best = 0;
+    each_above(-INFINITY, [&](uint32_t i, float v) {
+      const uint64_t k = rank_of(v, i);
+      best = k > best ? k : best;
+    });
+    return best;
+  }
+  // f(i, score) for the entries of at least `least` (and above -inf).
+  template <typename F>
+  __device__ __forceinline__ void each_above(float least, F&& f) {
+    if constexpr (J > 0) {
+      const uint32_t i = fresh(4u * threadIdx.x);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if ((uint32_t)j * 4u * NT >= A.n) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float v = fresh(x[4 * j + c]);
+          if (v >= least && v > -INFINITY) f(i + (uint32_t)(4 * j * NT + c), v);
+        }
+      }
+    } else {
+      each_score([&](uint32_t i, const float (&v)[4]) {
+        if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= least)) return;
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c)
+          if (v[c] >= least && v[c] > -INFINITY) f(i + c, v[c]);
+      });
+    }
   }
   // (J = 0) f(i, four scores) from i on
   template <typename F>
@@ -393,23 +432,26 @@ struct Row {
     } else {
       each_score([&](uint32_t i, const float (&v)[4]) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (uint32_t c = 0; c < 4; ++c) {
           const uint32_t w = weight(v[c]);
           if (w != 0) f(i + c, v[c], w);
         }
       });
     }
   }
-  // The parts' sums of w(i, score, weight).
+  // The parts' sums of w(i, score), which is 0 below the score `least`.
   template <typename SH, typename F>
-  __device__ __forceinline__ void sum_parts(SH& S, F&& w) {
+  __device__ __forceinline__ void sum_parts(SH& S, float least, F&& w) {
     if constexpr (J > 0) {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const uint32_t k = (uint32_t)j * NT + threadIdx.x;
         uint64_t sum = 0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) sum += w(4u * k + c, fresh(x[4 * j + c]), held(4 * j + c));
+        for (int c = 0; c < 4; ++c) {
+          const float v = fresh(x[4 * j + c]);
+          if (v >= least) sum += w(4u * k + c, v);
+        }
         S.part[k] = sum;
       }
     } else {
@@ -420,10 +462,12 @@ struct Row {
         for (uint32_t i = (uint32_t)a + 4u * lane; i < A.n && i - (uint32_t)a < A.part; i += 4u * kWave) {
           float v[4];
           load4<TYPE>(row, i, A.n, A.vec != 0, v);
+          if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= least)) continue;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) sum += w(i + c, v[c], weight(v[c]));
+          for (uint32_t c = 0; c < 4; ++c)
+            if (v[c] >= least) sum += w(i + c, v[c]);
         }
-        sum = wave_sum(sum);
+        if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
         if (lane == 0) S.part[a / A.part] = sum;
       }
     }
@@ -439,7 +483,7 @@ struct Row {
       uint32_t j = 0;
 #pragma unroll
       for (uint32_t c = 0; c < 3; ++c) {
-        before += w(4u * s + c, v[c], weight(v[c]));
+        before += w(4u * s + c, v[c]);
         if (before <= target) j = c + 1;
       }
       return 4u * s + j;
@@ -458,7 +502,7 @@ struct Row {
         }
 #pragma unroll
         for (uint32_t c = 0; c < 4; ++c) {
-          p[c] = i < end ? w(i + c, v[c], weight(v[c])) : 0;
+          p[c] = i < end ? w(i + c, v[c]) : 0;
           sum += p[c];
         }
         const uint64_t in = before + wave_scan(sum, lane);
@@ -481,24 +525,55 @@ struct Row {
   }
 };
 
-// The entries that weigh anything, in bins of falling score: entries and weights of each bin, as running sums.
-// BIN(x): a bin below kBins or one past them, rising as x falls.
-template <int NT, typename ROW, typename SH, typename BIN>
+// Entries of a row in a list: what is left after most of the row is known to be cut.
+template <int NT, typename SH>
+struct List {
+  SH& S;
+  const RowRule& R;
+  __device__ __forceinline__ uint32_t weight(float v) const { return v > -INFINITY ? weight_of(v, R) : 0u; }
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) {
+    for (uint32_t k = threadIdx.x; k < S.listed; k += NT) {
+      const uint64_t r = S.list[k];
+      const float x = key_score((uint32_t)(r >> 32));
+      const uint32_t q = weight(x);
+      if (q != 0) f(~(uint32_t)r, x, q);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each_above(float least, F&& f) {
+    for (uint32_t k = threadIdx.x; k < S.listed; k += NT) {
+      const uint64_t r = S.list[k];
+      const float x = key_score((uint32_t)(r >> 32));
+      if (x >= least) f(~(uint32_t)r, x);
+    }
+  }
+};
+
+// The entries that weigh anything, in bins of falling score: entries and weights of each bin, as running sums
+// (MASS false: entries above -inf, and no weights). BIN(i, x): a bin, or kBins for none, rising as x falls.
+template <bool MASS, int NT, typename ROW, typename SH, typename BIN>
 __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
   for (uint32_t i = threadIdx.x; i < SH::kBins; i += NT) {
     S.count[i] = 0;
     S.mass[i] = 0;
   }
   __syncthreads();
-  row.each([&](uint32_t i, float x, uint32_t q) {
-    const uint32_t b = bin(i, x);
-    if (b >= (uint32_t)SH::kBins) return;
-    atomicAdd(&S.count[b], 1u);
-    atomicAdd((unsigned long long*)&S.mass[b], (unsigned long long)q);
-  });
+  if constexpr (MASS) {
+    row.each([&](uint32_t i, float x, uint32_t q) {
+      const uint32_t b = bin(i, x);
+      if (b >= (uint32_t)SH::kBins) return;
+      atomicAdd(&S.count[b], 1u);
+      atomicAdd((unsigned long long*)&S.mass[b], (unsigned long long)q);
+    });
+  } else {
+    row.each_above(-INFINITY, [&](uint32_t i, float x) {
+      const uint32_t b = bin(i, x);
+      if (b < (uint32_t)SH::kBins) atomicAdd(&S.count[b], 1u);
+    });
+  }
   __syncthreads();
   const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave, b = 2u * threadIdx.x;
-  uint64_t m[2] = {S.mass[b], S.mass[b + 1]};
   const uint32_t c0 = S.count[b], c1 = S.count[b + 1];
   uint32_t c = c0 + c1;
 #pragma unroll
@@ -507,11 +582,15 @@ __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
     if (lane >= (uint32_t)o) c += w;
   }
   if (lane == kWave - 1) S.wcount[wv] = c;
-  block_scan<NT, 2>(m, S);  // (its barriers cover wcount)
+  if constexpr (MASS) {
+    uint64_t m[2] = {S.mass[b], S.mass[b + 1]};
+    block_scan<NT, 2>(m, S);
+    S.mass[b] = m[0];
+    S.mass[b + 1] = m[1];
+  }
+  __syncthreads();
 #pragma unroll
   for (uint32_t i = 0; i < NT / kWave; ++i) c += i < wv ? S.wcount[i] : 0u;
-  S.mass[b] = m[0];
-  S.mass[b + 1] = m[1];
   S.count[b] = c - c1;
   S.count[b + 1] = c;
   __syncthreads();
@@ -535,18 +614,25 @@ __device__ __forceinline__ uint32_t reach_bin(SH& S, double target) {
 }
 
 // The rank at which the entries ranking at `from` or above reach `target` by count (by weight), counted by
-// falling rank; *below receives the weight at and before it. The bins are filled by `first`; a bin of
-// many entries is divided again, evenly over its scores' bits, until few are left or all are equal.
-template <bool BY_MASS, int NT, int PARTS, typename ROW, typename SH, typename BIN>
-__device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double target, BIN&& first, uint64_t* below) {
+// falling rank; *below receives the weight at and before it (by count: not meant without weights in the
+// bins). The bins are filled by `first`; a bin of many entries is divided again, evenly over its scores'
+// bits, until few are left or all are equal. `some`: the row, or a list that holds every entry ranking
+// as high; `row`: the row.
+template <bool BY_MASS, bool MASS, int NT, int PARTS, typename SOME, typename ROW, typename SH, typename BIN>
+__device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t from, double target, BIN&& first,
+                                          uint64_t* below) {
   uint32_t b = reach_bin<BY_MASS, NT>(S, target);
-  uint64_t count = b ? S.count[b - 1] : 0, mass = b ? S.mass[b - 1] : 0;  // before the bin
+  uint64_t count = b ? S.count[b - 1] : 0, mass = MASS && b ? S.mass[b - 1] : 0;  // before the bin
   uint32_t inside = S.count[b] - (uint32_t)count;
   uint32_t lo = 0, hi = 0xFFFFFFFFu, level = 0;  // keys of the bin, from the second level on
   auto in_bin = [&](uint32_t i, float x) {
-    if (rank_of(x, i) < from) return false;
-    const uint32_t k = key_of(x);
-    return level == 0 ? first(i, x) == b : k >= lo && k <= hi;
+    if (level == 0) {
+      if (first(i, x) != b) return false;
+    } else {
+      const uint32_t k = key_of(x);
+      if (k < lo || k > hi) return false;
+    }
+    return rank_of(x, i) >= from && (!MASS || some.weight(x) != 0);
   };
   while (inside > kFew) {
     // the bin's least and largest keys
@@ -556,7 +642,7 @@ __device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double
     }
     __syncthreads();
     uint32_t l = 0xFFFFFFFFu, h = 0;
-    row.each([&](uint32_t i, float x, uint32_t) {
+    some.each_above(-INFINITY, [&](uint32_t i, float x) {
       if (!in_bin(i, x)) return;
       const uint32_t k = key_of(x);
       l = k < l ? k : l;
@@ -578,12 +664,11 @@ __device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double
     level = 1;
     __syncthreads();
     if (lo >= hi) {  // equal scores: the first of them by index
-      const uint32_t q = row.weight(key_score(hi));
+      const float same = key_score(hi);
+      const uint32_t q = some.weight(same);
       const uint64_t m = BY_MASS ? ties_of(target, mass, q) : (uint64_t)target - count;
-      auto is = [&](uint32_t i, float x, uint32_t) {
-        return (uint64_t)(i < row.A.n && key_of(x) == hi ? 1 : 0);
-      };
-      row.sum_parts(S, is);
+      auto is = [&](uint32_t i, float x) { return (uint64_t)(i < row.A.n && x == same ? 1 : 0); };
+      row.sum_parts(S, same, is);
       scan_parts<NT, PARTS>(S, row.parts());
       const uint32_t s = find_part(S, row.parts(), m - 1);
       const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, m - 1, is);
@@ -597,12 +682,12 @@ __device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double
       if (k < lo || k > hi || rank_of(x, i) < from) return (uint32_t)SH::kBins;
       return SH::kBins - 1u - (uint32_t)((uint64_t)(k - at) * SH::kBins / (width ? width : 1ull << 32));
     };
-    bin_row<NT>(row, S, bin);
+    bin_row<MASS, NT>(some, S, bin);
     b = reach_bin<BY_MASS, NT>(S, BY_MASS ? target - (double)mass : target - (double)count);
     inside = S.count[b] - (b ? S.count[b - 1] : 0u);
     if (b) {
       count += S.count[b - 1];
-      mass += S.mass[b - 1];
+      if (MASS) mass += S.mass[b - 1];
     }
     // the keys of that bin
     const uint64_t w = width ? width : 1ull << 32, j = SH::kBins - 1u - b;
@@ -612,12 +697,12 @@ __device__ __forceinline__ uint64_t reach(ROW& row, SH& S, uint64_t from, double
   }
   if (threadIdx.x == 0) S.n = 0;
   __syncthreads();
-  row.each([&](uint32_t i, float x, uint32_t q) {
+  some.each_above(-INFINITY, [&](uint32_t i, float x) {
     if (!in_bin(i, x)) return;
     const uint32_t at = atomicAdd(&S.n, 1u);
     if (at < kFew) {
       S.cand[at] = rank_of(x, i);
-      S.cq[at] = q;
+      S.cq[at] = some.weight(x);
     }
   });
   __syncthreads();
@@ -656,10 +741,11 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   const uint32_t lane = threadIdx.x % kWave;
   const int64_t r = blockIdx.x, d0 = r * A.draws;
   Row<TYPE, NT, J> row(A, static_cast<const T*>(A.x) + r * A.stride);
-  const uint64_t best = block_max<decltype(S), NT>(row.load(), S);
-  const RowRule R = row_rule(A, r, best);
-  if (!(R.m > -INFINITY) || R.greedy) {
-    const bool none = !(R.m > -INFINITY);
+  const float m = block_max<NT>(row.load(), S);
+  RowRule R = row_rule(A, r, (uint64_t)key_of(m) << 32);
+  if (!(m > -INFINITY) || R.greedy) {
+    const bool none = !(m > -INFINITY);
+    if (!none) R.first = ~(uint32_t)block_max<NT>(row.first_best(), S);
     for (int64_t d = (int64_t)blockIdx.y * NT + threadIdx.x; d < A.draws; d += (int64_t)gridDim.y * NT) {
       A.index[d0 + d] = none ? -1 : (int32_t)R.first;
       if (A.logp) A.logp[d0 + d] = none ? -INFINITY : 0.0f;
@@ -668,30 +754,55 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   }
   row.weigh(R);
   uint64_t from = 0;  // the least rank that is left
-  if (R.k > 0 || R.p < 1.0) {
-    // even bins of the exponent: weights fall to 0 at 31 ln 2 = 21.5
-    constexpr float kPer = (float)kBins / 21.5f;
-    auto bin = [&](uint32_t, float x) {
-      const uint32_t b = (uint32_t)((R.m - x) * R.inv * kPer);
-      return b < (uint32_t)kBins ? b : (uint32_t)kBins - 1u;
-    };
-    bin_row<NT>(row, S, bin);
-    uint64_t total = S.mass[kBins - 1];
-    if (R.k > 0 && S.count[kBins - 1] > R.k)
-      from = reach<false, NT, PARTS>(row, S, 0, (double)R.k, bin, &total);
-    if (R.p < 1.0) {
-      if (from != 0)
-        bin_row<NT>(row, S, [&](uint32_t i, float x) {
-          return rank_of(x, i) < from ? (uint32_t)kBins : bin(i, x);
+  bool listed = false;
+  // even bins of the exponent: weights fall to 0 at 31 ln 2 = 21.5
+  constexpr float kPer = (float)kBins / 21.5f;
+  auto bin = [&](uint32_t, float x) {
+    const float b = (R.m - x) * R.inv * kPer;
+    return b < (float)kBins ? (uint32_t)b : (uint32_t)kBins - 1u;
+  };
+  List<NT, decltype(S)> list{S, R};
+  if (R.k > 0) {
+    uint64_t below;
+    bin_row<false, NT>(row, S, bin);
+    if (S.count[kBins - 1] > R.k) {
+      // what can be among the k: with few others, all that follows is done on a list of it
+      const uint32_t b = reach_bin<false, NT>(S, (double)R.k);
+      listed = S.count[b] <= kList;
+      if (listed) {
+        if (threadIdx.x == 0) S.listed = 0;
+        __syncthreads();
+        row.each_above(-INFINITY, [&](uint32_t i, float x) {
+          if (bin(i, x) <= b) S.list[atomicAdd(&S.listed, 1u)] = rank_of(x, i);
         });
-      uint64_t below;
-      from = reach<true, NT, PARTS>(row, S, from, fmax(R.p * (double)total, 1.0), bin, &below);
+        __syncthreads();
+        from = reach<false, false, NT, PARTS>(list, row, S, 0, (double)R.k, bin, &below);
+      } else {
+        from = reach<false, false, NT, PARTS>(row, row, S, 0, (double)R.k, bin, &below);
+      }
     }
   }
-  auto kept = [&](uint32_t i, float x, uint32_t q) {
-    return (uint64_t)(q >= R.least && (from == 0 || rank_of(x, i) >= from) ? q : 0u);
+  if (R.p < 1.0) {
+    auto left = [&](uint32_t i, float x) { return rank_of(x, i) < from ? (uint32_t)kBins : bin(i, x); };
+    uint64_t below;
+    if (listed) {
+      bin_row<true, NT>(list, S, left);
+      from = reach<true, true, NT, PARTS>(list, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin,
+                                          &below);
+    } else {
+      bin_row<true, NT>(row, S, left);
+      from = reach<true, true, NT, PARTS>(row, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin,
+                                          &below);
+    }
+  }
+  const float least = from ? key_score((uint32_t)(from >> 32)) : -INFINITY;
+  const uint32_t last = ~(uint32_t)from;  // the last of those equal to it
+  auto kept = [&](uint32_t i, float x) {
+    if (from ? x < least || (x == least && i > last) : !(x > -INFINITY)) return (uint64_t)0;
+    const uint32_t q = weight_of(x, R);
+    return (uint64_t)(q >= R.least ? q : 0u);
   };
-  row.sum_parts(S, kept);
+  row.sum_parts(S, least, kept);
   const uint32_t parts = row.parts();
   const uint64_t total = scan_parts<NT, PARTS>(S, parts);
   if constexpr (J > 0) {
