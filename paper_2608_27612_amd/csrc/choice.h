@@ -13,7 +13,6 @@ namespace emr {
 
 constexpr int kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2;
 
-constexpr int kDrawThreads = 1024;      // a workgroup for a row
 constexpr uint32_t kDrawSegs = 4096;    // parts of a row with a sum each, at most
 constexpr uint32_t kDrawPart = 256;     // a part's entries: a multiple of this
 
@@ -22,7 +21,6 @@ struct SampleArgs {
   int64_t stride, rows;
   uint32_t n;
   int32_t type;
-  int32_t vec;          // every row starts at a multiple of four entries' bytes
   float t, p, min_p;    // for every row, where the pointer below is NULL
   int32_t k;
   const float* row_t;
@@ -40,7 +38,7 @@ struct LossArgs {
   const void* x;        // [rows] rows of n scores, stride entries apart
   int64_t stride, rows;
   uint32_t n;
-  int32_t type, vec;
+  int32_t type;
   float inv_t;
   const int32_t* index;  // [rows]
   const float* scale;    // [rows] or NULL: 1

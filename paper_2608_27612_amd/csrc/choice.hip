@@ -40,13 +40,11 @@ struct Score<kTypeF16> {
   static __device__ __forceinline__ T put(float v) { return (T)v; }
 };
 
-// A score as the draws take it: NaN as -inf, nothing above the largest float, one zero.
-__device__ __forceinline__ float clean(float x) {
-  x = x != x ? -INFINITY : (x > 3.402823466e38f ? 3.402823466e38f : x);
-  return x + 0.0f;
-}
-__device__ __forceinline__ uint32_t key_of(float x) {  // rises with x
-  const uint32_t b = __float_as_uint(x);
+__device__ __forceinline__ float capped(float x) { return x > 3.402823466e38f ? 3.402823466e38f : x; }
+// A score as the draws take it: NaN as -inf, nothing above the largest float.
+__device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : capped(x); }
+__device__ __forceinline__ uint32_t key_of(float x) {  // rises with x; one zero
+  const uint32_t b = __float_as_uint(x + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_score(uint32_t k) {
@@ -78,22 +76,24 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v, uint32_t lane) {  // i
   return v;
 }
 
-// Four entries of a row from i on (a multiple of four): those past the end as -inf.
+// Four entries of a row from i on (a multiple of four, at which the row's memory is aligned to four entries),
+// none above the largest float: those outside lo .. n - 1 as -inf. A NaN stays one: every comparison below
+// leaves it out, as it does -inf.
 template <int TYPE>
-__device__ __forceinline__ void load4(const typename Score<TYPE>::T* row, uint32_t i, uint32_t n,
-                                      bool vec, float (&v)[4]) {
+__device__ __forceinline__ void load4(const typename Score<TYPE>::T* row, uint32_t i, uint32_t lo, uint32_t n,
+                                      float (&v)[4]) {
   using T = typename Score<TYPE>::T;
   struct alignas(4 * sizeof(T)) Four {
     T v[4];
   };
-  if (vec && i + 4u <= n) {
+  if (i >= lo && i + 4u <= n) {
     const Four f = *reinterpret_cast<const Four*>(row + i);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = clean(Score<TYPE>::get(f.v[j]));
+    for (int j = 0; j < 4; ++j) v[j] = capped(Score<TYPE>::get(f.v[j]));
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      v[j] = i + (uint32_t)j < n ? clean(Score<TYPE>::get(row[i + j])) : -INFINITY;
+    for (uint32_t j = 0; j < 4; ++j)
+      v[j] = i + j >= lo && i + j < n ? capped(Score<TYPE>::get(row[i + j])) : -INFINITY;
   }
 }
 
@@ -121,6 +121,7 @@ __device__ __forceinline__ RowRule row_rule(const SampleArgs& A, int64_t r, uint
   R.least = mp > 0.0f ? (uint32_t)ceil((double)fminf(mp, 1.0f) * (double)kOne) : 0u;
   return R;
 }
+// (x: not a NaN)
 __device__ __forceinline__ uint32_t weight_of(float x, const RowRule& R) {
   return (uint32_t)(expf((x - R.m) * R.inv) * kOne);
 }
@@ -308,6 +309,9 @@ __device__ __forceinline__ uint32_t find_part(const SH& S, uint32_t parts, uint6
   return lo;
 }
 
+// Whether an entry weighs anything that counts: 2^-31 of the largest is at an exponent of -31 ln 2 = -21.49.
+__device__ __forceinline__ bool weighs(float x, const RowRule& R) { return (x - R.m) * R.inv > -21.5f; }
+
 // A register's value that the compiler does not follow: what a pass over a row in registers computes from it
 // is not kept for the next pass, which would take more registers than the row.
 template <typename T>
@@ -318,20 +322,24 @@ __device__ __forceinline__ T fresh(T v) {
 
 // A row's scores, and their weights once the rule is known: in registers as J groups of four to a thread
 // (part k is group k), or (J = 0) read again from memory each time (part k is A.part entries, a wave's).
+// Groups lie where memory is aligned: the row's first entry is number `lo` (0 .. 3) here, its last n - 1.
 template <int TYPE, int NT, int J>
 struct Row {
   using T = typename Score<TYPE>::T;
   const SampleArgs& A;
   const T* row;
+  uint32_t lo, n;
   static constexpr bool kWeights = NT * J <= 2048;  // (more do not fit the registers beside the scores)
   RowRule R;
   float x[4 * J + 1];
   uint32_t q[kWeights ? 4 * J + 1 : 1];
 
-  __device__ Row(const SampleArgs& a, const T* r) : A(a), row(r) {}
-  __device__ uint32_t parts() const {
-    return J > 0 ? (A.n + 3u) / 4u : (A.n + A.part - 1u) / A.part;
+  __device__ Row(const SampleArgs& a, const T* r) : A(a) {
+    lo = (uint32_t)((uintptr_t)r / sizeof(T)) % 4u;
+    row = r - lo;
+    n = a.n + lo;
   }
+  __device__ uint32_t parts() const { return J > 0 ? (n + 3u) / 4u : (n + A.part - 1u) / A.part; }
   // The maximum.
   __device__ __forceinline__ float load() {
     float best = -INFINITY;
@@ -340,7 +348,7 @@ struct Row {
       for (int j = 0; j < J; ++j) {
         const uint32_t i = 4u * ((uint32_t)j * NT + threadIdx.x);
         float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (i < A.n) load4<TYPE>(row, i, A.n, A.vec != 0, v);
+        if (i < n) load4<TYPE>(row, i, lo, n, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[4 * j + c] = v[c];
       }
@@ -369,7 +377,7 @@ struct Row {
       const uint32_t i = fresh(4u * threadIdx.x);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        if ((uint32_t)j * 4u * NT >= A.n) break;
+        if ((uint32_t)j * 4u * NT >= n) break;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float v = fresh(x[4 * j + c]);
@@ -390,16 +398,16 @@ struct Row {
   __device__ __forceinline__ void each_score(F&& f) {
     constexpr uint32_t U = 4, step = 4u * NT;
     uint32_t i = 4u * threadIdx.x;
-    for (; (uint64_t)i + (U - 1) * step < A.n; i += U * step) {
+    for (; (uint64_t)i + (U - 1) * step < n; i += U * step) {
       float v[U][4];
 #pragma unroll
-      for (uint32_t k = 0; k < U; ++k) load4<TYPE>(row, i + k * step, A.n, A.vec != 0, v[k]);
+      for (uint32_t k = 0; k < U; ++k) load4<TYPE>(row, i + k * step, lo, n, v[k]);
 #pragma unroll
       for (uint32_t k = 0; k < U; ++k) f(i + k * step, v[k]);
     }
-    for (; i < A.n; i += step) {
+    for (; i < n; i += step) {
       float v[4];
-      load4<TYPE>(row, i, A.n, A.vec != 0, v);
+      load4<TYPE>(row, i, lo, n, v);
       f(i, v);
     }
   }
@@ -411,64 +419,86 @@ struct Row {
       for (int j = 0; j < 4 * J; ++j) q[j] = weight(x[j]);
     }
   }
-  __device__ __forceinline__ uint32_t held(int j) const {
-    if constexpr (kWeights) return fresh(q[j]);
-    else return weight(fresh(x[j]));
-  }
-  // f(i, score, weight) for the entries that weigh anything
+  // f(i, score, weight) for the entries whose exponent is above -21.5
   template <typename F>
   __device__ __forceinline__ void each(F&& f) {
     if constexpr (J > 0) {
       const uint32_t i = fresh(4u * threadIdx.x);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        if ((uint32_t)j * 4u * NT >= A.n) break;
+        if ((uint32_t)j * 4u * NT >= n) break;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const uint32_t w = held(4 * j + c);
-          if (w != 0) f(i + (uint32_t)(4 * j * NT + c), fresh(x[4 * j + c]), w);
+          const float v = fresh(x[4 * j + c]);
+          if (weighs(v, R))
+            f(i + (uint32_t)(4 * j * NT + c), v, kWeights ? fresh(q[kWeights ? 4 * j + c : 0]) : weight_of(v, R));
         }
       }
     } else {
       each_score([&](uint32_t i, const float (&v)[4]) {
 #pragma unroll
-        for (uint32_t c = 0; c < 4; ++c) {
-          const uint32_t w = weight(v[c]);
-          if (w != 0) f(i + c, v[c], w);
-        }
+        for (uint32_t c = 0; c < 4; ++c)
+          if (weighs(v[c], R)) f(i + c, v[c], weight_of(v[c], R));
       });
     }
   }
-  // The parts' sums of w(i, score), which is 0 below the score `least`.
+  // The parts' sums of w(i, score) over the entries of at least the score `least`. Few lanes of a wave hold
+  // such an entry at a time where most of a row is cut, so each takes its next one in turn.
   template <typename SH, typename F>
   __device__ __forceinline__ void sum_parts(SH& S, float least, F&& w) {
+    auto four = [&](uint32_t i, const float (&v)[4]) {
+      uint64_t sum = 0;
+      uint32_t mask = (v[0] >= least ? 1u : 0u) | (v[1] >= least ? 2u : 0u) | (v[2] >= least ? 4u : 0u) |
+                      (v[3] >= least ? 8u : 0u);
+      while (mask != 0) {
+        const uint32_t c = (uint32_t)__builtin_ctz(mask);
+        mask &= mask - 1u;
+        const float a = c & 1u ? v[1] : v[0], b = c & 1u ? v[3] : v[2];
+        sum += w(i + c, c & 2u ? b : a);
+      }
+      return sum;
+    };
     if constexpr (J > 0) {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const uint32_t k = (uint32_t)j * NT + threadIdx.x;
-        uint64_t sum = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float v = fresh(x[4 * j + c]);
-          if (v >= least) sum += w(4u * k + c, v);
-        }
-        S.part[k] = sum;
+        const float v[4] = {fresh(x[4 * j]), fresh(x[4 * j + 1]), fresh(x[4 * j + 2]), fresh(x[4 * j + 3])};
+        S.part[k] = four(4u * k, v);
       }
     } else {
-      const uint32_t lane = threadIdx.x % kWave;
-      for (uint64_t a = (uint64_t)(threadIdx.x / kWave) * A.part; a < A.n;
-           a += (uint64_t)(NT / kWave) * A.part) {
-        uint64_t sum = 0;
-        for (uint32_t i = (uint32_t)a + 4u * lane; i < A.n && i - (uint32_t)a < A.part; i += 4u * kWave) {
-          float v[4];
-          load4<TYPE>(row, i, A.n, A.vec != 0, v);
-          if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= least)) continue;
+      // (a part of 256 entries is one group of four to a lane; four parts' loads in flight)
+      const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, parts_ = parts();
+      constexpr uint32_t U = 4, W = NT / kWave;
+      if (A.part == 4u * kWave) {
+        for (uint32_t p = wave; p < parts_; p += U * W) {
+          float v[U][4];
 #pragma unroll
-          for (uint32_t c = 0; c < 4; ++c)
-            if (v[c] >= least) sum += w(i + c, v[c]);
+          for (uint32_t k = 0; k < U; ++k) {
+            const uint32_t i = (p + k * W) * A.part + 4u * lane;
+            if (p + k * W < parts_ && i < n) {
+              load4<TYPE>(row, i, lo, n, v[k]);
+            } else {
+              v[k][0] = v[k][1] = v[k][2] = v[k][3] = NAN;
+            }
+          }
+#pragma unroll
+          for (uint32_t k = 0; k < U; ++k) {
+            uint64_t sum = four((p + k * W) * A.part + 4u * lane, v[k]);
+            if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
+            if (lane == 0 && p + k * W < parts_) S.part[p + k * W] = sum;
+          }
         }
-        if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
-        if (lane == 0) S.part[a / A.part] = sum;
+      } else {
+        for (uint32_t p = wave; p < parts_; p += W) {
+          uint64_t sum = 0;
+          for (uint32_t b = 4u * lane; b < A.part && (uint64_t)p * A.part + b < n; b += 4u * kWave) {
+            float v[4];
+            load4<TYPE>(row, p * A.part + b, lo, n, v);
+            sum += four(p * A.part + b, v);
+          }
+          if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
+          if (lane == 0) S.part[p] = sum;
+        }
       }
     }
     __syncthreads();
@@ -479,30 +509,30 @@ struct Row {
   __device__ __forceinline__ uint32_t find_entry(uint32_t s, uint64_t before, uint64_t target, F&& w) {
     if constexpr (J > 0) {
       float v[4];
-      load4<TYPE>(row, 4u * s, A.n, A.vec != 0, v);
+      load4<TYPE>(row, 4u * s, lo, n, v);
       uint32_t j = 0;
 #pragma unroll
       for (uint32_t c = 0; c < 3; ++c) {
-        before += w(4u * s + c, v[c]);
+        before += v[c] > -INFINITY ? w(4u * s + c, v[c]) : 0;
         if (before <= target) j = c + 1;
       }
       return 4u * s + j;
     } else {
       const uint32_t lane = threadIdx.x % kWave;
       const uint32_t a = s * A.part;
-      const uint32_t end = A.n - a < A.part ? A.n : a + A.part;
+      const uint32_t end = n - a < A.part ? n : a + A.part;
       for (uint32_t b = a; b < end; b += 4u * kWave) {
         float v[4];
         uint64_t p[4], sum = 0;
         const uint32_t i = b + 4u * lane;
         if (i < end) {
-          load4<TYPE>(row, i, A.n, A.vec != 0, v);
+          load4<TYPE>(row, i, lo, n, v);
         } else {
           v[0] = v[1] = v[2] = v[3] = -INFINITY;
         }
 #pragma unroll
         for (uint32_t c = 0; c < 4; ++c) {
-          p[c] = i < end ? w(i + c, v[c]) : 0;
+          p[c] = i < end && v[c] > -INFINITY ? w(i + c, v[c]) : 0;
           sum += p[c];
         }
         const uint64_t in = before + wave_scan(sum, lane);
@@ -536,8 +566,7 @@ struct List {
     for (uint32_t k = threadIdx.x; k < S.listed; k += NT) {
       const uint64_t r = S.list[k];
       const float x = key_score((uint32_t)(r >> 32));
-      const uint32_t q = weight(x);
-      if (q != 0) f(~(uint32_t)r, x, q);
+      if (weighs(x, R)) f(~(uint32_t)r, x, weight_of(x, R));
     }
   }
   template <typename F>
@@ -550,8 +579,8 @@ struct List {
   }
 };
 
-// The entries that weigh anything, in bins of falling score: entries and weights of each bin, as running sums
-// (MASS false: entries above -inf, and no weights). BIN(i, x): a bin, or kBins for none, rising as x falls.
+// The entries whose exponent is above -21.5, in bins of falling score: entries and weights of each bin, as
+// running sums (MASS false: all entries above -inf, and no weights). BIN(i, x): a bin, or kBins for none, rising as x falls.
 template <bool MASS, int NT, typename ROW, typename SH, typename BIN>
 __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
   for (uint32_t i = threadIdx.x; i < SH::kBins; i += NT) {
@@ -632,7 +661,7 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
       const uint32_t k = key_of(x);
       if (k < lo || k > hi) return false;
     }
-    return rank_of(x, i) >= from && (!MASS || some.weight(x) != 0);
+    return rank_of(x, i) >= from && (!MASS || weighs(x, some.R));
   };
   while (inside > kFew) {
     // the bin's least and largest keys
@@ -667,7 +696,7 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
       const float same = key_score(hi);
       const uint32_t q = some.weight(same);
       const uint64_t m = BY_MASS ? ties_of(target, mass, q) : (uint64_t)target - count;
-      auto is = [&](uint32_t i, float x) { return (uint64_t)(i < row.A.n && x == same ? 1 : 0); };
+      auto is = [&](uint32_t i, float x) { return (uint64_t)(i < row.n && x == same ? 1 : 0); };
       row.sum_parts(S, same, is);
       scan_parts<NT, PARTS>(S, row.parts());
       const uint32_t s = find_part(S, row.parts(), m - 1);
@@ -747,7 +776,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
     const bool none = !(m > -INFINITY);
     if (!none) R.first = ~(uint32_t)block_max<NT>(row.first_best(), S);
     for (int64_t d = (int64_t)blockIdx.y * NT + threadIdx.x; d < A.draws; d += (int64_t)gridDim.y * NT) {
-      A.index[d0 + d] = none ? -1 : (int32_t)R.first;
+      A.index[d0 + d] = none ? -1 : (int32_t)(R.first - row.lo);
       if (A.logp) A.logp[d0 + d] = none ? -INFINITY : 0.0f;
     }
     return;
@@ -798,7 +827,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   const float least = from ? key_score((uint32_t)(from >> 32)) : -INFINITY;
   const uint32_t last = ~(uint32_t)from;  // the last of those equal to it
   auto kept = [&](uint32_t i, float x) {
-    if (from ? x < least || (x == least && i > last) : !(x > -INFINITY)) return (uint64_t)0;
+    if (x < least || (x == least && from != 0 && i > last)) return (uint64_t)0;
     const uint32_t q = weight_of(x, R);
     return (uint64_t)(q >= R.least ? q : 0u);
   };
@@ -810,7 +839,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
       const uint64_t target = target_of(A.u[d0 + d], total);
       const uint32_t s = find_part(S, parts, target);
       const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, target, kept);
-      A.index[d0 + d] = (int32_t)i;
+      A.index[d0 + d] = (int32_t)(i - row.lo);
       if (A.logp) A.logp[d0 + d] = logp_of(clean(Score<TYPE>::get(row.row[i])), R, total);
     }
   } else {
@@ -820,7 +849,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
       const uint32_t s = find_part(S, parts, target);
       const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, target, kept);
       if (lane == 0) {
-        A.index[d0 + d] = (int32_t)i;
+        A.index[d0 + d] = (int32_t)(i - row.lo);
         if (A.logp) A.logp[d0 + d] = logp_of(clean(Score<TYPE>::get(row.row[i])), R, total);
       }
     }
@@ -829,55 +858,204 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
 
 // ----------------------------------------------------------------------------- loss
 
-__device__ __forceinline__ float wave_sum(float v) {
+// e^((x - m) / T) as a power of two, of (x - m) with the factor log2(e) / T: a rounding less than in steps.
+__device__ __forceinline__ float power(float d, float factor) { return __builtin_amdgcn_exp2f(d * factor); }
+
+// Sum (maximum) over groups of G lanes.
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+  for (int o = G / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, G);
   return v;
 }
-__device__ __forceinline__ float wave_max(float v) {
+template <int G>
+__device__ __forceinline__ float lanes_max(float v) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const float w = __shfl_xor(v, o, kWave);
-    v = w > v || w != w ? w : v;  // (a NaN stays)
+  for (int o = G / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, G));
+  return v;
+}
+
+// A row's answer: none for an index outside it, or scores that are all -inf (or NaN: the loss is one then).
+__device__ __forceinline__ bool answers(const LossArgs& A, int32_t index, float m, float sum) {
+  return index >= 0 && (uint32_t)index < A.n && (m > -INFINITY || sum != sum);
+}
+__device__ __forceinline__ float loss_of(const LossArgs& A, float x, float m, float sum, float c) {
+  return (logf(sum) - (x - m) * A.inv_t) * c;
+}
+
+// Rows of up to G scores, G lanes each.
+template <int TYPE, int G>
+__global__ void __launch_bounds__(256) k_loss_short(LossArgs A) {
+  using T = typename Score<TYPE>::T;
+  const uint32_t lane = threadIdx.x % G;
+  const int64_t rows = (int64_t)gridDim.x * (256 / G);
+  const float factor = A.inv_t * 1.44269504f;
+  for (int64_t r0 = (int64_t)blockIdx.x * (256 / G); r0 < A.rows; r0 += rows) {
+    const int64_t r = r0 + threadIdx.x / G;
+    if (r >= A.rows) return;  // (whole groups of lanes)
+    const bool in = lane < A.n;
+    const float x = in ? Score<TYPE>::get(static_cast<const T*>(A.x)[r * A.stride + lane]) : -INFINITY;
+    const int32_t a = A.index[r];
+    const float c = A.scale ? A.scale[r] : 1.0f;
+    const float m = lanes_max<G>(x);
+    const float e = x != -INFINITY ? power(x - m, factor) : 0.0f;
+    const float sum = lanes_sum<G>(e);
+    const bool some = answers(A, a, m, sum);
+    if (A.loss && (some ? lane == (uint32_t)a : lane == 0)) A.loss[r] = some ? loss_of(A, x, m, sum, c) : 0.0f;
+    if (A.grad && in) {
+      const float p = e / sum, g = (lane == (uint32_t)a ? p - 1.0f : p) * (c * A.inv_t);
+      static_cast<T*>(A.grad)[r * A.grad_stride + lane] = Score<TYPE>::put(some ? g : 0.0f);
+    }
+  }
+}
+
+// Sum (maximum) over a row's NT threads.
+template <int NT>
+__device__ __forceinline__ double row_sum(double v, double* part) {
+#pragma unroll
+  for (int o = kWave / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+  if constexpr (NT > kWave) {
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) v += part[i];
+  }
+  return v;
+}
+template <int NT>
+__device__ __forceinline__ float row_max(float v, float* part) {
+  v = lanes_max<kWave>(v);
+  if constexpr (NT > kWave) {
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < NT / kWave; ++i) v = fmaxf(v, part[i]);
   }
   return v;
 }
 
-// A wave for a row: maximum, sum, then the gradient, the row read three times.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_loss_row(LossArgs A) {
+// A row for NT threads (a wave: four rows to a workgroup), its scores in registers as J groups of 16 bytes to
+// a thread, or (J = 0) read for the maximum, the sum and the gradient. Groups lie where memory is aligned; the
+// row's first entry is number `lo` of its first group. The sum is taken in doubles, so that its float does
+// not depend on where the row lies. One read and one write of each row, which is what bounds it.
+template <int TYPE, int NT, int J>
+__global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A) {
   using T = typename Score<TYPE>::T;
-  const uint32_t lane = threadIdx.x % kWave;
-  const int64_t waves = (int64_t)gridDim.x * (256 / kWave);
-  for (int64_t r = (int64_t)blockIdx.x * (256 / kWave) + threadIdx.x / kWave; r < A.rows; r += waves) {
-    const T* row = static_cast<const T*>(A.x) + r * A.stride;
-    T* grad = A.grad ? static_cast<T*>(A.grad) + r * A.grad_stride : nullptr;
-    const int32_t a = A.index[r];
-    const float c = A.scale ? A.scale[r] : 1.0f;
+  constexpr uint32_t V = 16 / sizeof(T);
+  struct alignas(16) Group {
+    T v[V];
+  };
+  __shared__ float mpart[NT / kWave];
+  __shared__ double spart[NT / kWave];
+  const uint32_t tid = threadIdx.x % NT;
+  const int64_t r = (int64_t)blockIdx.x * (NT == kWave ? 4 : 1) + threadIdx.x / NT;
+  if (r >= A.rows) return;  // (a wave's row)
+  const T* row = static_cast<const T*>(A.x) + r * A.stride;
+  T* grad = A.grad ? static_cast<T*>(A.grad) + r * A.grad_stride : const_cast<T*>(row);  // (unused)
+  const uint32_t lo = (uint32_t)((uintptr_t)row / sizeof(T)) % V, n = A.n + lo;
+  // (stores of whole groups where the gradient's row lies like the scores')
+  const bool same = (uint32_t)((uintptr_t)grad / sizeof(T)) % V == lo;
+  row -= lo;
+  grad -= lo;
+  const int32_t a = A.index[r];
+  const float c = A.scale ? A.scale[r] : 1.0f;
+  const float factor = A.inv_t * 1.44269504f;
+  auto load = [&](uint32_t i, float (&v)[V]) {
+    if (i >= lo && i + V <= n) {
+      const Group f = *reinterpret_cast<const Group*>(row + i);
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) v[k] = Score<TYPE>::get(f.v[k]);
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k)
+        v[k] = i + k >= lo && i + k < n ? Score<TYPE>::get(row[i + k]) : -INFINITY;
+    }
+  };
+  const uint32_t at = lo + (uint32_t)a;  // the answer's place
+  auto store = [&](uint32_t i, const float (&e)[V], float sum, bool some) {
+    const float g = some ? c * A.inv_t : 0.0f, inv = some ? 1.0f / sum : 0.0f, scaled = inv * g;
+    Group f;
+#pragma unroll
+    for (uint32_t k = 0; k < V; ++k) {
+      const float d = i + k == at ? (e[k] * inv - 1.0f) * g : e[k] * scaled;
+      f.v[k] = Score<TYPE>::put(some ? d : 0.0f);
+    }
+    if (same && i >= lo && i + V <= n) {
+      *reinterpret_cast<Group*>(grad + i) = f;
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k)
+        if (i + k >= lo && i + k < n) grad[i + k] = f.v[k];
+    }
+  };
+  float x_at = 0.0f;
+  if (a >= 0 && (uint32_t)a < A.n) x_at = Score<TYPE>::get(row[at]);  // (before a gradient over the scores)
+  if constexpr (J > 0) {
+    float x[J][V];
     float m = -INFINITY;
-    for (uint32_t i = lane; i < A.n; i += kWave) {
-      const float v = Score<TYPE>::get(row[i]);
-      m = v > m || v != v ? v : m;
-    }
-    m = wave_max(m);
-    if (a < 0 || (uint32_t)a >= A.n || m == -INFINITY) {  // no answer
-      if (A.loss && lane == 0) A.loss[r] = 0.0f;
-      if (grad)
-        for (uint32_t i = lane; i < A.n; i += kWave) grad[i] = Score<TYPE>::put(0.0f);
-      continue;
-    }
-    float sum = 0.0f;
-    for (uint32_t i = lane; i < A.n; i += kWave)
-      sum += expf((Score<TYPE>::get(row[i]) - m) * A.inv_t);
-    sum = wave_sum(sum);
-    if (A.loss && lane == 0)
-      A.loss[r] = (logf(sum) - (Score<TYPE>::get(row[a]) - m) * A.inv_t) * c;
-    if (grad) {
-      const float g = c * A.inv_t, inv = 1.0f / sum;
-      for (uint32_t i = lane; i < A.n; i += kWave) {
-        const float p = expf((Score<TYPE>::get(row[i]) - m) * A.inv_t) * inv;
-        grad[i] = Score<TYPE>::put((i == (uint32_t)a ? p - 1.0f : p) * g);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const uint32_t i = V * ((uint32_t)j * NT + tid);
+      if ((uint32_t)j * NT * V < n) {  // (the row's)
+        load(i, x[j]);
+      } else {
+#pragma unroll
+        for (uint32_t k = 0; k < V; ++k) x[j][k] = -INFINITY;
       }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) m = fmaxf(m, x[j][k]);
+    m = row_max<NT>(m, mpart);
+    double all = 0.0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if ((uint32_t)j * NT * V >= n) break;
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) {
+        x[j][k] = x[j][k] != -INFINITY ? power(x[j][k] - m, factor) : 0.0f;
+        all += (double)x[j][k];
+      }
+    }
+    const float sum = (float)row_sum<NT>(all, spart);
+    const bool some = answers(A, a, m, sum);
+    if (A.loss && tid == 0) A.loss[r] = some ? loss_of(A, x_at, m, sum, c) : 0.0f;
+    if (!A.grad) return;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if ((uint32_t)j * NT * V >= n) break;
+      const uint32_t i = V * ((uint32_t)j * NT + tid);
+      if (i < n) store(i, x[j], sum, some);
+    }
+  } else {
+    float m = -INFINITY;
+    for (uint32_t i = V * tid; i < n; i += V * NT) {
+      float v[V];
+      load(i, v);
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) m = fmaxf(m, v[k]);
+    }
+    m = row_max<NT>(m, mpart);
+    double all = 0.0;
+    for (uint32_t i = V * tid; i < n; i += V * NT) {
+      float v[V];
+      load(i, v);
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) all += v[k] != -INFINITY ? (double)power(v[k] - m, factor) : 0.0;
+    }
+    const float sum = (float)row_sum<NT>(all, spart);
+    const bool some = answers(A, a, m, sum);
+    if (A.loss && tid == 0) A.loss[r] = some ? loss_of(A, x_at, m, sum, c) : 0.0f;
+    if (!A.grad) return;
+    for (uint32_t i = V * tid; i < n; i += V * NT) {
+      float v[V];
+      load(i, v);
+#pragma unroll
+      for (uint32_t k = 0; k < V; ++k) v[k] = power(v[k] - m, factor);
+      store(i, v, sum, some);
     }
   }
 }
@@ -900,17 +1078,38 @@ void launch_sample(const SampleArgs& A, hipStream_t s) {
   else if (A.n <= 16) launch_short<TYPE, 16>(A, s);
   else if (A.n <= 32) launch_short<TYPE, 32>(A, s);
   else if (A.n <= 64) launch_short<TYPE, 64>(A, s);
-  else if (A.n <= 1024) launch_row<TYPE, 256, 1>(A, s);
-  else if (A.n <= 4096) launch_row<TYPE, 256, 4>(A, s);
-  else if (A.n <= 8192) launch_row<TYPE, 256, 8>(A, s);
-  else if (A.n <= 16384) launch_row<TYPE, 1024, 4>(A, s);
-  else if (A.n <= 32768) launch_row<TYPE, 1024, 8>(A, s);
+  // (up to three entries more where a row is not aligned)
+  else if (A.n <= 1024 - 3) launch_row<TYPE, 256, 1>(A, s);
+  else if (A.n <= 4096 - 3) launch_row<TYPE, 256, 4>(A, s);
+  else if (A.n <= 8192 - 3) launch_row<TYPE, 256, 8>(A, s);
+  else if (A.n <= 16384 - 3) launch_row<TYPE, 1024, 4>(A, s);
+  else if (A.n <= 32768 - 3) launch_row<TYPE, 1024, 8>(A, s);
   else launch_row<TYPE, 1024, 0>(A, s);
+}
+template <int TYPE, int G>
+void launch_loss_short(const LossArgs& A, hipStream_t s) {
+  const int64_t b = (A.rows + 256 / G - 1) / (256 / G);
+  hipLaunchKernelGGL((k_loss_short<TYPE, G>), dim3((uint32_t)(b < 65536 ? b : 65536)), dim3(256), 0, s, A);
+}
+template <int TYPE, int NT, int J>
+void launch_loss_row(const LossArgs& A, hipStream_t s) {
+  const int64_t b = NT == kWave ? (A.rows + 3) / 4 : A.rows;
+  hipLaunchKernelGGL((k_loss_row<TYPE, NT, J>), dim3((uint32_t)b), dim3(NT == kWave ? 256 : NT), 0, s, A);
 }
 template <int TYPE>
 void launch_loss(const LossArgs& A, hipStream_t s) {
-  const int64_t b = (A.rows + 3) / 4;
-  hipLaunchKernelGGL(k_loss_row<TYPE>, dim3((uint32_t)(b < 8192 ? b : 8192)), dim3(256), 0, s, A);
+  constexpr uint32_t V = 16 / sizeof(typename Score<TYPE>::T);
+  const uint32_t n = A.n + V - 1;  // (where a row is not aligned)
+  if (A.n <= 8) launch_loss_short<TYPE, 8>(A, s);
+  else if (A.n <= 16) launch_loss_short<TYPE, 16>(A, s);
+  else if (A.n <= 32) launch_loss_short<TYPE, 32>(A, s);
+  else if (A.n <= 64) launch_loss_short<TYPE, 64>(A, s);
+  else if (n <= 16 * 64) launch_loss_row<TYPE, 64, 16 / V>(A, s);
+  else if (n <= 16 * 256) launch_loss_row<TYPE, 256, 16 / V>(A, s);
+  else if (n <= 64 * 256) launch_loss_row<TYPE, 256, 64 / V>(A, s);
+  else if (n <= 64 * 512) launch_loss_row<TYPE, 512, 64 / V>(A, s);
+  else if (n <= 64 * 1024) launch_loss_row<TYPE, 1024, 64 / V>(A, s);
+  else launch_loss_row<TYPE, 1024, 0>(A, s);
 }
 
 }  // namespace
@@ -923,7 +1122,7 @@ extern "C" hipError_t emr_launch_choice(int kind, const void* args, hipStream_t 
     const auto& A = *static_cast<const SampleArgs*>(args);
     if (A.rows <= 0 || A.draws <= 0) return hipSuccess;
     if (A.n == 0 || A.rows > 0x7FFFFFFF || A.part == 0 || A.part % kDrawPart != 0 ||
-        (A.n + A.part - 1) / A.part > kDrawSegs)
+        ((uint64_t)A.n + 3 + A.part - 1) / A.part > kDrawSegs)
       return hipErrorInvalidValue;
     switch (A.type) {
       case kTypeF32: launch_sample<kTypeF32>(A, s); break;

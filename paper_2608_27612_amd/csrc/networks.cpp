@@ -1483,11 +1483,6 @@ emr_status check_scores(const char* who, const emr_scores* S) {
   return EMR_OK;
 }
 
-// Whether groups of four entries of every row are aligned to their size.
-int32_t aligned4(const void* p, int64_t stride, int32_t type) {
-  return (uintptr_t)p % (uintptr_t)(4 * type_size(type)) == 0 && stride % 4 == 0;
-}
-
 }  // namespace
 
 extern "C" {
@@ -1755,7 +1750,6 @@ emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const 
   a.rows = scores->rows;
   a.n = (uint32_t)scores->n;
   a.type = scores->type;
-  a.vec = aligned4(scores->x, scores->stride, scores->type);
   a.t = rule->temperature;
   a.p = rule->top_p;
   a.min_p = rule->min_p;
@@ -1768,7 +1762,7 @@ emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const 
   a.draws = draws;
   a.index = index;
   a.logp = logp;
-  const uint32_t groups = (a.n + emr::kDrawPart - 1) / emr::kDrawPart;
+  const uint32_t groups = (a.n + 3 + emr::kDrawPart - 1) / emr::kDrawPart;
   a.part = (groups + emr::kDrawSegs - 1) / emr::kDrawSegs * emr::kDrawPart;
   const hipError_t e = emr_launch_net(40, &a, (hipStream_t)stream);
   if (e != hipSuccess) return failf(EMR_E_DEVICE, "sample: %s", hipGetErrorString(e));
@@ -1797,8 +1791,6 @@ emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const
   a.rows = scores->rows;
   a.n = (uint32_t)scores->n;
   a.type = scores->type;
-  a.vec = aligned4(scores->x, scores->stride, scores->type) &&
-          (!grad || aligned4(grad, grad_stride, scores->type));
   a.inv_t = 1.0f / temperature;
   a.index = index;
   a.scale = scale;
