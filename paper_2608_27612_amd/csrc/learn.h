@@ -87,6 +87,11 @@ constexpr uint32_t kLearnLds = 160u * 1024u;
 inline constexpr uint32_t learn_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 48u * groups; }
 constexpr uint32_t kLearnNodes = kLearnLds / 48u - 1u;
 
+// Nodes of a genome whose steps are launches of their own, several workgroups to a block of patterns: one
+// array of at least four patterns.
+inline constexpr uint32_t step_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 16u * groups; }
+constexpr uint32_t kStepNodes = kLearnLds / 16u - 1u;
+
 // Places and slices of one of a genome's layouts, at most: a slice's length is rounded up by up to kLearnPad - 1
 // sixteens; a heavy row or an output leaves up to fifteen places more; falling rows of at most
 // min(kLightEdges, e) edges leave sixteen times that.
@@ -144,6 +149,14 @@ struct LearnFillArgs {
   int64_t n;
 };
 
+// A workgroup of a step's launch: every chunks-th slice of a genome for one block of 4 `groups` patterns.
+struct LearnStepItem {
+  uint32_t genome, block, chunk, chunks;
+  int64_t values;  // of the block, in float4: [node][groups] in each of the three arrays
+  int64_t part;
+  uint32_t groups, pad;
+};
+
 struct LearnArgs {
   LearnSet set[kSets];
   const LearnItem* items;
@@ -165,6 +178,11 @@ struct LearnArgs {
   uint32_t steps;
   uint32_t first_item, n_items, n_joins;
   uint32_t threads, lds_bytes;
+  // a step's launch
+  const LearnStepItem* step_items;
+  const float4 *cur;           // values before it (derivatives after it), and the others
+  float4 *nxt, *held;          // held: the input edges' sums (the sum of the steps' derivatives)
+  uint32_t step;               // 1 .. steps, or (gradients) 1: the input edges
 };
 
 }  // namespace emr

@@ -194,8 +194,8 @@ constexpr uint32_t kAbsent = 0xFFFFFFFFu;
 
 // One of a genome's four layouts (blockIdx.y).
 __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs A) {
-  __shared__ uint32_t key[kLearnNodes];    // edges of a row (bit 31: an output's, always heavy), or kAbsent
-  __shared__ uint16_t rank[kLearnNodes];   // a row's place in the order
+  __shared__ uint32_t key[kStepNodes];    // edges of a row (bit 31: an output's, always heavy), or kAbsent
+  __shared__ uint16_t rank[kStepNodes];   // a row's place in the order
   __shared__ uint32_t part[kLayoutThreads / kWave];
   __shared__ uint32_t heavy, rows, places;
   const uint32_t g = A.genomes[blockIdx.x];
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs
   const bool inputs = which == kInInp || which == kOutInp;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (n > kLearnNodes) return;  // (host-checked)
+  if (n > kStepNodes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   constexpr uint32_t waves = kLayoutThreads / kWave;
   uint2* ent = S.ent + A.place[g];
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs
       d = (uint32_t)(A.out_offset[node + 1] - A.out_offset[node]);
     }
     if (lane == 0) {
-      const bool in = by_in ? !is_input && (!inputs || d > 0) : is_input == inputs;
+      const bool in = by_in ? !is_input : is_input == inputs;
       key[i] = in ? d : kAbsent;
     }
   }
@@ -383,7 +383,8 @@ __device__ __forceinline__ void heavy_sum(float4& a) {
 template <int LN>
 struct Place {
   uint32_t q, r;
-  uint32_t base, len, most;  // of the slice; the longest of the wave's slices
+  uint32_t base, len, full;  // of the slice; `full` past the first edges too
+  uint32_t most;             // the longest of the wave's slices
   uint32_t row;              // kNoRow: none
   bool heavy, any_heavy;
   bool writes;               // the lane holds its row's sum
@@ -402,6 +403,7 @@ __device__ __forceinline__ Place<LN> place_of(const LearnSlice* slices, const ui
     const LearnSlice S = slices[at];
     P.base = S.base;
     P.len = P.most = length(S);
+    P.full = S.len;
     P.heavy = P.any_heavy = S.heavy != 0;
     P.row = rows[16u * at + P.r];
   } else {
@@ -418,6 +420,7 @@ __device__ __forceinline__ Place<LN> place_of(const LearnSlice* slices, const ui
     const LearnSlice S = slices[in ? s : at];
     P.base = S.base;
     P.len = in ? length(S) : 0u;
+    P.full = in ? S.len : 0u;
     P.heavy = in && S.heavy != 0;
     P.row = in ? rows[16u * s + P.r] : kNoRow;
   }
@@ -468,11 +471,12 @@ __device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint2* __re
 }
 
 // The same for derivatives gz, and beside it the derivatives of the edges' weights, gz times the row's
-// own states s summed over the patterns, added to `sum` at the edges' places.
+// own states s summed over the patterns, added to `sum` at the edges' places (set: stored there, the first
+// time; with FIRST, zeros at the places past those).
 template <int LN>
 __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __restrict__ ent,
                                             const float4* gz, uint32_t n, const float4& s,
-                                            float* __restrict__ sum) {
+                                            float* __restrict__ sum, bool set) {
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   if (P.most > 0) {
     const uint64_t* e = reinterpret_cast<const uint64_t*>(ent) + P.base;
@@ -484,7 +488,7 @@ __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __r
     auto sums_at = [&](uint32_t k, float (&v)[own]) {
 #pragma unroll
       for (int c = 0; c < own; ++c)
-        v[c] = LN == 4 || k < P.len ? mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] : 0.0f;
+        v[c] = !set && (LN == 4 || k < P.len) ? mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] : 0.0f;
     };
     edges_at<LN>(e, 0, P, n, a);
     sums_at(0, had);
@@ -515,6 +519,8 @@ __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __r
       for (int c = 0; c < own; ++c) had[c] = next[c];
     }
   }
+  if (set)
+    for (uint32_t k = P.len + P.q; k < P.full; k += LN) sum[P.base + 16u * k + P.r] = 0.0f;
   if (P.any_heavy) {
     float4 h = acc;
     heavy_sum<LN>(h);
@@ -626,11 +632,11 @@ __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I
   const uint32_t hn = H.n_slices[g], in = E.n_slices[g], hp = H.n_places[g], ip = E.n_places[g];
   float *hsum = A.partial + I.part, *isum = hsum + hp;
   float4 *cur = lds, *nxt = lds + (n + 1u) * LN, *all = nxt + (n + 1u) * LN;
-  for (uint32_t i = threadIdx.x; i < hp + ip; i += blockDim.x) hsum[i] = 0.0f;
+  if (A.steps < 2)  // (no step of theirs)
+    for (uint32_t i = threadIdx.x; i < hp; i += blockDim.x) hsum[i] = 0.0f;
   for (uint32_t b = I.b0; b < I.b1; ++b) {
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
     for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) cur[i] = nxt[i] = all[i] = zero;
-    __threadfence_block();
     __syncthreads();
     const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
     for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
@@ -649,7 +655,7 @@ __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I
                                  : place_of<LN, false>(hs, hr, at, hn, lane);
         const uint32_t c =
             P.row != kNoRow ? *kept_at(A.kept, A.nodes, step - 2, b * LN + P.q, n0 + P.row) : 0u;
-        const float4 d = row_grads<LN>(P, he, cur, n, states(c), hsum);
+        const float4 d = row_grads<LN>(P, he, cur, n, states(c), hsum, last && b == I.b0);
         if (!P.writes) continue;
         const float4 v = make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
                                      d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
@@ -667,7 +673,7 @@ __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I
       const Place<LN> P = place_of<LN, false>(is, ir, at, in, lane);
       const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
       const float4 x = slot >= 0 ? pattern4(A, slot, b * LN + P.q) : zero;
-      const float4 d = row_grads<LN>(P, ie, all, n, x, isum);
+      const float4 d = row_grads<LN>(P, ie, all, n, x, isum, b == I.b0);
       if (!A.grad_inputs || !P.writes) continue;
       const float v[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
@@ -697,6 +703,152 @@ __global__ void __launch_bounds__(1024, 4) k_learn(LearnArgs A) {
     case 1: BACK ? back_item<1>(A, I, learn_lds_mem) : keep_item<1>(A, I, learn_lds_mem); break;
     case 2: BACK ? back_item<2>(A, I, learn_lds_mem) : keep_item<2>(A, I, learn_lds_mem); break;
     default: BACK ? back_item<4>(A, I, learn_lds_mem) : keep_item<4>(A, I, learn_lds_mem); break;
+  }
+}
+
+// One step of genomes too large for that, or too few to fill the chip: a workgroup holds all nodes' values of a
+// block of patterns and takes a share of the slices.
+template <int LN>
+__device__ __forceinline__ void keep_step(const LearnArgs& A, const LearnStepItem& I, float4* lds) {
+  const uint32_t g = I.genome;
+  const int64_t n0 = A.node_offset[g];
+  const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
+  if (step_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  const uint32_t lane = threadIdx.x % kWave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  constexpr uint32_t per = 4 / LN;
+  const bool first = A.step == 1, last = A.step == A.steps;
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4* cur = A.cur + I.values;
+  float4 *nxt = A.nxt + I.values, *held = A.held + I.values;
+  const LearnSet& E = A.set[first ? kInInp : kInHid];
+  const uint2* ent = E.ent + A.place[g];
+  const LearnSlice* slices = E.slices + A.slice[g];
+  const uint16_t* rows = E.rows + 16 * A.slice[g];
+  for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) {
+    const uint32_t node = i / LN;
+    float4 v = zero;
+    if (first) {  // the patterns; and what nodes without input edges hold
+      const int32_t slot = node < n ? A.node_in[n0 + node] : -1;
+      if (slot >= 0) v = pattern4(A, slot, I.block * LN + i % LN);
+      if (I.chunk == 0 && slot >= 0)
+        for (uint32_t t = 0; t < A.kept.planes; ++t)
+          *kept_at(A.kept, A.nodes, t, I.block * LN + i % LN, n0 + node) = 0;
+    } else if (node < n) {
+      v = cur[i];
+    }
+    lds[i] = v;
+  }
+  __syncthreads();
+  auto put = [&](uint32_t row, uint32_t q, const float4& z) {
+    const float4 s = make_float4(sigmoid_f(z.x), sigmoid_f(z.y), sigmoid_f(z.z), sigmoid_f(z.w));
+    nxt[row * LN + q] = s;
+    if (!last)
+      *kept_at(A.kept, A.nodes, A.step - 1, I.block * LN + q, n0 + row) =
+          code_of(s.x) | code_of(s.y) << 8 | code_of(s.z) << 16 | code_of(s.w) << 24;
+  };
+  const uint32_t end = first ? E.n_slices[g] : (last ? A.n_outputs : E.n_slices[g]);
+  for (uint32_t at = (wave * I.chunks + I.chunk) * per; at < end; at += waves * I.chunks * per) {
+    const Place<LN> P = place_of<LN, false>(slices, rows, at, end, lane);
+    const float4 z = row_sums<LN>(P, ent, lds, n);
+    if (!P.writes) continue;
+    const uint32_t i = P.row * LN + P.q;
+    if (first) {
+      held[i] = z;
+      put(P.row, P.q, z);
+    } else {
+      const float4 y = held[i];
+      put(P.row, P.q, make_float4(z.x + y.x, z.y + y.y, z.z + y.z, z.w + y.w));
+    }
+  }
+}
+
+template <int LN>
+__device__ __forceinline__ void back_step(const LearnArgs& A, const LearnStepItem& I, float4* lds) {
+  const uint32_t g = I.genome;
+  const int64_t n0 = A.node_offset[g];
+  const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
+  if (step_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  const uint32_t lane = threadIdx.x % kWave;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  constexpr uint32_t per = 4 / LN;
+  const bool inputs = A.step == 1, last = A.step == A.steps;
+  const LearnSet &H = A.set[kOutHid], &E = A.set[inputs ? kOutInp : kOutHid];
+  const uint2* ent = E.ent + A.place[g];
+  const LearnSlice* slices = E.slices + A.slice[g];
+  const uint16_t* rows = E.rows + 16 * A.slice[g];
+  float* sum = A.partial + I.part + (inputs ? H.n_places[g] : 0u);
+  const float4* from = (inputs ? A.held : A.cur) + I.values;
+  float4 *nxt = A.nxt + I.values, *all = A.held + I.values;
+  const uint32_t p0 = I.block * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
+  // the derivatives after the step (of all steps); those after the last are at the output nodes alone
+  for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
+    lds[i] = last || i >= n * LN ? make_float4(0.f, 0.f, 0.f, 0.f) : from[i];
+  __syncthreads();
+  if (last) {
+    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
+      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+      const int64_t r = ((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o;
+      const float v = A.outputs[r];
+      reinterpret_cast<float*>(lds)[(uint32_t)A.out_node[o] * 4u * LN + p] = A.grad_outputs[r] * v * (1.0f - v);
+    }
+    __syncthreads();
+  }
+  if (inputs && last)  // (one step: the other edges have no part)
+    for (uint32_t i = I.chunk * blockDim.x + threadIdx.x; i < H.n_places[g]; i += I.chunks * blockDim.x)
+      A.partial[I.part + i] = 0.0f;
+  const uint32_t end = E.n_slices[g];
+  for (uint32_t at = (wave * I.chunks + I.chunk) * per; at < end; at += waves * I.chunks * per) {
+    const Place<LN> P = last && !inputs ? place_of<LN, true>(slices, rows, at, end, lane)
+                                        : place_of<LN, false>(slices, rows, at, end, lane);
+    if (inputs) {
+      const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
+      const float4 x = slot >= 0 ? pattern4(A, slot, I.block * LN + P.q) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 d = row_grads<LN>(P, ent, lds, n, x, sum, true);
+      if (!A.grad_inputs || !P.writes) continue;
+      const float v[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t p = p0 + 4u * P.q + k;
+        if (p < A.n_patterns)
+          A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[k];
+      }
+      continue;
+    }
+    const uint32_t c =
+        P.row != kNoRow ? *kept_at(A.kept, A.nodes, A.step - 2, I.block * LN + P.q, n0 + P.row) : 0u;
+    const float4 d = row_grads<LN>(P, ent, lds, n, states(c), sum, last);
+    if (!P.writes) continue;
+    const float4 v = make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
+                                 d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
+    const uint32_t i = P.row * LN + P.q;
+    nxt[i] = v;
+    const float4 a = last ? lds[i] : all[i];
+    all[i] = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
+  }
+}
+
+template <bool BACK>
+__global__ void __launch_bounds__(1024, 4) k_learn_step(LearnArgs A) {
+  extern __shared__ float4 learn_lds_mem[];
+  const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
+  switch (I.groups) {
+    case 1: BACK ? back_step<1>(A, I, learn_lds_mem) : keep_step<1>(A, I, learn_lds_mem); break;
+    case 2: BACK ? back_step<2>(A, I, learn_lds_mem) : keep_step<2>(A, I, learn_lds_mem); break;
+    default: BACK ? back_step<4>(A, I, learn_lds_mem) : keep_step<4>(A, I, learn_lds_mem); break;
+  }
+}
+
+// The outputs of stepped genomes, from their states after the last step.
+__global__ void __launch_bounds__(kNetThreads) k_step_outputs(LearnArgs A) {
+  const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
+  if (I.chunk != 0) return;
+  const float* v = reinterpret_cast<const float*>(A.cur + I.values);
+  const uint32_t wide = 4u * I.groups, p0 = I.block * wide, np = min(A.n_patterns - p0, wide);
+  for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += kNetThreads) {
+    const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+    A.outputs[((int64_t)I.genome * A.n_patterns + p0 + p) * A.n_outputs + o] =
+        A.steps ? v[(uint32_t)A.out_node[o] * wide + p] : 0.0f;
   }
 }
 
@@ -733,7 +885,8 @@ uint32_t stride_blocks(int64_t n) {
 }  // namespace emr
 
 // Steps: 0 the edges' keys by source, 1 their offsets (after the sort), 2 a layout, 3 its weights; all steps
-// of the genomes in LDS: 4 activation, 5 gradients, 6 their joined sums; a larger genome: 7 the derivatives by
+// of the genomes in LDS: 4 activation, 5 gradients, 6 their joined sums; one step of others: 11 activation, 12
+// gradients, 13 the outputs; a genome larger than the LDS: 7 the derivatives by
 // the outputs' sums into gz_before (the other half behind it cleared), 8 one step's weight derivatives, 9 one
 // step backwards; 10 zeros.
 extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s) {
@@ -813,6 +966,21 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       const auto& A = *static_cast<const LearnFillArgs*>(args);
       if (A.n <= 0) return hipSuccess;
       hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(A.n)), blk, 0, s, A);
+      break;
+    }
+    case 11:
+    case 12:
+    case 13: {
+      const auto& A = *static_cast<const LearnArgs*>(args);
+      if (A.n_items == 0) return hipSuccess;
+      if (A.lds_bytes > kLearnLds || A.threads == 0 || A.threads > 1024u || A.threads % kWave != 0)
+        return hipErrorInvalidValue;
+      if (step == 11)
+        hipLaunchKernelGGL(k_learn_step<false>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      else if (step == 12)
+        hipLaunchKernelGGL(k_learn_step<true>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      else
+        hipLaunchKernelGGL(k_step_outputs, dim3(A.n_items), blk, 0, s, A);
       break;
     }
     default:

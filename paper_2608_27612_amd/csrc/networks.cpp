@@ -307,22 +307,25 @@ struct emr_networks {
     };
     struct Plan {
       int32_t patterns = 0;
-      Dev items, joins;
+      Dev items, joins, step_items;
       uint32_t n_joins = 0;
       std::vector<Run> runs;
+      Run steps{};                // the stepped genomes' launches
+      int64_t values = 0;         // float4 of each of their three arrays
       int64_t partial_floats = 0;
     };
     std::vector<std::unique_ptr<Plan>> plans;  // by number of patterns, the oldest first
-    Dev partial, back;
+    Dev partial, back, values;
     void release_idle() {
       for (int k = 0; k < emr::kSets; ++k)
         for (Dev* d : {&ent[k], &edge[k], &slices[k], &rows[k]}) d->reset_idle();
       for (Dev* d : {&n_slices, &n_places, &place, &slice, &fits, &large, &edge_dst, &out_offset, &out_edge,
-                     &partial, &back})
+                     &partial, &back, &values})
         d->reset_idle();
       for (auto& p : plans) {
         p->items.reset_idle();
         p->joins.reset_idle();
+        p->step_items.reset_idle();
       }
     }
   } learn;
@@ -1091,7 +1094,7 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
       const int64_t n = N.node_off[g + 1] - N.node_off[g], e = N.edge_off[g + 1] - N.edge_off[g];
       place[g] = places;
       slice[g] = slices;
-      if (n > (int64_t)emr::kLearnNodes || emr::learn_places(n, e, N.n_out) > INT32_MAX) {
+      if (n > (int64_t)emr::kStepNodes || emr::learn_places(n, e, N.n_out) > INT32_MAX) {
         L.big.push_back(g);
         continue;
       }
@@ -1200,6 +1203,11 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
   double total = 0.0;
   for (uint32_t g : L.fit) total += load(g) * shape(g).blocks;
+  // A genome is stepped that does not fit, or of which one block is longer work than four times a compute
+  // unit's share of all, and than its steps' launches (8192 edges: about 12 us a step).
+  auto stepped = [&](uint32_t g) {
+    return nodes(g) > (int64_t)emr::kLearnNodes || load(g) > std::max(4.0 * total / 256.0, 8192.0);
+  };
   // large workgroups alone on a compute unit, in pairs, and small ones
   constexpr struct { uint32_t lds, threads; } kRuns[] = {
       {emr::kLearnLds, 1024}, {emr::kLearnLds / 2, 1024}, {emr::kLearnLds / 4, 256}};
@@ -1212,7 +1220,7 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
     uint32_t lds = 0;
     for (uint32_t g : L.fit) {
       const Shape S = shape(g);
-      if (run_of(S.lds) != r) continue;
+      if (stepped(g) || run_of(S.lds) != r) continue;
       by.emplace_back(-load(g) * S.blocks, g);
       lds = std::max(lds, S.lds);
     }
@@ -1233,7 +1241,38 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
     if (items.size() > first)
       plan->runs.push_back({first, (uint32_t)items.size() - first, kRuns[r].threads, lds});
   }
-  if (items.size() > 0x7FFFFFFF) return failf(EMR_E_LIMIT, "networks: too many genomes x patterns");
+  // stepped genomes: about two workgroups for each compute unit
+  std::vector<emr::LearnStepItem> steps;
+  auto step_shape = [&](uint32_t g) {
+    Shape S{n_patterns <= 4 ? 1u : (n_patterns <= 8 ? 2u : 4u), 0, 0};
+    while (S.groups > 1 && emr::step_lds((uint32_t)nodes(g), S.groups) > emr::kLearnLds) S.groups /= 2;
+    S.lds = emr::step_lds((uint32_t)nodes(g), S.groups);
+    S.blocks = ((uint32_t)n_patterns + 4 * S.groups - 1) / (4 * S.groups);
+    return S;
+  };
+  double all = 0.0;
+  for (uint32_t g : L.fit)
+    if (stepped(g)) all += load(g) * step_shape(g).blocks;
+  for (uint32_t g : L.fit) {
+    if (!stepped(g)) continue;
+    const Shape S = step_shape(g);
+    const uint32_t waves = ((uint32_t)nodes(g) / 16 + 1) * S.groups / 4 + 1;
+    const uint32_t chunks = (uint32_t)std::min<double>(
+        std::max(1u, waves / 16), std::max(1.0, std::ceil(load(g) * 512.0 / std::max(all, 1.0))));
+    const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
+    joins.push_back({g, S.blocks, part, stride});
+    plan->steps.lds = std::max(plan->steps.lds, S.lds);
+    for (uint32_t b = 0; b < S.blocks; ++b, part += stride) {
+      for (uint32_t c = 0; c < chunks; ++c) steps.push_back({g, b, c, chunks, plan->values, part, S.groups, 0});
+      plan->values += nodes(g) * S.groups;
+    }
+  }
+  plan->steps.threads = 1024;
+  plan->steps.count = (uint32_t)steps.size();
+  if (items.size() + steps.size() > 0x7FFFFFFF)
+    return failf(EMR_E_LIMIT, "networks: too many genomes x patterns");
+  NET_TRY(alloc(plan->step_items, steps.size() * sizeof(emr::LearnStepItem), "learning items", s));
+  NET_TRY(to_device(plan->step_items.p, steps.data(), steps.size() * sizeof(emr::LearnStepItem), s));
   NET_TRY(alloc(plan->items, items.size() * sizeof(emr::LearnItem), "learning items", s));
   NET_TRY(to_device(plan->items.p, items.data(), items.size() * sizeof(emr::LearnItem), s));
   NET_TRY(alloc(plan->joins, joins.size() * sizeof(emr::LearnJoin), "learning joins", s));
@@ -1260,6 +1299,9 @@ emr_status learn_args(emr_networks& N, const float* inputs, int32_t n_patterns, 
   A->items = (*plan)->items.as<emr::LearnItem>();
   A->joins = (*plan)->joins.as<emr::LearnJoin>();
   A->n_joins = (*plan)->n_joins;
+  A->step_items = (*plan)->step_items.as<emr::LearnStepItem>();
+  const size_t need = (size_t)(*plan)->values * 48;
+  if (N.learn.values.bytes < need) NET_TRY(alloc(N.learn.values, need, "stepped values", s));
   A->place = N.learn.place.as<int64_t>();
   A->slice = N.learn.slice.as<int64_t>();
   A->node_offset = N.node_offset.as<int64_t>();
@@ -1275,6 +1317,18 @@ emr_status learn_args(emr_networks& N, const float* inputs, int32_t n_patterns, 
   A->n_sub = (uint32_t)N.n_sub;
   A->steps = (uint32_t)steps;
   return EMR_OK;
+}
+
+// The stepped genomes' launches: value arrays a and b swap from step to step.
+void step_args(const emr_networks& N, const emr_networks::Learning::Plan& plan, int swap, emr::LearnArgs& A) {
+  float4* v = N.learn.values.as<float4>();
+  A.first_item = 0;
+  A.n_items = plan.steps.count;
+  A.threads = plan.steps.threads;
+  A.lds_bytes = plan.steps.lds;
+  A.cur = v + (swap ? plan.values : 0);
+  A.nxt = v + (swap ? 0 : plan.values);
+  A.held = v + 2 * plan.values;
 }
 
 // The items' launches (step: 24 activation, 25 gradients).
@@ -1295,6 +1349,16 @@ emr_status run_keep(emr_networks& N, const float* inputs, int32_t n_patterns, in
   emr_networks::Learning::Plan* plan;
   NET_TRY(learn_args(N, inputs, n_patterns, steps, outputs, K, &A, &plan, s));
   NET_TRY(run_items(*plan, A, 24, s));
+  if (plan->steps.count > 0) {
+    int swap = 0;
+    for (int32_t t = 1; t <= steps; ++t, swap ^= 1) {
+      step_args(N, *plan, swap, A);
+      A.step = (uint32_t)t;
+      NET_HIP(emr_launch_net(31, &A, s));
+    }
+    step_args(N, *plan, swap, A);
+    NET_HIP(emr_launch_net(33, &A, s));
+  }
   const auto& big = N.learn.big;
   const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
   const size_t half = (size_t)pblocks * (size_t)N.nodes * 16;
@@ -1354,6 +1418,14 @@ emr_status run_backward(emr_networks& N, const float* inputs, int32_t n_patterns
   A.grad_w = grad_w;
   A.grad_inputs = grad_inputs;
   NET_TRY(run_items(*plan, A, 25, s));
+  if (plan->steps.count > 0) {
+    int swap = 0;
+    for (int32_t t = steps; t >= 1; --t, swap ^= 1) {
+      step_args(N, *plan, swap, A);
+      A.step = (uint32_t)t;
+      NET_HIP(emr_launch_net(32, &A, s));
+    }
+  }
   NET_HIP(emr_launch_net(26, &A, s));
   const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
   size_t half = 0;

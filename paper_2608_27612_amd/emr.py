@@ -932,6 +932,7 @@ class Networks:
 
     def __init__(self, handle):
         self.handle = handle
+        self._counts = None
 
     def __del__(self):
         if getattr(self, "handle", None) and _lib is not None:
@@ -942,6 +943,13 @@ class Networks:
         i = emr_network_info()
         _check(lib().emr_networks_info(self.handle, C.byref(i)))
         return i
+
+    def _sizes(self):
+        """(genomes, nodes, edges, inputs, outputs), which no call changes."""
+        if self._counts is None:
+            i = self.info()
+            self._counts = (i.n_genomes, i.nodes, i.edges, i.n_inputs, i.n_outputs)
+        return self._counts
 
     def to_host(self, stream=None):
         """Per genome dict(cells: kept hidden cells ascending, src, dst, w: the edges with the
@@ -1024,42 +1032,37 @@ class Networks:
     def set_weights(self, w, stream=None):
         """The weight of every edge (a float32 device tensor in the order of in_w) for later calls."""
         import torch
-        with _on(stream):
-            w = _on_device("w", w, torch.float32, (self.info().edges,)).contiguous()
-            _check(lib().emr_networks_set_weights(self.handle, C.c_void_p(w.data_ptr()),
-                                                  _stream_ptr(stream)))
+        with _On(stream) as raw:
+            w = _on_device("w", w, torch.float32, (self._sizes()[2],)).contiguous()
+            _check(lib().emr_networks_set_weights(self.handle, w.data_ptr(), raw))
 
     def weights(self, stream=None):
         """A copy of the edges' weights (numpy, in the order of in_w)."""
         i = self.info()
         return _dev_to_host(i.in_w, i.edges, np.float32, stream)
 
-    def _patterns(self, inputs, info):
+    def _patterns(self, inputs):
         import torch
+        n_in = self._sizes()[3]
         _on_device("inputs", inputs, torch.float32)
-        if inputs.dim() != 2 or inputs.shape[1] != info.n_inputs:
-            raise ValueError("inputs: shape (patterns, %d) is needed, not %s"
-                             % (info.n_inputs, tuple(inputs.shape)))
+        if inputs.dim() != 2 or inputs.shape[1] != n_in:
+            raise ValueError("inputs: shape (patterns, %d) is needed, not %s" % (n_in, tuple(inputs.shape)))
         return inputs.contiguous()
 
     def activate_keep(self, inputs, steps: int, stream=None):
         """Outputs (float32 device tensor [n_genomes, n_patterns, n_outputs]) of emr_activate_keep for
         `inputs` (float32 device tensor [n_patterns, n_inputs]), and the Kept states; not synchronized."""
         import torch
-        with _on(stream):
-            i = self.info()
-            x = self._patterns(inputs, i)
+        with _On(stream) as raw:
+            G, nodes, edges, n_in, n_out = self._sizes()
+            x = self._patterns(inputs)
             P = x.shape[0]
-            n = C.c_int64()
-            _check(lib().emr_kept_bytes(self.handle, P, steps, C.byref(n)))
-            out = torch.empty((i.n_genomes, P, i.n_outputs), dtype=torch.float32, device=x.device)
+            out = torch.empty((G, P, n_out), dtype=torch.float32, device=x.device)
             b = _kept_width(P)
-            codes = torch.empty((max(steps - 1, 0), -(-P // b), i.nodes, b), dtype=torch.uint8,
+            codes = torch.empty((max(steps - 1, 0), -(-P // b), nodes, b), dtype=torch.uint8,
                                 device=x.device)
-            assert codes.numel() == n.value
-            _check(lib().emr_activate_keep(self.handle, C.c_void_p(x.data_ptr()), P, steps,
-                                           C.c_void_p(out.data_ptr()), C.c_void_p(codes.data_ptr()),
-                                           n.value, _stream_ptr(stream)))
+            _check(lib().emr_activate_keep(self.handle, x.data_ptr(), P, steps, out.data_ptr(),
+                                           codes.data_ptr(), codes.numel(), raw))
             return out, Kept(codes, P)
 
     def activate_backward(self, inputs, steps: int, outputs, kept, grad_outputs, grad_inputs: bool = False,
@@ -1069,25 +1072,24 @@ class Networks:
         activate_keep's inputs, outputs and Kept and the derivatives by the outputs; see
         emr_activate_backward in include/emr.h. Not synchronized."""
         import torch
-        with _on(stream):
-            i = self.info()
-            x = self._patterns(inputs, i)
+        with _On(stream) as raw:
+            G, nodes, edges, n_in, n_out = self._sizes()
+            x = self._patterns(inputs)
             P = x.shape[0]
-            shape = (i.n_genomes, P, i.n_outputs)
+            shape = (G, P, n_out)
             outputs = _on_device("outputs", outputs, torch.float32, shape).contiguous()
             grad_outputs = _on_device("grad_outputs", grad_outputs, torch.float32, shape).contiguous()
             b = _kept_width(P)
             codes = _on_device("kept", kept.codes, torch.uint8,
-                               (max(steps - 1, 0), -(-P // b), i.nodes, b)).contiguous()
-            grad_w = torch.empty(i.edges, dtype=torch.float32, device=x.device)
-            grad_x = torch.empty((i.n_genomes, P, i.n_inputs), dtype=torch.float32,
+                               (max(steps - 1, 0), -(-P // b), nodes, b)).contiguous()
+            grad_w = torch.empty(edges, dtype=torch.float32, device=x.device)
+            grad_x = torch.empty((G, P, n_in), dtype=torch.float32,
                                  device=x.device) if grad_inputs else None
             # (a network without edges has no memory for them: any address will do)
             _check(lib().emr_activate_backward(
-                self.handle, C.c_void_p(x.data_ptr()), P, steps, C.c_void_p(outputs.data_ptr()),
-                C.c_void_p(codes.data_ptr()), codes.numel(), C.c_void_p(grad_outputs.data_ptr()),
-                C.c_void_p(grad_w.data_ptr() or x.data_ptr()),
-                C.c_void_p(0 if grad_x is None else grad_x.data_ptr()), _stream_ptr(stream)))
+                self.handle, x.data_ptr(), P, steps, outputs.data_ptr(), codes.data_ptr(), codes.numel(),
+                grad_outputs.data_ptr(), grad_w.data_ptr() or x.data_ptr(),
+                None if grad_x is None else grad_x.data_ptr(), raw))
             return grad_w, grad_x
 
 
@@ -1169,23 +1171,48 @@ def _on_device(name, t, dtype=None, shape=None):
     return t
 
 
-def _on(stream):
-    """The stream that a call's copies and results are made on: the call's own."""
-    import contextlib
-    import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+class _On:
+    """The stream that a call's copies and results are made on: the call's own, as `raw`."""
+
+    def __init__(self, stream):
+        import torch
+        if stream is not None:
+            self.outer, self.raw = torch.cuda.stream(stream), stream.cuda_stream
+            return
+        self.outer = None
+        try:  # (without a Stream object: that takes longer than most calls' launch)
+            self.raw = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        except AttributeError:
+            self.raw = torch.cuda.current_stream().cuda_stream
+
+    def __enter__(self):
+        if self.outer is not None:
+            self.outer.__enter__()
+        return self.raw
+
+    def __exit__(self, *e):
+        if self.outer is not None:
+            self.outer.__exit__(*e)
+
+
+_SCORE_TYPES = {}
 
 
 def _scores(x):
     """emr_scores of a device tensor [rows, n] (a copy where its last dimension is strided), and the
     tensor that holds them."""
-    import torch
-    types = {torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16}
-    if not torch.is_tensor(x) or not x.is_cuda or x.dim() != 2 or x.dtype not in types:
+    if not _SCORE_TYPES:
+        import torch
+        _SCORE_TYPES.update({torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16})
+    kind = _SCORE_TYPES.get(getattr(x, "dtype", None))
+    if kind is None or not x.is_cuda or x.dim() != 2:
         raise ValueError("scores: a device tensor [rows, n] of float32, bfloat16 or float16 is needed")
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    rows, n = x.shape
+    stride, inner = x.stride()
+    if inner != 1 and n > 1:
         x = x.contiguous()
-    return emr_scores(x.data_ptr(), types[x.dtype], x.shape[0], x.shape[1], x.stride(0)), x
+        stride = n
+    return emr_scores(x.data_ptr(), kind, rows, n, stride), x
 
 
 def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: bool = True, stream=None):
@@ -1194,28 +1221,27 @@ def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: 
     one for each row (float32; top_k int32). Returns index (int32 [rows, draws]) and their
     log-probabilities (float32, or None without logp), not synchronized."""
     import torch
-    with _on(stream):
+    with _On(stream) as raw:
         st, x = _scores(scores)
-        rows = x.shape[0]
+        rows = st.rows
         _on_device("u", u, torch.float32)
         if u.dim() != 2 or u.shape[0] != rows:
             raise ValueError("u: shape (%d, draws) is needed, not %s" % (rows, tuple(u.shape)))
         u = u.contiguous()
-        value, held = {}, []
+        rule, held = [], []
         for name, v, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                                ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
             if torch.is_tensor(v):
                 v = _on_device(name, v, dtype, (rows,)).contiguous()
                 held.append(v)
-                value[name], value["row_" + name] = 0, v.data_ptr()
+                rule += (0, v.data_ptr())
             else:
-                value[name], value["row_" + name] = v, 0
-        rule = emr_sampling(**value)
-        index = torch.empty(u.shape, dtype=torch.int32, device=x.device)
-        lp = torch.empty(u.shape, dtype=torch.float32, device=x.device) if logp else None
-        _check(lib().emr_sample(C.byref(st), C.byref(rule), C.c_void_p(u.data_ptr()), u.shape[1],
-                                C.c_void_p(index.data_ptr()),
-                                C.c_void_p(lp.data_ptr() if logp else 0), _stream_ptr(stream)))
+                rule += (v, None)
+        rule = emr_sampling(*rule)
+        index = torch.empty_like(u, dtype=torch.int32)
+        lp = torch.empty_like(u) if logp else None
+        _check(lib().emr_sample(C.byref(st), C.byref(rule), u.data_ptr(), u.shape[1], index.data_ptr(),
+                                lp.data_ptr() if logp else None, raw))
         return index, lp
 
 
@@ -1224,16 +1250,14 @@ def emr_answer_loss(scores, index, scale=None, temperature: float = 1.0, stream=
     include/emr.h. index: int32 [rows]; scale: float32 [rows] or None. Returns loss (float32 [rows]) and
     grad ([rows, n], of the scores' type), not synchronized."""
     import torch
-    with _on(stream):
+    with _On(stream) as raw:
         st, x = _scores(scores)
-        rows = x.shape[0]
+        rows, n = x.shape
         index = _on_device("index", index, torch.int32, (rows,)).contiguous()
         if scale is not None:
             scale = _on_device("scale", scale, torch.float32, (rows,)).contiguous()
         loss = torch.empty(rows, dtype=torch.float32, device=x.device)
-        grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        _check(lib().emr_answer_loss(C.byref(st), C.c_void_p(index.data_ptr()),
-                                     C.c_void_p(0 if scale is None else scale.data_ptr()),
-                                     C.c_float(temperature), C.c_void_p(loss.data_ptr()),
-                                     C.c_void_p(grad.data_ptr()), x.shape[1], _stream_ptr(stream)))
+        grad = torch.empty((rows, n), dtype=x.dtype, device=x.device)
+        _check(lib().emr_answer_loss(C.byref(st), index.data_ptr(), None if scale is None else scale.data_ptr(),
+                                     temperature, loss.data_ptr(), grad.data_ptr(), n, raw))
         return loss, grad
