@@ -3,12 +3,12 @@
 // Rows. A genome's edges are laid out four times, by destination ("in") and by source ("out"), the ones
 // from input nodes apart from the others ("inp", "hid"): an input holds still over the steps, so its edges
 // count once where the others count in every step. A row is a node with its edges of one kind. Rows
-// lie in slices of sixteen places:
+// lie in slices of sixteen places, the heavy ones first:
+//   - a heavy slice holds one row of many edges (more than kLightEdges; the output nodes of "in" always),
+//     its edge k at base + k: the lanes of a wave share it and add their sums at the end;
 //   - a light slice holds sixteen rows, the edge k of its row r at base + 16 k + r, so that the
 //     lanes of a wave, a row each, read sixteen edges side by side; rows come in falling order of
-//     edges, which leaves few places empty;
-//   - a heavy slice holds one row of many edges (more than kLightEdges; the output nodes of "in" always),
-//     its edge k at base + k: sixteen lanes share it and add their sums at the end.
+//     edges, which leaves few places empty.
 // An empty place has the weight 0 and, as the other node, the one past the genome's last, whose values
 // are zeros.
 #pragma once
@@ -78,19 +78,24 @@ struct LearnSet {
   LearnSlice* slices;
   uint16_t* rows;      // [slice * 16] local nodes (heavy: the same one), kNoRow: none
   uint32_t* n_slices;  // [n_genomes]
+  uint32_t* n_heavy;   // [n_genomes] of them
   uint32_t* n_places;  // [n_genomes]
 };
 constexpr uint32_t kNoRow = 0xFFFFu;
 
-// Nodes that fit a workgroup: three arrays of at least four patterns of floats, and one node more.
+// A workgroup's block of patterns: a row has `lanes` lanes, each with `groups` times four of them. The values
+// of a genome's nodes before a step lie in LDS, those after it and a third array (the input edges' sums, the
+// sum of the steps' derivatives) there too (local), or in memory.
+struct LearnShape {
+  uint32_t lanes, groups, local;
+};
+constexpr LearnShape kLearnShapes[] = {{1, 1, 1}, {1, 1, 0}, {2, 1, 1}, {2, 1, 0},
+                                       {4, 1, 1}, {4, 1, 0}, {4, 2, 1}, {4, 2, 0}};
 constexpr uint32_t kLearnLds = 160u * 1024u;
-inline constexpr uint32_t learn_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 48u * groups; }
-constexpr uint32_t kLearnNodes = kLearnLds / 48u - 1u;
-
-// Nodes of a genome whose steps are launches of their own, several workgroups to a block of patterns: one
-// array of at least four patterns.
-inline constexpr uint32_t step_lds(uint32_t n, uint32_t groups) { return (n + 1u) * 16u * groups; }
-constexpr uint32_t kStepNodes = kLearnLds / 16u - 1u;
+inline constexpr uint32_t learn_lds(uint32_t n, const LearnShape& S) {
+  return (n + 1u) * 16u * S.lanes * S.groups * (S.local ? 3u : 1u);
+}
+constexpr uint32_t kLearnNodes = kLearnLds / 16u - 1u;  // the most nodes of a genome that any shape takes
 
 // Places and slices of one of a genome's layouts, at most: a slice's length is rounded up by up to kLearnPad - 1
 // sixteens; a heavy row or an output leaves up to fifteen places more; falling rows of at most
@@ -104,8 +109,16 @@ inline constexpr int64_t learn_places(int64_t n, int64_t e, int64_t n_out) {
   return (e + 15 * (e / kLightEdges + n_out) + 16 * light +
           16 * (kLearnPad - 1) * learn_slices(used, e, n_out) + 31) / 16 * 16;
 }
+struct LearnRow {
+  int64_t place;   // of its first edge
+  uint32_t node0;  // the genome's first node
+  uint32_t slice;  // of the genome (while rows are ranked: the row's rank); bit 31: heavy; kNoEdge: no row
+};
 struct LearnLayoutArgs {
-  LearnSet set[kSets];
+  LearnSet set;
+  int32_t which;
+  uint32_t* key;               // [nodes] edges of the node's row, or kNoEdge
+  LearnRow* row;               // [nodes]
   const uint32_t* genomes;     // [count]
   const int64_t* place;        // [n_genomes]
   const int64_t* slice;        // [n_genomes]
@@ -117,6 +130,7 @@ struct LearnLayoutArgs {
   const float* in_w;
   const int64_t* out_offset;
   const uint64_t* out_edge;    // [edges] edge | destination << 32
+  int64_t nodes;
   uint32_t count, n_outputs, n_sub;
 };
 
@@ -129,13 +143,13 @@ struct LearnWeightsArgs {
   uint32_t count;
 };
 
-// A workgroup's share: patterns blocks b0 .. b1 - 1 of 4 `groups` patterns of one genome. The weights'
-// derivatives of its share are summed at partial + part (places of kOutHid, then of kOutInp).
+// A workgroup's share: blocks of patterns b0 .. b1 - 1 of one genome. The weights' derivatives of its share
+// are summed at partial + part (places of kOutHid, then of kOutInp).
 struct LearnItem {
-  uint32_t genome, b0, b1, groups;
-  int64_t part;
+  uint32_t genome, b0, b1;
   uint32_t alone;     // the genome has no other item: its derivatives go to grad_w directly
-  uint32_t pad;
+  int64_t part;
+  int64_t values;     // (not local) in float4: [2][node][lanes * groups]
 };
 
 // The genomes of more than one item.
@@ -149,12 +163,12 @@ struct LearnFillArgs {
   int64_t n;
 };
 
-// A workgroup of a step's launch: every chunks-th slice of a genome for one block of 4 `groups` patterns.
+// A workgroup of a step's launch: every chunks-th unit of rows of a genome for one block of 4 `lanes` patterns.
 struct LearnStepItem {
   uint32_t genome, block, chunk, chunks;
-  int64_t values;  // of the block, in float4: [node][groups] in each of the three arrays
+  int64_t values;  // of the block, in float4: [node][lanes] in each of the three arrays
   int64_t part;
-  uint32_t groups, pad;
+  uint32_t lanes, pad;
 };
 
 struct LearnArgs {
@@ -178,6 +192,8 @@ struct LearnArgs {
   uint32_t steps;
   uint32_t first_item, n_items, n_joins;
   uint32_t threads, lds_bytes;
+  uint32_t shape;              // of kLearnShapes
+  float4* values;              // (not local)
   // a step's launch
   const LearnStepItem* step_items;
   const float4 *cur;           // values before it (derivatives after it), and the others

@@ -164,6 +164,30 @@ __global__ void __launch_bounds__(kNetThreads) k_back_nodes(NetBackArgs A) {
 
 // ----------------------------------------------------------------------------- layouts
 
+__device__ __forceinline__ bool by_destination(int which) { return which == kInHid || which == kInInp; }
+__device__ __forceinline__ bool of_inputs(int which) { return which == kInInp || which == kOutInp; }
+
+// A wave for a node: the edges of its row.
+__global__ void __launch_bounds__(kNetThreads) k_layout_degrees(LearnLayoutArgs A) {
+  const uint32_t lane = threadIdx.x % kWave;
+  const bool in = by_destination(A.which), inputs = of_inputs(A.which);
+  for (int64_t i = grid_thread() / kWave; i < A.nodes; i += grid_threads() / kWave) {
+    const bool is_input = A.node_in[i] >= 0;
+    uint32_t d = kNoEdge;
+    if (!in) {
+      if (is_input == inputs) d = (uint32_t)(A.out_offset[i + 1] - A.out_offset[i]);
+    } else if (!is_input) {
+      const int64_t e1 = A.in_offset[i + 1];
+      d = 0;
+      for (int64_t e = A.in_offset[i]; e < e1; e += kWave) {
+        const int64_t k = e + lane;
+        d += (uint32_t)__popcll(__ballot(k < e1 && (A.node_in[A.in_src[k < e1 ? k : e]] >= 0) == inputs));
+      }
+    }
+    if (lane == 0) A.key[i] = d;
+  }
+}
+
 // Exclusive prefix sum over the workgroup (every thread must call it); *total receives the sum.
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* part, uint32_t* total) {
   const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
@@ -190,82 +214,71 @@ __device__ __forceinline__ uint32_t padded(uint32_t len) {
 }
 
 constexpr int kLayoutThreads = 512;
-constexpr uint32_t kAbsent = 0xFFFFFFFFu;
+constexpr uint32_t kLayoutBins = 1024;  // by edges; the last: output nodes of kInHid, then all longer rows
 
-// One of a genome's four layouts (blockIdx.y).
-__global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs A) {
-  __shared__ uint32_t key[kStepNodes];    // edges of a row (bit 31: an output's, always heavy), or kAbsent
-  __shared__ uint16_t rank[kStepNodes];   // a row's place in the order
+// A workgroup for a genome: its rows ranked by falling edges (equal ones by node), its slices, and where each
+// row's edges go.
+__global__ void __launch_bounds__(kLayoutThreads) k_layout_slices(LearnLayoutArgs A) {
+  __shared__ uint32_t bin[kLayoutBins];  // rows of it, then the rank of its next one
+  __shared__ uint32_t key[kLayoutThreads];
   __shared__ uint32_t part[kLayoutThreads / kWave];
-  __shared__ uint32_t heavy, rows, places;
   const uint32_t g = A.genomes[blockIdx.x];
-  const int which = (int)blockIdx.y;
-  const LearnSet S = A.set[which];
-  const bool by_in = which == kInHid || which == kInInp;
-  const bool inputs = which == kInInp || which == kOutInp;
+  const LearnSet& S = A.set;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (n > kStepNodes) return;  // (host-checked)
-  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  constexpr uint32_t waves = kLayoutThreads / kWave;
-  uint2* ent = S.ent + A.place[g];
-  uint32_t* edge = S.edge + A.place[g];
   LearnSlice* slices = S.slices + A.slice[g];
   uint16_t* row_of = S.rows + 16 * A.slice[g];
-  if (threadIdx.x == 0) heavy = rows = 0;
+  if (A.which == kInHid)
+    for (uint32_t o = threadIdx.x; o < A.n_outputs; o += kLayoutThreads)
+      A.key[n0 + A.out_node[o]] |= 0x80000000u;
+  for (uint32_t i = threadIdx.x; i < kLayoutBins; i += kLayoutThreads) bin[i] = 0;
+  __threadfence_block();
   __syncthreads();
-  for (uint32_t i = wave; i < n; i += waves) {
-    const int64_t node = n0 + i;
-    const bool is_input = A.node_in[node] >= 0;
-    uint32_t d = 0;
-    if (by_in) {
-      if (!is_input)
-        for (int64_t e = A.in_offset[node]; e < A.in_offset[node + 1]; e += kWave) {
-          const int64_t k = e + lane;
-          const bool mine = k < A.in_offset[node + 1] && (A.node_in[A.in_src[k]] >= 0) == inputs;
-          d += (uint32_t)__popcll(__ballot(mine));
-        }
-    } else if (is_input == inputs) {
-      d = (uint32_t)(A.out_offset[node + 1] - A.out_offset[node]);
-    }
-    if (lane == 0) {
-      const bool in = by_in ? !is_input : is_input == inputs;
-      key[i] = in ? d : kAbsent;
-    }
+  auto bin_of = [](uint32_t k) {
+    return k & 0x80000000u ? kLayoutBins - 1u : (k < kLayoutBins - 2u ? k : kLayoutBins - 2u);
+  };
+  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
+    const uint32_t k = A.key[n0 + i];
+    if (k != kNoEdge) atomicAdd(&bin[bin_of(k)], 1u);
   }
   __syncthreads();
-  if (which == kInHid) {
-    for (uint32_t o = threadIdx.x; o < A.n_outputs; o += kLayoutThreads)
-      key[A.out_node[o]] |= 0x80000000u;
+  // ranks of the bins' first rows, from the last bin down
+  uint32_t rows = 0, nh = 0;
+  {
+    static_assert(kLayoutBins == 2 * kLayoutThreads, "two bins to a thread");
+    const uint32_t b = kLayoutBins - 1u - 2u * threadIdx.x;
+    const uint32_t c0 = bin[b], c1 = bin[b - 1];
+    const uint32_t at = block_scan(c0 + c1, part, &rows);
+    bin[b] = at;
+    bin[b - 1] = at + c0;
+    __syncthreads();
+    nh = bin[kLightEdges];  // (rows of more edges)
     __syncthreads();
   }
-  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
-    const uint32_t k = key[i];
-    if (k == kAbsent) continue;
-    uint32_t r = 0;
-    for (uint32_t j = 0; j < n; ++j) {
-      const uint32_t o = key[j];
-      r += o != kAbsent && (o > k || (o == k && j < i)) ? 1u : 0u;
+  const uint32_t ns = nh + (rows - nh + 15u) / 16u;
+  for (uint32_t i0 = 0; i0 < n; i0 += kLayoutThreads) {
+    const uint32_t i = i0 + threadIdx.x;
+    const uint32_t k = i < n ? A.key[n0 + i] : kNoEdge;
+    const uint32_t mine = k == kNoEdge ? kNoEdge : bin_of(k);
+    key[threadIdx.x] = mine;
+    __syncthreads();
+    uint32_t before = 0;
+    for (uint32_t j = 0; j < threadIdx.x; ++j) before += key[j] == mine ? 1u : 0u;
+    const uint32_t r = mine == kNoEdge ? kNoEdge : bin[mine] + before;
+    __syncthreads();
+    if (mine != kNoEdge) {
+      atomicAdd(&bin[mine], 1u);
+      if (r < nh) {
+        slices[r] = {0, padded(((k & 0x7FFFFFFFu) + 15u) / 16u), 0, 1};
+        for (uint32_t j = 0; j < 16; ++j) row_of[16u * r + j] = (uint16_t)i;
+      } else {
+        const uint32_t s = nh + (r - nh) / 16u;
+        if ((r - nh) % 16u == 0) slices[s] = {0, padded(k), 0, 0};
+        row_of[16u * s + (r - nh) % 16u] = (uint16_t)i;
+      }
     }
-    rank[i] = (uint16_t)r;
-    atomicAdd(&rows, 1u);
-    if (k > kLightEdges) atomicAdd(&heavy, 1u);
-  }
-  __syncthreads();
-  const uint32_t nh = heavy, ns = nh + (rows - nh + 15u) / 16u;
-  // the slices' lengths, then their bases
-  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
-    const uint32_t k = key[i];
-    if (k == kAbsent) continue;
-    const uint32_t r = rank[i];
-    if (r < nh) {
-      slices[r] = {0, padded(((k & 0x7FFFFFFFu) + 15u) / 16u), 0, 1};
-      for (uint32_t j = 0; j < 16; ++j) row_of[16u * r + j] = (uint16_t)i;
-    } else {
-      const uint32_t s = nh + (r - nh) / 16u;
-      if ((r - nh) % 16u == 0) slices[s] = {0, padded(k), 0, 0};
-      row_of[16u * s + (r - nh) % 16u] = (uint16_t)i;
-    }
+    if (i < n) A.row[n0 + i] = {0, (uint32_t)n0, r};
+    __syncthreads();
   }
   for (uint32_t r = rows + threadIdx.x; r < nh + 16u * (ns - nh); r += kLayoutThreads)
     row_of[16u * (nh + (r - nh) / 16u) + (r - nh) % 16u] = (uint16_t)kNoRow;
@@ -280,33 +293,46 @@ __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs
     base += total;
   }
   if (threadIdx.x == 0) {
-    places = base;
     S.n_slices[g] = ns;
+    S.n_heavy[g] = nh;
     S.n_places[g] = base;
   }
   __threadfence_block();
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < places; i += kLayoutThreads) {
+  for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
+    const uint32_t r = A.row[n0 + i].slice;
+    if (r == kNoEdge) continue;
+    const uint32_t s = r < nh ? r : nh + (r - nh) / 16u;
+    A.row[n0 + i] = {A.place[g] + slices[s].base + (r < nh ? 0u : (r - nh) % 16u), (uint32_t)n0,
+                     s | (r < nh ? 0x80000000u : 0u)};
+  }
+  uint2* ent = S.ent + A.place[g];
+  uint32_t* edge = S.edge + A.place[g];
+  for (uint32_t i = threadIdx.x; i < base; i += kLayoutThreads) {
     ent[i] = make_uint2(n, 0u);
     edge[i] = kNoEdge;
   }
-  __threadfence_block();
-  __syncthreads();
-  for (uint32_t i = wave; i < n; i += waves) {
-    if (key[i] == kAbsent) continue;
-    const int64_t node = n0 + i;
-    const uint32_t r = rank[i];
-    const bool is_heavy = r < nh;
-    const uint32_t s = is_heavy ? r : nh + (r - nh) / 16u;
-    const uint32_t b = slices[s].base + (is_heavy ? 0u : (r - nh) % 16u), step = is_heavy ? 1u : 16u;
-    const int64_t* off = by_in ? A.in_offset : A.out_offset;
+}
+
+// A wave for a node: its row's edges to their places. (blockIdx.y: the genome's number in the list.)
+__global__ void __launch_bounds__(kNetThreads) k_layout_fill(LearnLayoutArgs A) {
+  const uint32_t lane = threadIdx.x % kWave;
+  const bool by_in = by_destination(A.which), inputs = of_inputs(A.which);
+  const uint32_t g = A.genomes[blockIdx.y];
+  const int64_t end = A.node_offset[g + 1];
+  LearnSlice* slices = A.set.slices + A.slice[g];
+  const int64_t* off = by_in ? A.in_offset : A.out_offset;
+  for (int64_t i = A.node_offset[g] + grid_thread() / kWave; i < end; i += grid_threads() / kWave) {
+    const LearnRow R = A.row[i];
+    if (R.slice == kNoEdge) continue;
+    const bool heavy = R.slice >> 31;
+    const uint32_t step = heavy ? 1u : 16u;
     uint32_t done = 0, outs = 0;
-    for (int64_t e = off[node]; e < off[node + 1]; e += kWave) {
+    for (int64_t e = off[i]; e < off[i + 1]; e += kWave) {
       const int64_t k = e + lane;
-      const bool in = k < off[node + 1];
       uint32_t other = 0, id = 0;
-      bool mine = in;
-      if (in) {
+      bool mine = k < off[i + 1];
+      if (mine) {
         if (by_in) {
           other = A.in_src[k];
           id = (uint32_t)k;
@@ -316,18 +342,19 @@ __global__ void __launch_bounds__(kLayoutThreads) k_learn_layout(LearnLayoutArgs
           other = (uint32_t)(v >> 32);
           id = (uint32_t)v;
         }
-        other -= (uint32_t)n0;
+        other -= R.node0;
       }
       const uint64_t m = __ballot(mine);
       if (mine) {
-        const uint32_t at = b + step * (done + (uint32_t)__popcll(m & ((1ull << lane) - 1ull)));
-        ent[at] = make_uint2(other, __float_as_uint(A.in_w[id]));
-        edge[at] = id;
+        const int64_t at = R.place + (int64_t)step * (done + (uint32_t)__popcll(m & ((1ull << lane) - 1ull)));
+        A.set.ent[at] = make_uint2(other, __float_as_uint(A.in_w[id]));
+        A.set.edge[at] = id;
       }
       done += (uint32_t)__popcll(m);
       outs += (uint32_t)__popcll(__ballot(mine && other < A.n_sub));
     }
-    if (lane == 0 && outs > 0) atomicMax(&slices[s].first, is_heavy ? (outs + 15u) / 16u : outs);
+    if (lane == 0 && outs > 0)
+      atomicMax(&slices[R.slice & 0x7FFFFFFFu].first, heavy ? (outs + 15u) / 16u : outs);
   }
 }
 
@@ -343,7 +370,7 @@ __global__ void __launch_bounds__(kNetThreads) k_learn_weights(LearnWeightsArgs 
   }
 }
 
-// ----------------------------------------------------------------------------- a genome in LDS
+// ----------------------------------------------------------------------------- rows
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float v) {
@@ -351,7 +378,7 @@ __device__ __forceinline__ float dpp_add(float v) {
                  0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 constexpr int kDppXor2 = 0x4E, kDppXor1 = 0xB1;
-// The sum over a row's LN lanes (of four patterns each).
+// The sum over a row's LN lanes.
 template <int LN>
 __device__ __forceinline__ float row_sum(float v) {
   if constexpr (LN >= 2) v = dpp_add<kDppXor1>(v);
@@ -367,88 +394,114 @@ __device__ __forceinline__ void fma4(float4& a, float w, const float4& x) {
   a.z = fmaf(w, x.z, a.z);
   a.w = fmaf(w, x.w, a.w);
 }
-// The sum over the sixteen places of a heavy slice.
+
+// One of a genome's layouts.
+struct Rows {
+  const uint64_t* ent;
+  const LearnSlice* slices;
+  const uint16_t* rows;
+  uint32_t n, heavy;  // slices
+};
+__device__ __forceinline__ Rows rows_of(const LearnArgs& A, int which, uint32_t g) {
+  const LearnSet& S = A.set[which];
+  return {reinterpret_cast<const uint64_t*>(S.ent + A.place[g]), S.slices + A.slice[g],
+          S.rows + 16 * A.slice[g], S.n_slices[g], S.n_heavy[g]};
+}
+// A wave takes a heavy slice, or 4 / LN light ones, at a time: units of work.
 template <int LN>
-__device__ __forceinline__ void heavy_sum(float4& a) {
-#pragma unroll
-  for (int o = LN; o < 16 * LN; o <<= 1) {
-    a.x += __shfl_xor(a.x, o, kWave);
-    a.y += __shfl_xor(a.y, o, kWave);
-    a.z += __shfl_xor(a.z, o, kWave);
-    a.w += __shfl_xor(a.w, o, kWave);
-  }
+__device__ __forceinline__ uint32_t units_of(const Rows& R) {
+  return R.heavy + (R.n - R.heavy + 4u / LN - 1u) / (4u / LN);
 }
 
-// What a lane works on: group q of four patterns of the row at place r of a slice.
+// What a lane does of a unit: lane q of the LN of its row, edges off + step k, k < count.
 template <int LN>
 struct Place {
-  uint32_t q, r;
-  uint32_t base, len, full;  // of the slice; `full` past the first edges too
-  uint32_t most;             // the longest of the wave's slices
-  uint32_t row;              // kNoRow: none
-  bool heavy, any_heavy;
-  bool writes;               // the lane holds its row's sum
+  uint32_t q, off, step;
+  uint32_t count, most, full;  // the lane's edges, the most of the wave's lanes', those past the first too
+  uint32_t row;                // kNoRow: none
+  bool heavy;                  // (the wave's)
+  bool writes;                 // the lane holds its row's sum
 };
 // FIRST: only the edges that reach output nodes.
 template <int LN, bool FIRST>
-__device__ __forceinline__ Place<LN> place_of(const LearnSlice* slices, const uint16_t* rows, uint32_t at,
-                                              uint32_t ns, uint32_t lane) {
+__device__ __forceinline__ Place<LN> place_of(const Rows& R, uint32_t unit, uint32_t lane) {
   Place<LN> P;
   P.q = lane % LN;
-  P.r = lane / LN % 16u;
-  auto length = [](const LearnSlice& S) {
-    return FIRST ? (S.first + kLearnPad - 1u) / kLearnPad * kLearnPad : S.len;
-  };
-  if constexpr (LN == 4) {  // the wave's slice
-    const LearnSlice S = slices[at];
-    P.base = S.base;
-    P.len = P.most = length(S);
-    P.full = S.len;
-    P.heavy = P.any_heavy = S.heavy != 0;
-    P.row = rows[16u * at + P.r];
-  } else {
-    P.most = 0;
-    P.any_heavy = false;
-    for (uint32_t j = 0; j < 4u / LN; ++j) {
-      if (at + j >= ns) break;
-      const uint32_t l = length(slices[at + j]);
-      P.most = l > P.most ? l : P.most;
-      P.any_heavy |= slices[at + j].heavy != 0;
-    }
-    const uint32_t s = at + lane / (16u * LN);
-    const bool in = s < ns;
-    const LearnSlice S = slices[in ? s : at];
-    P.base = S.base;
-    P.len = in ? length(S) : 0u;
-    P.full = in ? S.len : 0u;
-    P.heavy = in && S.heavy != 0;
-    P.row = in ? rows[16u * s + P.r] : kNoRow;
+  P.heavy = unit < R.heavy;
+  if (P.heavy) {
+    constexpr uint32_t each = kWave / LN;  // edges at a time
+    const LearnSlice S = R.slices[unit];
+    P.off = S.base + lane / LN;
+    P.step = each;
+    P.full = 16u * S.len / each;
+    P.count = FIRST ? (16u * S.first + each - 1u) / each : P.full;
+    if (LN == 4) P.count = padded(P.count);
+    P.most = P.count;
+    P.row = R.rows[16u * unit];
+    P.writes = lane < (uint32_t)LN;
+    return P;
   }
-  P.writes = P.row != kNoRow && (!P.heavy || P.r == 0);
+  const uint32_t r = lane / LN % 16u;
+  P.step = 16;
+  if constexpr (LN == 4) {  // the wave's slice
+    const uint32_t s = unit;
+    const LearnSlice S = R.slices[s];
+    P.off = S.base + r;
+    P.full = S.len;
+    P.count = P.most = FIRST ? padded(S.first) : S.len;
+    P.row = R.rows[16u * s + r];
+  } else {
+    const uint32_t s0 = R.heavy + (unit - R.heavy) * (4u / LN);
+    P.most = 0;
+    for (uint32_t j = 0; j < 4u / LN && s0 + j < R.n; ++j) {
+      const uint32_t l = FIRST ? R.slices[s0 + j].first : R.slices[s0 + j].len;
+      P.most = l > P.most ? l : P.most;
+    }
+    const uint32_t s = s0 + lane / (16u * LN);
+    const bool in = s < R.n;
+    const LearnSlice S = R.slices[in ? s : s0];
+    P.off = S.base + r;
+    P.full = in ? S.len : 0u;
+    P.count = in ? (FIRST ? S.first : S.len) : 0u;
+    P.row = in ? R.rows[16u * s + r] : kNoRow;
+  }
+  P.writes = P.row != kNoRow;
   return P;
 }
 
-// Four edges from the k-th of a lane's row on; a wave whose slices differ in length takes empty ones past
-// its own slice's end (lengths are multiples of four).
+// Four of a lane's edges from the k-th on: with LN 4 all lanes of a wave have as many, a multiple of four;
+// else empty ones past a lane's own.
 template <int LN>
 __device__ __forceinline__ void edges_at(const uint64_t* __restrict__ e, uint32_t k, const Place<LN>& P,
                                          uint32_t n, uint64_t (&v)[kLearnPad]) {
-  if (LN == 4 || k < P.len) {
 #pragma unroll
-    for (uint32_t j = 0; j < kLearnPad; ++j) v[j] = e[16u * (k + j) + P.r];
-  } else {
-#pragma unroll
-    for (uint32_t j = 0; j < kLearnPad; ++j) v[j] = n;
+  for (uint32_t j = 0; j < kLearnPad; ++j) {
+    v[j] = n;
+    if (LN == 4 || k + j < P.count) v[j] = e[P.off + P.step * (k + j)];
   }
 }
 
-// The weighted sums of a slice's rows over x (the values of the genome's nodes, LN float4 each).
-template <int LN>
-__device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint2* __restrict__ ent,
-                                           const float4* x, uint32_t n) {
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+// The sum over the lanes of a heavy slice.
+template <int LN, int K>
+__device__ __forceinline__ void heavy_sum(float4 (&a)[K]) {
+#pragma unroll
+  for (int o = LN; o < kWave; o <<= 1)
+#pragma unroll
+    for (int g = 0; g < K; ++g) {
+      a[g].x += __shfl_xor(a[g].x, o, kWave);
+      a[g].y += __shfl_xor(a[g].y, o, kWave);
+      a[g].z += __shfl_xor(a[g].z, o, kWave);
+      a[g].w += __shfl_xor(a[g].w, o, kWave);
+    }
+}
+
+// The weighted sums of a unit's rows over x (the values of the genome's nodes, K groups of LN float4 each).
+template <int LN, int K>
+__device__ __forceinline__ void row_sums(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* x,
+                                         uint32_t n, float4 (&acc)[K]) {
+#pragma unroll
+  for (int g = 0; g < K; ++g) acc[g] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (P.most > 0) {
-    const uint64_t* e = reinterpret_cast<const uint64_t*>(ent) + P.base;
     uint64_t a[kLearnPad], b[kLearnPad];
     edges_at<LN>(e, 0, P, n, a);
     for (uint32_t k = kLearnPad;; k += kLearnPad) {
@@ -456,39 +509,37 @@ __device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint2* __re
       if (more) edges_at<LN>(e, k, P, n, b);
 #pragma unroll
       for (uint32_t j = 0; j < kLearnPad; ++j)
-        fma4(acc, __uint_as_float((uint32_t)(a[j] >> 32)), x[(uint32_t)a[j] * LN + P.q]);
+#pragma unroll
+        for (int g = 0; g < K; ++g)
+          fma4(acc[g], __uint_as_float((uint32_t)(a[j] >> 32)), x[(uint32_t)a[j] * (LN * K) + g * LN + P.q]);
       if (!more) break;
 #pragma unroll
       for (uint32_t j = 0; j < kLearnPad; ++j) a[j] = b[j];
     }
   }
-  if (P.any_heavy) {
-    float4 h = acc;
-    heavy_sum<LN>(h);
-    if (P.heavy) acc = h;
-  }
-  return acc;
+  if (P.heavy) heavy_sum<LN, K>(acc);
 }
 
 // The same for derivatives gz, and beside it the derivatives of the edges' weights, gz times the row's
 // own states s summed over the patterns, added to `sum` at the edges' places (set: stored there, the first
-// time; with FIRST, zeros at the places past those).
-template <int LN>
-__device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __restrict__ ent,
-                                            const float4* gz, uint32_t n, const float4& s,
-                                            float* __restrict__ sum, bool set) {
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+// time; with FIRST, zeros at the places past those). An edge's derivative, read once from LDS, serves both.
+template <int LN, int K>
+__device__ __forceinline__ void row_grads(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* gz,
+                                          uint32_t n, const float4 (&s)[K], float* __restrict__ sum, bool set,
+                                          float4 (&acc)[K]) {
+#pragma unroll
+  for (int g = 0; g < K; ++g) acc[g] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (P.most > 0) {
-    const uint64_t* e = reinterpret_cast<const uint64_t*>(ent) + P.base;
-    float* mine = sum + P.base;
     // each of a row's lanes adds the derivatives of one edge in LN
     constexpr int own = (int)kLearnPad / LN;
     uint64_t a[kLearnPad], b[kLearnPad];
     float had[own], next[own];
     auto sums_at = [&](uint32_t k, float (&v)[own]) {
 #pragma unroll
-      for (int c = 0; c < own; ++c)
-        v[c] = !set && (LN == 4 || k < P.len) ? mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] : 0.0f;
+      for (int c = 0; c < own; ++c) {
+        const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
+        v[c] = !set && (LN == 4 || kk < P.count) ? sum[P.off + P.step * kk] : 0.0f;
+      }
     };
     edges_at<LN>(e, 0, P, n, a);
     sums_at(0, had);
@@ -501,16 +552,22 @@ __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __r
       float d[kLearnPad];
 #pragma unroll
       for (uint32_t j = 0; j < kLearnPad; ++j) {
-        const float4 v = gz[(uint32_t)a[j] * LN + P.q];
-        fma4(acc, __uint_as_float((uint32_t)(a[j] >> 32)), v);
-        d[j] = row_sum<LN>(dot4(v, s));
+        float t = 0.0f;
+#pragma unroll
+        for (int g = 0; g < K; ++g) {
+          const float4 v = gz[(uint32_t)a[j] * (LN * K) + g * LN + P.q];
+          fma4(acc[g], __uint_as_float((uint32_t)(a[j] >> 32)), v);
+          t = g == 0 ? dot4(v, s[g]) : t + dot4(v, s[g]);
+        }
+        d[j] = row_sum<LN>(t);
       }
 #pragma unroll
       for (int c = 0; c < own; ++c) {
         float v = d[c * LN];
 #pragma unroll
         for (int j = 1; j < LN; ++j) v = P.q == (uint32_t)j ? d[c * LN + j] : v;
-        if (LN == 4 || k < P.len) mine[16u * (k + (uint32_t)(c * LN) + P.q) + P.r] = had[c] + v;
+        const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
+        if (LN == 4 || kk < P.count) sum[P.off + P.step * kk] = had[c] + v;
       }
       if (!more) break;
 #pragma unroll
@@ -520,23 +577,34 @@ __device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint2* __r
     }
   }
   if (set)
-    for (uint32_t k = P.len + P.q; k < P.full; k += LN) sum[P.base + 16u * k + P.r] = 0.0f;
-  if (P.any_heavy) {
-    float4 h = acc;
-    heavy_sum<LN>(h);
-    if (P.heavy) acc = h;
-  }
-  return acc;
+    for (uint32_t k = P.count + P.q; k < P.full; k += LN) sum[P.off + P.step * k] = 0.0f;
+  if (P.heavy) heavy_sum<LN, K>(acc);
 }
 
 __device__ __forceinline__ float sigmoid_f(float z) { return 1.0f / (1.0f + expf(-z)); }
+__device__ __forceinline__ float4 sigmoid4(const float4& z) {
+  return make_float4(sigmoid_f(z.x), sigmoid_f(z.y), sigmoid_f(z.z), sigmoid_f(z.w));
+}
+__device__ __forceinline__ float4 add4(const float4& a, const float4& b) {
+  return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
 __device__ __forceinline__ uint32_t code_of(float s) { return (uint32_t)__float2uint_rn(255.0f * s); }
+__device__ __forceinline__ uint32_t codes_of(const float4& s) {
+  return code_of(s.x) | code_of(s.y) << 8 | code_of(s.z) << 16 | code_of(s.w) << 24;
+}
+// d s (1 - s) for four codes.
+__device__ __forceinline__ float4 slopes(const float4& d, uint32_t c) {
+  return make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u), d.z * slope_of((c >> 16) & 255u),
+                     d.w * slope_of(c >> 24));
+}
 // The four codes of a node's state for pattern group pg.
 __device__ __forceinline__ uint32_t* kept_at(const NetKept& K, int64_t nodes, uint32_t plane, uint32_t pg,
                                              int64_t node) {
   return reinterpret_cast<uint32_t*>(
       K.codes + (((int64_t)plane * K.blocks + pg / K.q) * nodes + node) * (4 * K.q) + 4 * (pg % K.q));
 }
+// (a block's last groups may lie past the codes' blocks, whose patterns do not exist)
+__device__ __forceinline__ bool kept_in(const NetKept& K, uint32_t pg) { return pg < K.blocks * K.q; }
 __device__ __forceinline__ float4 pattern4(const LearnArgs& A, int32_t slot, uint32_t pg) {
   float c[4];
 #pragma unroll
@@ -546,220 +614,274 @@ __device__ __forceinline__ float4 pattern4(const LearnArgs& A, int32_t slot, uin
   }
   return make_float4(c[0], c[1], c[2], c[3]);
 }
+// A block's patterns at the input nodes, 0 elsewhere and past the last node; the input nodes' codes.
+template <int W>
+__device__ __forceinline__ void fill_patterns(const LearnArgs& A, int64_t n0, uint32_t n, uint32_t block,
+                                              bool codes, float4* x) {
+  for (uint32_t i = threadIdx.x; i < (n + 1u) * W; i += blockDim.x) {
+    const uint32_t node = i / W, pg = block * W + i % W;
+    const int32_t slot = node < n ? A.node_in[n0 + node] : -1;
+    x[i] = slot >= 0 ? pattern4(A, slot, pg) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (codes && slot >= 0 && kept_in(A.kept, pg))
+      for (uint32_t t = 0; t < A.kept.planes; ++t) *kept_at(A.kept, A.nodes, t, pg, n0 + node) = 0;
+  }
+}
+// A block's derivatives by the output nodes' sums in the last step, over zeros. (Every thread of the
+// workgroup; a barrier before their use is the caller's.)
+template <int W>
+__device__ __forceinline__ void fill_outputs(const LearnArgs& A, uint32_t g, uint32_t n, uint32_t block,
+                                             float4* x) {
+  for (uint32_t i = threadIdx.x; i < (n + 1u) * W; i += blockDim.x) x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  __syncthreads();
+  const uint32_t p0 = block * 4u * W, np = min(A.n_patterns - p0, 4u * W);
+  for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
+    const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+    const int64_t r = ((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o;
+    const float v = A.outputs[r];
+    reinterpret_cast<float*>(x)[(uint32_t)A.out_node[o] * 4u * W + p] = A.grad_outputs[r] * v * (1.0f - v);
+  }
+}
+// A unit's rows of input nodes: their edges' derivatives, and their patterns'.
+template <int LN, int K>
+__device__ __forceinline__ void input_rows(const LearnArgs& A, const Rows& R, uint32_t unit, uint32_t g,
+                                           int64_t n0, uint32_t n, uint32_t block, const float4* gz, float* sum,
+                                           bool set) {
+  const Place<LN> P = place_of<LN, false>(R, unit, threadIdx.x % kWave);
+  const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
+  float4 x[K], d[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    x[k] = slot >= 0 ? pattern4(A, slot, block * (LN * K) + k * LN + P.q) : make_float4(0.f, 0.f, 0.f, 0.f);
+  row_grads<LN, K>(P, R.ent, gz, n, x, sum, set, d);
+  if (!A.grad_inputs || !P.writes) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const float v[4] = {d[k].x, d[k].y, d[k].z, d[k].w};
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint32_t p = 4u * (block * (LN * K) + k * LN + P.q) + j;
+      if (p < A.n_patterns)
+        A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[j];
+    }
+  }
+}
 
-// All steps of one genome for an item's blocks of 4 LN patterns: states in LDS as two halves that the steps
-// swap and the sums of the input edges, which no step changes. A wave holds a slice of sixteen rows with
-// LN lanes each (or 4 / LN slices).
-template <int LN>
+// ----------------------------------------------------------------------------- all steps of a genome
+
+// The values after a step become those before the next.
+template <int W, bool LOCAL>
+__device__ __forceinline__ void advance(float4*& cur, float4*& nxt, uint32_t n) {
+  if constexpr (LOCAL) {
+    __syncthreads();
+    float4* x = cur;
+    cur = nxt;
+    nxt = x;
+  } else {
+    __threadfence_block();
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n * W; i += blockDim.x) cur[i] = nxt[i];
+    __syncthreads();
+  }
+}
+
+// All steps of one genome for an item's blocks of 4 LN K patterns.
+template <int LN, int K, bool LOCAL>
 __device__ __forceinline__ void keep_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
+  constexpr int W = LN * K;
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, K, LOCAL}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  constexpr uint32_t per = 4 / LN;
-  const LearnSet &H = A.set[kInHid], &E = A.set[kInInp];
-  const uint2 *he = H.ent + A.place[g], *ie = E.ent + A.place[g];
-  const LearnSlice *hs = H.slices + A.slice[g], *is = E.slices + A.slice[g];
-  const uint16_t *hr = H.rows + 16 * A.slice[g], *ir = E.rows + 16 * A.slice[g];
-  const uint32_t hn = H.n_slices[g], in = E.n_slices[g];
-  float4 *cur = lds, *nxt = lds + (n + 1u) * LN, *held = nxt + (n + 1u) * LN;
+  const Rows H = rows_of(A, kInHid, g), E = rows_of(A, kInInp, g);
+  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * W : A.values + I.values, *held = nxt + (n + 1u) * W;
+  if (LOCAL)
+    for (uint32_t i = threadIdx.x; i < W; i += blockDim.x) nxt[n * W + i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (uint32_t b = I.b0; b < I.b1; ++b) {
-    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) {
-      const uint32_t node = i / LN;
-      const int32_t slot = node < n ? A.node_in[n0 + node] : -1;
-      const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-      cur[i] = slot >= 0 ? pattern4(A, slot, b * LN + i % LN) : z;
-      nxt[i] = z;
-      held[i] = z;
-      if (slot >= 0)
-        for (uint32_t t = 0; t < A.kept.planes; ++t)
-          *kept_at(A.kept, A.nodes, t, b * LN + i % LN, n0 + node) = 0;
-    }
+    fill_patterns<W>(A, n0, n, b, true, cur);
     __syncthreads();
-    for (uint32_t at = wave * per; at < in; at += waves * per) {
-      const Place<LN> P = place_of<LN, false>(is, ir, at, in, lane);
-      const float4 z = row_sums<LN>(P, ie, cur, n);
-      if (P.writes) held[P.row * LN + P.q] = z;
-    }
-    __syncthreads();
-    for (uint32_t step = 1; step <= A.steps; ++step) {
-      // the last step: output nodes alone, the first slices
-      const uint32_t end = step == A.steps ? A.n_outputs : hn;
-      for (uint32_t at = wave * per; at < end; at += waves * per) {
-        Place<LN> P = place_of<LN, false>(hs, hr, at, end, lane);
-        if (step == 1) P.most = 0;  // (hidden states are 0: their edges add nothing)
-        float4 z = row_sums<LN>(P, he, cur, n);
-        if (!P.writes) continue;
-        const float4 y = held[P.row * LN + P.q];
-        const float4 s = make_float4(sigmoid_f(z.x + y.x), sigmoid_f(z.y + y.y), sigmoid_f(z.z + y.z),
-                                     sigmoid_f(z.w + y.w));
-        nxt[P.row * LN + P.q] = s;
-        if (step < A.steps)
-          *kept_at(A.kept, A.nodes, step - 1, b * LN + P.q, n0 + P.row) =
-              code_of(s.x) | code_of(s.y) << 8 | code_of(s.z) << 16 | code_of(s.w) << 24;
+    auto put = [&](uint32_t row, uint32_t q, uint32_t step, const float4 (&z)[K]) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t i = row * W + k * LN + q, pg = b * W + k * LN + q;
+        const float4 s = sigmoid4(z[k]);
+        nxt[i] = s;
+        if (step < A.steps && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, step - 1, pg, n0 + row) = codes_of(s);
       }
-      __syncthreads();
-      float4* x = cur;
-      cur = nxt;
-      nxt = x;
+    };
+    // the first step: the inputs' edges alone, whose sums stay (hidden states are 0)
+    if (A.steps > 0)
+      for (uint32_t u = wave; u < units_of<LN>(E); u += waves) {
+        const Place<LN> P = place_of<LN, false>(E, u, lane);
+        float4 z[K];
+        row_sums<LN, K>(P, E.ent, cur, n, z);
+        if (!P.writes) continue;
+#pragma unroll
+        for (int k = 0; k < K; ++k) held[P.row * W + k * LN + P.q] = z[k];
+        put(P.row, P.q, 1, z);
+      }
+    for (uint32_t step = 2; step <= A.steps; ++step) {
+      advance<W, LOCAL>(cur, nxt, n);
+      // the last step: output nodes alone, the first units
+      const uint32_t end = step == A.steps ? A.n_outputs : units_of<LN>(H);
+      for (uint32_t u = wave; u < end; u += waves) {
+        const Place<LN> P = place_of<LN, false>(H, u, lane);
+        float4 z[K];
+        row_sums<LN, K>(P, H.ent, cur, n, z);
+        if (!P.writes) continue;
+#pragma unroll
+        for (int k = 0; k < K; ++k) z[k] = add4(z[k], held[P.row * W + k * LN + P.q]);
+        put(P.row, P.q, step, z);
+      }
     }
-    const float* c = reinterpret_cast<const float*>(cur);
-    const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
+    __threadfence_block();
+    __syncthreads();
+    const float* c = reinterpret_cast<const float*>(nxt);
+    const uint32_t p0 = b * 4u * W, np = min(A.n_patterns - p0, 4u * W);
     for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
       const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
       A.outputs[((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o] =
-          c[(uint32_t)A.out_node[o] * 4u * LN + p];
+          A.steps > 0 ? c[(uint32_t)A.out_node[o] * 4u * W + p] : 0.0f;
     }
     __syncthreads();
   }
 }
 
-template <int LN>
+template <int LN, int K, bool LOCAL>
 __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
+  constexpr int W = LN * K;
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, K, LOCAL}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  constexpr uint32_t per = 4 / LN;
-  const LearnSet &H = A.set[kOutHid], &E = A.set[kOutInp];
-  const uint2 *he = H.ent + A.place[g], *ie = E.ent + A.place[g];
-  const LearnSlice *hs = H.slices + A.slice[g], *is = E.slices + A.slice[g];
-  const uint16_t *hr = H.rows + 16 * A.slice[g], *ir = E.rows + 16 * A.slice[g];
-  const uint32_t hn = H.n_slices[g], in = E.n_slices[g], hp = H.n_places[g], ip = E.n_places[g];
+  const Rows H = rows_of(A, kOutHid, g), E = rows_of(A, kOutInp, g);
+  const uint32_t hp = A.set[kOutHid].n_places[g], ip = A.set[kOutInp].n_places[g];
   float *hsum = A.partial + I.part, *isum = hsum + hp;
-  float4 *cur = lds, *nxt = lds + (n + 1u) * LN, *all = nxt + (n + 1u) * LN;
+  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * W : A.values + I.values, *all = nxt + (n + 1u) * W;
+  if (LOCAL)
+    for (uint32_t i = threadIdx.x; i < W; i += blockDim.x)
+      nxt[n * W + i] = all[n * W + i] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (A.steps < 2)  // (no step of theirs)
     for (uint32_t i = threadIdx.x; i < hp; i += blockDim.x) hsum[i] = 0.0f;
   for (uint32_t b = I.b0; b < I.b1; ++b) {
-    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) cur[i] = nxt[i] = all[i] = zero;
-    __syncthreads();
-    const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
-    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
-      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
-      const int64_t r = ((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o;
-      const float v = A.outputs[r], d = A.grad_outputs[r] * v * (1.0f - v);
-      const uint32_t at = (uint32_t)A.out_node[o] * 4u * LN + p;
-      reinterpret_cast<float*>(cur)[at] = d;
-      reinterpret_cast<float*>(all)[at] = d;
-    }
+    fill_outputs<W>(A, g, n, b, cur);
     __syncthreads();
     for (uint32_t step = A.steps; step >= 2; --step) {
       const bool last = step == A.steps;  // derivatives at the output nodes alone
-      for (uint32_t at = wave * per; at < hn; at += waves * per) {
-        const Place<LN> P = last ? place_of<LN, true>(hs, hr, at, hn, lane)
-                                 : place_of<LN, false>(hs, hr, at, hn, lane);
-        const uint32_t c =
-            P.row != kNoRow ? *kept_at(A.kept, A.nodes, step - 2, b * LN + P.q, n0 + P.row) : 0u;
-        const float4 d = row_grads<LN>(P, he, cur, n, states(c), hsum, last && b == I.b0);
-        if (!P.writes) continue;
-        const float4 v = make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
-                                     d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
-        const uint32_t i = P.row * LN + P.q;
-        nxt[i] = v;
-        const float4 a = all[i];
-        all[i] = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
-      }
-      __syncthreads();
-      float4* x = cur;
-      cur = nxt;
-      nxt = x;
-    }
-    for (uint32_t at = wave * per; at < in; at += waves * per) {
-      const Place<LN> P = place_of<LN, false>(is, ir, at, in, lane);
-      const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
-      const float4 x = slot >= 0 ? pattern4(A, slot, b * LN + P.q) : zero;
-      const float4 d = row_grads<LN>(P, ie, all, n, x, isum, b == I.b0);
-      if (!A.grad_inputs || !P.writes) continue;
-      const float v[4] = {d.x, d.y, d.z, d.w};
+      for (uint32_t u = wave; u < units_of<LN>(H); u += waves) {
+        const Place<LN> P = last ? place_of<LN, true>(H, u, lane) : place_of<LN, false>(H, u, lane);
+        uint32_t c[K];
+        float4 s[K], d[K];
 #pragma unroll
-      for (uint32_t k = 0; k < 4; ++k) {
-        const uint32_t p = p0 + 4u * P.q + k;
-        if (p < A.n_patterns)
-          A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[k];
+        for (int k = 0; k < K; ++k) {
+          const uint32_t pg = b * W + k * LN + P.q;
+          c[k] = P.row != kNoRow && kept_in(A.kept, pg)
+                     ? *kept_at(A.kept, A.nodes, step - 2, pg, n0 + P.row) : 0u;
+          s[k] = states(c[k]);
+        }
+        row_grads<LN, K>(P, H.ent, cur, n, s, hsum, last && b == I.b0, d);
+        if (!P.writes) continue;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const uint32_t i = P.row * W + k * LN + P.q;
+          const float4 v = slopes(d[k], c[k]);
+          nxt[i] = v;
+          all[i] = add4(last ? cur[i] : all[i], v);
+        }
       }
+      advance<W, LOCAL>(cur, nxt, n);
     }
+    const float4* sum_gz = A.steps < 2 ? cur : all;
+    if (!LOCAL && A.steps >= 2) {
+      for (uint32_t i = threadIdx.x; i < n * W; i += blockDim.x) cur[i] = all[i];
+      __syncthreads();
+      sum_gz = cur;
+    }
+    for (uint32_t u = wave; u < units_of<LN>(E); u += waves)
+      input_rows<LN, K>(A, E, u, g, n0, n, b, sum_gz, isum, b == I.b0);
     __syncthreads();
   }
   if (!I.alone) return;
   __threadfence_block();
   __syncthreads();
-  const uint32_t *hi = H.edge + A.place[g], *ii = E.edge + A.place[g];
+  const uint32_t *hi = A.set[kOutHid].edge + A.place[g], *ii = A.set[kOutInp].edge + A.place[g];
   for (uint32_t i = threadIdx.x; i < hp; i += blockDim.x)
     if (hi[i] != kNoEdge) A.grad_w[hi[i]] = hsum[i];
   for (uint32_t i = threadIdx.x; i < ip; i += blockDim.x)
     if (ii[i] != kNoEdge) A.grad_w[ii[i]] = isum[i];
 }
 
-template <bool BACK>
+template <bool BACK, int LN, int K, bool LOCAL>
 __global__ void __launch_bounds__(1024, 4) k_learn(LearnArgs A) {
   extern __shared__ float4 learn_lds_mem[];
   const LearnItem I = A.items[A.first_item + blockIdx.x];
-  switch (I.groups) {
-    case 1: BACK ? back_item<1>(A, I, learn_lds_mem) : keep_item<1>(A, I, learn_lds_mem); break;
-    case 2: BACK ? back_item<2>(A, I, learn_lds_mem) : keep_item<2>(A, I, learn_lds_mem); break;
-    default: BACK ? back_item<4>(A, I, learn_lds_mem) : keep_item<4>(A, I, learn_lds_mem); break;
-  }
+  if constexpr (BACK) back_item<LN, K, LOCAL>(A, I, learn_lds_mem);
+  else keep_item<LN, K, LOCAL>(A, I, learn_lds_mem);
 }
 
+template <bool BACK>
+hipError_t launch_learn(const LearnArgs& A, hipStream_t s) {
+  const dim3 grid(A.n_items), blk(A.threads);
+  static_assert(sizeof kLearnShapes / sizeof kLearnShapes[0] == 8, "a case for each shape");
+#define EMR_LEARN_CASE(i)                                                                                   \
+  case i:                                                                                                   \
+    hipLaunchKernelGGL((k_learn<BACK, (int)kLearnShapes[i].lanes, (int)kLearnShapes[i].groups,             \
+                                kLearnShapes[i].local != 0>),                                               \
+                       grid, blk, A.lds_bytes, s, A);                                                       \
+    break;
+  switch (A.shape) {
+    EMR_LEARN_CASE(0)
+    EMR_LEARN_CASE(1)
+    EMR_LEARN_CASE(2)
+    EMR_LEARN_CASE(3)
+    EMR_LEARN_CASE(4)
+    EMR_LEARN_CASE(5)
+    EMR_LEARN_CASE(6)
+    EMR_LEARN_CASE(7)
+    default: return hipErrorInvalidValue;
+  }
+#undef EMR_LEARN_CASE
+  return hipSuccess;
+}
+
+// ----------------------------------------------------------------------------- a step of a genome
+
 // One step of genomes too large for that, or too few to fill the chip: a workgroup holds all nodes' values of a
-// block of patterns and takes a share of the slices.
+// block of patterns and takes a share of the units.
 template <int LN>
 __device__ __forceinline__ void keep_step(const LearnArgs& A, const LearnStepItem& I, float4* lds) {
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (step_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, 1, 0}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  constexpr uint32_t per = 4 / LN;
   const bool first = A.step == 1, last = A.step == A.steps;
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   const float4* cur = A.cur + I.values;
   float4 *nxt = A.nxt + I.values, *held = A.held + I.values;
-  const LearnSet& E = A.set[first ? kInInp : kInHid];
-  const uint2* ent = E.ent + A.place[g];
-  const LearnSlice* slices = E.slices + A.slice[g];
-  const uint16_t* rows = E.rows + 16 * A.slice[g];
-  for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x) {
-    const uint32_t node = i / LN;
-    float4 v = zero;
-    if (first) {  // the patterns; and what nodes without input edges hold
-      const int32_t slot = node < n ? A.node_in[n0 + node] : -1;
-      if (slot >= 0) v = pattern4(A, slot, I.block * LN + i % LN);
-      if (I.chunk == 0 && slot >= 0)
-        for (uint32_t t = 0; t < A.kept.planes; ++t)
-          *kept_at(A.kept, A.nodes, t, I.block * LN + i % LN, n0 + node) = 0;
-    } else if (node < n) {
-      v = cur[i];
-    }
-    lds[i] = v;
+  const Rows R = rows_of(A, first ? kInInp : kInHid, g);
+  if (first) {
+    fill_patterns<LN>(A, n0, n, I.block, I.chunk == 0, lds);
+  } else {
+    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
+      lds[i] = i < n * LN ? cur[i] : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __syncthreads();
-  auto put = [&](uint32_t row, uint32_t q, const float4& z) {
-    const float4 s = make_float4(sigmoid_f(z.x), sigmoid_f(z.y), sigmoid_f(z.z), sigmoid_f(z.w));
-    nxt[row * LN + q] = s;
-    if (!last)
-      *kept_at(A.kept, A.nodes, A.step - 1, I.block * LN + q, n0 + row) =
-          code_of(s.x) | code_of(s.y) << 8 | code_of(s.z) << 16 | code_of(s.w) << 24;
-  };
-  const uint32_t end = first ? E.n_slices[g] : (last ? A.n_outputs : E.n_slices[g]);
-  for (uint32_t at = (wave * I.chunks + I.chunk) * per; at < end; at += waves * I.chunks * per) {
-    const Place<LN> P = place_of<LN, false>(slices, rows, at, end, lane);
-    const float4 z = row_sums<LN>(P, ent, lds, n);
+  const uint32_t end = last && !first ? A.n_outputs : units_of<LN>(R);
+  for (uint32_t u = wave * I.chunks + I.chunk; u < end; u += waves * I.chunks) {
+    const Place<LN> P = place_of<LN, false>(R, u, lane);
+    float4 z[1];
+    row_sums<LN, 1>(P, R.ent, lds, n, z);
     if (!P.writes) continue;
-    const uint32_t i = P.row * LN + P.q;
-    if (first) {
-      held[i] = z;
-      put(P.row, P.q, z);
-    } else {
-      const float4 y = held[i];
-      put(P.row, P.q, make_float4(z.x + y.x, z.y + y.y, z.z + y.z, z.w + y.w));
-    }
+    const uint32_t i = P.row * LN + P.q, pg = I.block * LN + P.q;
+    if (first) held[i] = z[0];
+    else z[0] = add4(z[0], held[i]);
+    const float4 s = sigmoid4(z[0]);
+    nxt[i] = s;
+    if (!last && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, A.step - 1, pg, n0 + P.row) = codes_of(s);
   }
 }
 
@@ -768,63 +890,43 @@ __device__ __forceinline__ void back_step(const LearnArgs& A, const LearnStepIte
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (step_lds(n, LN) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, 1, 0}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-  constexpr uint32_t per = 4 / LN;
   const bool inputs = A.step == 1, last = A.step == A.steps;
-  const LearnSet &H = A.set[kOutHid], &E = A.set[inputs ? kOutInp : kOutHid];
-  const uint2* ent = E.ent + A.place[g];
-  const LearnSlice* slices = E.slices + A.slice[g];
-  const uint16_t* rows = E.rows + 16 * A.slice[g];
-  float* sum = A.partial + I.part + (inputs ? H.n_places[g] : 0u);
+  const uint32_t hp = A.set[kOutHid].n_places[g];
+  const Rows R = rows_of(A, inputs ? kOutInp : kOutHid, g);
+  float* sum = A.partial + I.part + (inputs ? hp : 0u);
   const float4* from = (inputs ? A.held : A.cur) + I.values;
   float4 *nxt = A.nxt + I.values, *all = A.held + I.values;
-  const uint32_t p0 = I.block * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
   // the derivatives after the step (of all steps); those after the last are at the output nodes alone
-  for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
-    lds[i] = last || i >= n * LN ? make_float4(0.f, 0.f, 0.f, 0.f) : from[i];
-  __syncthreads();
   if (last) {
-    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
-      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
-      const int64_t r = ((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o;
-      const float v = A.outputs[r];
-      reinterpret_cast<float*>(lds)[(uint32_t)A.out_node[o] * 4u * LN + p] = A.grad_outputs[r] * v * (1.0f - v);
-    }
-    __syncthreads();
+    fill_outputs<LN>(A, g, n, I.block, lds);
+  } else {
+    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
+      lds[i] = i < n * LN ? from[i] : make_float4(0.f, 0.f, 0.f, 0.f);
   }
+  __syncthreads();
   if (inputs && last)  // (one step: the other edges have no part)
-    for (uint32_t i = I.chunk * blockDim.x + threadIdx.x; i < H.n_places[g]; i += I.chunks * blockDim.x)
+    for (uint32_t i = I.chunk * blockDim.x + threadIdx.x; i < hp; i += I.chunks * blockDim.x)
       A.partial[I.part + i] = 0.0f;
-  const uint32_t end = E.n_slices[g];
-  for (uint32_t at = (wave * I.chunks + I.chunk) * per; at < end; at += waves * I.chunks * per) {
-    const Place<LN> P = last && !inputs ? place_of<LN, true>(slices, rows, at, end, lane)
-                                        : place_of<LN, false>(slices, rows, at, end, lane);
+  for (uint32_t u = wave * I.chunks + I.chunk; u < units_of<LN>(R); u += waves * I.chunks) {
     if (inputs) {
-      const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
-      const float4 x = slot >= 0 ? pattern4(A, slot, I.block * LN + P.q) : make_float4(0.f, 0.f, 0.f, 0.f);
-      const float4 d = row_grads<LN>(P, ent, lds, n, x, sum, true);
-      if (!A.grad_inputs || !P.writes) continue;
-      const float v[4] = {d.x, d.y, d.z, d.w};
-#pragma unroll
-      for (uint32_t k = 0; k < 4; ++k) {
-        const uint32_t p = p0 + 4u * P.q + k;
-        if (p < A.n_patterns)
-          A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[k];
-      }
+      input_rows<LN, 1>(A, R, u, g, n0, n, I.block, lds, sum, true);
       continue;
     }
-    const uint32_t c =
-        P.row != kNoRow ? *kept_at(A.kept, A.nodes, A.step - 2, I.block * LN + P.q, n0 + P.row) : 0u;
-    const float4 d = row_grads<LN>(P, ent, lds, n, states(c), sum, last);
+    const Place<LN> P = last ? place_of<LN, true>(R, u, lane) : place_of<LN, false>(R, u, lane);
+    const uint32_t pg = I.block * LN + P.q;
+    const uint32_t c = P.row != kNoRow && kept_in(A.kept, pg)
+                           ? *kept_at(A.kept, A.nodes, A.step - 2, pg, n0 + P.row) : 0u;
+    const float4 s[1] = {states(c)};
+    float4 d[1];
+    row_grads<LN, 1>(P, R.ent, lds, n, s, sum, last, d);
     if (!P.writes) continue;
-    const float4 v = make_float4(d.x * slope_of(c & 255u), d.y * slope_of((c >> 8) & 255u),
-                                 d.z * slope_of((c >> 16) & 255u), d.w * slope_of(c >> 24));
     const uint32_t i = P.row * LN + P.q;
+    const float4 v = slopes(d[0], c);
     nxt[i] = v;
-    const float4 a = last ? lds[i] : all[i];
-    all[i] = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
+    all[i] = add4(last ? lds[i] : all[i], v);
   }
 }
 
@@ -832,7 +934,7 @@ template <bool BACK>
 __global__ void __launch_bounds__(1024, 4) k_learn_step(LearnArgs A) {
   extern __shared__ float4 learn_lds_mem[];
   const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
-  switch (I.groups) {
+  switch (I.lanes) {
     case 1: BACK ? back_step<1>(A, I, learn_lds_mem) : keep_step<1>(A, I, learn_lds_mem); break;
     case 2: BACK ? back_step<2>(A, I, learn_lds_mem) : keep_step<2>(A, I, learn_lds_mem); break;
     default: BACK ? back_step<4>(A, I, learn_lds_mem) : keep_step<4>(A, I, learn_lds_mem); break;
@@ -844,7 +946,7 @@ __global__ void __launch_bounds__(kNetThreads) k_step_outputs(LearnArgs A) {
   const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
   if (I.chunk != 0) return;
   const float* v = reinterpret_cast<const float*>(A.cur + I.values);
-  const uint32_t wide = 4u * I.groups, p0 = I.block * wide, np = min(A.n_patterns - p0, wide);
+  const uint32_t wide = 4u * I.lanes, p0 = I.block * wide, np = min(A.n_patterns - p0, wide);
   for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += kNetThreads) {
     const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
     A.outputs[((int64_t)I.genome * A.n_patterns + p0 + p) * A.n_outputs + o] =
@@ -906,7 +1008,16 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
     case 2: {
       const auto& A = *static_cast<const LearnLayoutArgs*>(args);
       if (A.count == 0) return hipSuccess;
-      hipLaunchKernelGGL(k_learn_layout, dim3(A.count, kSets), dim3(kLayoutThreads), 0, s, A);
+      hipLaunchKernelGGL(k_layout_degrees, dim3(stride_blocks(A.nodes * kWave)), blk, 0, s, A);
+      hipLaunchKernelGGL(k_layout_slices, dim3(A.count), dim3(kLayoutThreads), 0, s, A);
+      // (about 4096 workgroups over the genomes, a wave to a node)
+      const uint32_t x = A.count < 4096u ? 4096u / A.count : 1u;
+      for (uint32_t a = 0; a < A.count; a += 65535u) {
+        LearnLayoutArgs B = A;
+        B.genomes = A.genomes + a;
+        hipLaunchKernelGGL(k_layout_fill, dim3(x < 512u ? x : 512u, A.count - a < 65535u ? A.count - a : 65535u),
+                           blk, 0, s, B);
+      }
       break;
     }
     case 3: {
@@ -925,10 +1036,8 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       if (A.n_items == 0) return hipSuccess;
       if (A.lds_bytes > kLearnLds || A.threads == 0 || A.threads > 1024u || A.threads % kWave != 0)
         return hipErrorInvalidValue;
-      if (step == 4)
-        hipLaunchKernelGGL(k_learn<false>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
-      else
-        hipLaunchKernelGGL(k_learn<true>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      const hipError_t e = step == 4 ? launch_learn<false>(A, s) : launch_learn<true>(A, s);
+      if (e != hipSuccess) return e;
       break;
     }
     case 6: {

@@ -299,11 +299,11 @@ struct emr_networks {
   // number of patterns; partial sums, and a larger genome's derivatives
   struct Learning {
     bool laid = false;
-    Dev ent[emr::kSets], edge[emr::kSets], slices[emr::kSets], rows[emr::kSets], n_slices, n_places;
+    Dev ent[emr::kSets], edge[emr::kSets], slices[emr::kSets], rows[emr::kSets], n_slices, n_heavy, n_places;
     Dev place, slice, fits, large, edge_dst, out_offset, out_edge;
     std::vector<uint32_t> fit, big;
     struct Run {
-      uint32_t first, count, threads, lds;
+      uint32_t first, count, threads, lds, shape;
     };
     struct Plan {
       int32_t patterns = 0;
@@ -312,6 +312,7 @@ struct emr_networks {
       std::vector<Run> runs;
       Run steps{};                // the stepped genomes' launches
       int64_t values = 0;         // float4 of each of their three arrays
+      int64_t scratch = 0;        // float4 of the items' values outside LDS
       int64_t partial_floats = 0;
     };
     std::vector<std::unique_ptr<Plan>> plans;  // by number of patterns, the oldest first
@@ -319,7 +320,7 @@ struct emr_networks {
     void release_idle() {
       for (int k = 0; k < emr::kSets; ++k)
         for (Dev* d : {&ent[k], &edge[k], &slices[k], &rows[k]}) d->reset_idle();
-      for (Dev* d : {&n_slices, &n_places, &place, &slice, &fits, &large, &edge_dst, &out_offset, &out_edge,
+      for (Dev* d : {&n_slices, &n_heavy, &n_places, &place, &slice, &fits, &large, &edge_dst, &out_offset, &out_edge,
                      &partial, &back, &values})
         d->reset_idle();
       for (auto& p : plans) {
@@ -1076,6 +1077,7 @@ void learn_sets(emr_networks& N, emr::LearnSet* out) {
   for (int k = 0; k < emr::kSets; ++k)
     out[k] = {L.ent[k].as<uint2>(), L.edge[k].as<uint32_t>(), L.slices[k].as<emr::LearnSlice>(),
               L.rows[k].as<uint16_t>(), L.n_slices.as<uint32_t>() + (size_t)k * N.n_genomes,
+              L.n_heavy.as<uint32_t>() + (size_t)k * N.n_genomes,
               L.n_places.as<uint32_t>() + (size_t)k * N.n_genomes};
 }
 
@@ -1094,7 +1096,7 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
       const int64_t n = N.node_off[g + 1] - N.node_off[g], e = N.edge_off[g + 1] - N.edge_off[g];
       place[g] = places;
       slice[g] = slices;
-      if (n > (int64_t)emr::kStepNodes || emr::learn_places(n, e, N.n_out) > INT32_MAX) {
+      if (n > (int64_t)emr::kLearnNodes || emr::learn_places(n, e, N.n_out) > INT32_MAX) {
         L.big.push_back(g);
         continue;
       }
@@ -1125,7 +1127,11 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
     }
     NET_HIP(emr_launch_net(21, &a, s));
     NET_TRY(alloc(L.n_slices, emr::kSets * G * 4, "slice counts", s));
+    NET_TRY(alloc(L.n_heavy, emr::kSets * G * 4, "slice counts", s));
     NET_TRY(alloc(L.n_places, emr::kSets * G * 4, "place counts", s));
+    Dev degrees, row;
+    NET_TRY(alloc(degrees, (size_t)N.nodes * 4, "row lengths", s));
+    NET_TRY(alloc(row, (size_t)N.nodes * sizeof(emr::LearnRow), "row places", s));
     for (int k = 0; k < emr::kSets; ++k) {
       NET_TRY(alloc(L.ent[k], (size_t)places * 8, "laid out edges", s));
       NET_TRY(alloc(L.edge[k], (size_t)places * 4, "laid out edge numbers", s));
@@ -1139,8 +1145,12 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
       NET_TRY(alloc(*u.d, u.bytes, "learning tables", s));
       NET_TRY(to_device(u.d->p, u.src, u.bytes, s));
     }
+    emr::LearnSet sets[emr::kSets];
+    learn_sets(N, sets);
     emr::LearnLayoutArgs la{};
-    learn_sets(N, la.set);
+    la.key = degrees.as<uint32_t>();
+    la.row = row.as<emr::LearnRow>();
+    la.nodes = N.nodes;
     la.genomes = L.fits.as<uint32_t>();
     la.place = L.place.as<int64_t>();
     la.slice = L.slice.as<int64_t>();
@@ -1155,7 +1165,10 @@ emr_status lay_out(emr_networks& N, hipStream_t s) {
     la.count = (uint32_t)L.fit.size();
     la.n_outputs = (uint32_t)N.n_out;
     la.n_sub = (uint32_t)N.n_sub;
-    NET_HIP(emr_launch_net(22, &la, s));
+    for (la.which = 0; la.which < emr::kSets; ++la.which) {
+      la.set = sets[la.which];
+      NET_HIP(emr_launch_net(22, &la, s));
+    }
     NET_HIP(hipStreamSynchronize(s));  // (the tables above are the host's)
     L.laid = true;
   }
@@ -1189,66 +1202,70 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   auto plan = std::make_unique<emr_networks::Learning::Plan>();
   plan->patterns = n_patterns;
   struct Shape {
-    uint32_t groups, lds, blocks;
+    uint32_t id, lds, blocks, threads;
   };
   auto nodes = [&](uint32_t g) { return N.node_off[g + 1] - N.node_off[g]; };
   auto edges = [&](uint32_t g) { return N.edge_off[g + 1] - N.edge_off[g]; };
-  auto shape = [&](uint32_t g) {
-    Shape S{n_patterns <= 4 ? 1u : (n_patterns <= 8 ? 2u : 4u), 0, 0};
-    while (S.groups > 1 && emr::learn_lds((uint32_t)nodes(g), S.groups) > emr::kLearnLds) S.groups /= 2;
-    S.lds = emr::learn_lds((uint32_t)nodes(g), S.groups);
-    S.blocks = ((uint32_t)n_patterns + 4 * S.groups - 1) / (4 * S.groups);
+  auto shape_of = [&](uint32_t g, uint32_t id) {
+    const emr::LearnShape& f = emr::kLearnShapes[id];
+    const uint32_t wide = 4 * f.lanes * f.groups;
+    Shape S{id, emr::learn_lds((uint32_t)nodes(g), f), ((uint32_t)n_patterns + wide - 1) / wide, 0};
+    S.threads = S.lds > emr::kLearnLds / 2 ? 1024 : (S.lds > emr::kLearnLds / 4 ? 512 : 256);
     return S;
+  };
+  // As many patterns beside each other as there are (an edge is read once for them), all arrays in LDS where
+  // two workgroups still share a compute unit.
+  auto shape = [&](uint32_t g) {
+    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
+    while (id > 1 && shape_of(g, (uint32_t)id).lds > emr::kLearnLds) id -= 2;
+    const Shape local = shape_of(g, (uint32_t)id - 1);
+    return local.lds <= emr::kLearnLds / 2 ? local : shape_of(g, (uint32_t)id);
   };
   auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
   double total = 0.0;
   for (uint32_t g : L.fit) total += load(g) * shape(g).blocks;
-  // A genome is stepped that does not fit, or of which one block is longer work than four times a compute
-  // unit's share of all, and than its steps' launches (8192 edges: about 12 us a step).
-  auto stepped = [&](uint32_t g) {
-    return nodes(g) > (int64_t)emr::kLearnNodes || load(g) > std::max(4.0 * total / 256.0, 8192.0);
-  };
-  // large workgroups alone on a compute unit, in pairs, and small ones
-  constexpr struct { uint32_t lds, threads; } kRuns[] = {
-      {emr::kLearnLds, 1024}, {emr::kLearnLds / 2, 1024}, {emr::kLearnLds / 4, 256}};
-  auto run_of = [&](uint32_t lds) { return lds > kRuns[1].lds ? 0 : (lds > kRuns[2].lds ? 1 : 2); };
+  // A genome is stepped of which one block is longer work than four times a compute unit's share of all,
+  // and than its steps' launches (8192 edges: about 12 us a step).
+  auto stepped = [&](uint32_t g) { return load(g) > std::max(4.0 * total / 256.0, 8192.0); };
   std::vector<emr::LearnItem> items;
   std::vector<emr::LearnJoin> joins;
   int64_t part = 0;
-  for (int r = 0; r < 3; ++r) {
-    std::vector<std::pair<double, uint32_t>> by;
-    uint32_t lds = 0;
-    for (uint32_t g : L.fit) {
+  // runs of one shape and workgroup size, the largest workgroups first, the heaviest genomes of a run first
+  std::map<std::pair<int, int>, std::vector<std::pair<double, uint32_t>>> by;
+  for (uint32_t g : L.fit) {
+    if (stepped(g)) continue;
+    const Shape S = shape(g);
+    by[{-(int)S.threads, -(int)S.id}].emplace_back(-load(g) * S.blocks, g);
+  }
+  for (auto& kv : by) {
+    std::stable_sort(kv.second.begin(), kv.second.end());
+    emr_networks::Learning::Run run{(uint32_t)items.size(), 0, (uint32_t)-kv.first.first, 0,
+                                    (uint32_t)-kv.first.second};
+    for (const auto& e : kv.second) {
+      const uint32_t g = e.second;
       const Shape S = shape(g);
-      if (stepped(g) || run_of(S.lds) != r) continue;
-      by.emplace_back(-load(g) * S.blocks, g);
-      lds = std::max(lds, S.lds);
-    }
-    std::stable_sort(by.begin(), by.end());
-    const uint32_t first = (uint32_t)items.size();
-    for (const auto& b : by) {
-      const uint32_t g = b.second;
-      const Shape S = shape(g);
+      const emr::LearnShape& f = emr::kLearnShapes[S.id];
+      run.lds = std::max(run.lds, S.lds);
       const uint32_t n = (uint32_t)std::min<double>(
           S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnWaves /
-                                                    (std::max(total, 1.0) * (kRuns[r].threads / 64)))));
+                                            (std::max(total, 1.0) * (S.threads / 64)))));
       const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
       if (n > 1) joins.push_back({g, n, part, stride});
-      for (uint32_t k = 0; k < n; ++k, part += stride)
+      for (uint32_t k = 0; k < n; ++k, part += stride) {
         items.push_back({g, (uint32_t)((uint64_t)S.blocks * k / n), (uint32_t)((uint64_t)S.blocks * (k + 1) / n),
-                         S.groups, part, n == 1 ? 1u : 0u, 0});
+                         n == 1 ? 1u : 0u, part, plan->scratch});
+        if (!f.local) plan->scratch += 2 * (nodes(g) + 1) * f.lanes * f.groups;
+      }
     }
-    if (items.size() > first)
-      plan->runs.push_back({first, (uint32_t)items.size() - first, kRuns[r].threads, lds});
+    run.count = (uint32_t)items.size() - run.first;
+    plan->runs.push_back(run);
   }
   // stepped genomes: about two workgroups for each compute unit
   std::vector<emr::LearnStepItem> steps;
   auto step_shape = [&](uint32_t g) {
-    Shape S{n_patterns <= 4 ? 1u : (n_patterns <= 8 ? 2u : 4u), 0, 0};
-    while (S.groups > 1 && emr::step_lds((uint32_t)nodes(g), S.groups) > emr::kLearnLds) S.groups /= 2;
-    S.lds = emr::step_lds((uint32_t)nodes(g), S.groups);
-    S.blocks = ((uint32_t)n_patterns + 4 * S.groups - 1) / (4 * S.groups);
-    return S;
+    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : 5);
+    while (id > 1 && shape_of(g, (uint32_t)id).lds > emr::kLearnLds) id -= 2;
+    return shape_of(g, (uint32_t)id);
   };
   double all = 0.0;
   for (uint32_t g : L.fit)
@@ -1256,15 +1273,16 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   for (uint32_t g : L.fit) {
     if (!stepped(g)) continue;
     const Shape S = step_shape(g);
-    const uint32_t waves = ((uint32_t)nodes(g) / 16 + 1) * S.groups / 4 + 1;
+    const uint32_t lanes = emr::kLearnShapes[S.id].lanes;
+    const uint32_t waves = ((uint32_t)nodes(g) / 16 + 1) * lanes / 4 + 1;
     const uint32_t chunks = (uint32_t)std::min<double>(
         std::max(1u, waves / 16), std::max(1.0, std::ceil(load(g) * 512.0 / std::max(all, 1.0))));
     const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
     joins.push_back({g, S.blocks, part, stride});
     plan->steps.lds = std::max(plan->steps.lds, S.lds);
     for (uint32_t b = 0; b < S.blocks; ++b, part += stride) {
-      for (uint32_t c = 0; c < chunks; ++c) steps.push_back({g, b, c, chunks, plan->values, part, S.groups, 0});
-      plan->values += nodes(g) * S.groups;
+      for (uint32_t c = 0; c < chunks; ++c) steps.push_back({g, b, c, chunks, plan->values, part, lanes, 0});
+      plan->values += nodes(g) * lanes;
     }
   }
   plan->steps.threads = 1024;
@@ -1300,8 +1318,9 @@ emr_status learn_args(emr_networks& N, const float* inputs, int32_t n_patterns, 
   A->joins = (*plan)->joins.as<emr::LearnJoin>();
   A->n_joins = (*plan)->n_joins;
   A->step_items = (*plan)->step_items.as<emr::LearnStepItem>();
-  const size_t need = (size_t)(*plan)->values * 48;
-  if (N.learn.values.bytes < need) NET_TRY(alloc(N.learn.values, need, "stepped values", s));
+  const size_t need = ((size_t)(*plan)->values * 3 + (size_t)(*plan)->scratch) * 16;
+  if (N.learn.values.bytes < need) NET_TRY(alloc(N.learn.values, need, "learning values", s));
+  A->values = N.learn.values.as<float4>() + 3 * (*plan)->values;
   A->place = N.learn.place.as<int64_t>();
   A->slice = N.learn.slice.as<int64_t>();
   A->node_offset = N.node_offset.as<int64_t>();
@@ -1338,6 +1357,7 @@ emr_status run_items(const emr_networks::Learning::Plan& plan, emr::LearnArgs& A
     A.n_items = r.count;
     A.threads = r.threads;
     A.lds_bytes = r.lds;
+    A.shape = r.shape;
     NET_HIP(emr_launch_net(step, &A, s));
   }
   return EMR_OK;

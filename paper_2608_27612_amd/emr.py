@@ -1205,7 +1205,7 @@ def _scores(x):
         import torch
         _SCORE_TYPES.update({torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16})
     kind = _SCORE_TYPES.get(getattr(x, "dtype", None))
-    if kind is None or not x.is_cuda or x.dim() != 2:
+    if kind is None or x.dim() != 2:
         raise ValueError("scores: a device tensor [rows, n] of float32, bfloat16 or float16 is needed")
     rows, n = x.shape
     stride, inner = x.stride()
@@ -1221,6 +1221,8 @@ def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: 
     one for each row (float32; top_k int32). Returns index (int32 [rows, draws]) and their
     log-probabilities (float32, or None without logp), not synchronized."""
     import torch
+    if not torch.is_tensor(scores) or not scores.is_cuda:
+        raise ValueError("scores: a device tensor is needed")
     with _On(stream) as raw:
         st, x = _scores(scores)
         rows = st.rows
@@ -1250,6 +1252,8 @@ def emr_answer_loss(scores, index, scale=None, temperature: float = 1.0, stream=
     include/emr.h. index: int32 [rows]; scale: float32 [rows] or None. Returns loss (float32 [rows]) and
     grad ([rows, n], of the scores' type), not synchronized."""
     import torch
+    if not torch.is_tensor(scores) or not scores.is_cuda:
+        raise ValueError("scores: a device tensor is needed")
     with _On(stream) as raw:
         st, x = _scores(scores)
         rows, n = x.shape
