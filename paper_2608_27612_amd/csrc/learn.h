@@ -4,7 +4,7 @@
 // from input nodes apart from the others ("inp", "hid"): an input holds still over the steps, so its edges
 // count once where the others count in every step. A row is a node with its edges of one kind. Rows
 // lie in slices of sixteen places, the heavy ones first:
-//   - a heavy slice holds one row of many edges (more than kLightEdges; the output nodes of "in" always),
+//   - a heavy slice holds one row of many edges (more than light_edges; the output nodes of "in" always),
 //     its edge k at base + k: the lanes of a wave share it and add their sums at the end;
 //   - a light slice holds sixteen rows, the edge k of its row r at base + 16 k + r, so that the
 //     lanes of a wave, a row each, read sixteen edges side by side; rows come in falling order of
@@ -59,7 +59,13 @@ struct NetBackArgs {
   uint32_t last;               // whether it is the first one looked at: gradients are set, not added to
 };
 
-constexpr uint32_t kLightEdges = 64;
+constexpr uint32_t kLayoutBins = 1024;  // of rows by edges (learn.hip)
+// Edges of a light row, at most: four times the mean, so that no slice is much longer than the others. (Rows
+// over the mean as heavy ones: a wave's sum and setup for each made the gradients three times as long.)
+inline constexpr uint32_t light_edges(uint32_t edges, uint32_t rows) {
+  const uint32_t four = 4u * (edges / (rows < 16u ? 16u : rows) + 1u);
+  return four < 64u ? 64u : (four < kLayoutBins - 3u ? four : kLayoutBins - 3u);
+}
 constexpr uint32_t kLearnPad = 4;  // a slice's length is a multiple of this
 constexpr int kInHid = 0, kInInp = 1, kOutHid = 2, kOutInp = 3, kSets = 4;
 constexpr uint32_t kNoEdge = 0xFFFFFFFFu;
@@ -98,16 +104,17 @@ inline constexpr uint32_t learn_lds(uint32_t n, const LearnShape& S) {
 constexpr uint32_t kLearnNodes = kLearnLds / 16u - 1u;  // the most nodes of a genome that any shape takes
 
 // Places and slices of one of a genome's layouts, at most: a slice's length is rounded up by up to kLearnPad - 1
-// sixteens; a heavy row or an output leaves up to fifteen places more; falling rows of at most
-// min(kLightEdges, e) edges leave sixteen times that.
+// sixteens; a heavy row (of more than 64 edges) or an output leaves up to fifteen places more; falling rows
+// leave sixteen times the first one's edges, of which light_edges is the bound.
 inline constexpr int64_t learn_slices(int64_t n, int64_t e, int64_t n_out) {
-  return n / 16 + 2 + e / kLightEdges + n_out;
+  return n / 16 + 2 + e / 64 + n_out;
 }
 inline constexpr int64_t learn_places(int64_t n, int64_t e, int64_t n_out) {
-  const int64_t light = e < (int64_t)kLightEdges ? e : (int64_t)kLightEdges;
+  const int64_t most = e / 4 + 4 < (int64_t)kLayoutBins ? e / 4 + 4 : (int64_t)kLayoutBins;
+  const int64_t light = e < (most < 64 ? 64 : most) ? e : (most < 64 ? 64 : most);
   const int64_t used = e < n ? e : n;  // (rows with edges)
-  return (e + 15 * (e / kLightEdges + n_out) + 16 * light +
-          16 * (kLearnPad - 1) * learn_slices(used, e, n_out) + 31) / 16 * 16;
+  return (e + 15 * (e / 64 + n_out) + 16 * light + 16 * (kLearnPad - 1) * learn_slices(used, e, n_out) + 31) /
+         16 * 16;
 }
 struct LearnRow {
   int64_t place;   // of its first edge

@@ -214,16 +214,17 @@ __device__ __forceinline__ uint32_t padded(uint32_t len) {
 }
 
 constexpr int kLayoutThreads = 512;
-constexpr uint32_t kLayoutBins = 1024;  // by edges; the last: output nodes of kInHid, then all longer rows
-
+// (kLayoutBins: the last one holds the output nodes of kInHid, the one before it all longer rows)
 // A workgroup for a genome: its rows ranked by falling edges (equal ones by node), its slices, and where each
 // row's edges go.
 __global__ void __launch_bounds__(kLayoutThreads) k_layout_slices(LearnLayoutArgs A) {
   __shared__ uint32_t bin[kLayoutBins];  // rows of it, then the rank of its next one
   __shared__ uint32_t key[kLayoutThreads];
   __shared__ uint32_t part[kLayoutThreads / kWave];
+  __shared__ uint32_t edges;
   const uint32_t g = A.genomes[blockIdx.x];
   const LearnSet& S = A.set;
+  if (threadIdx.x == 0) edges = 0;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
   LearnSlice* slices = S.slices + A.slice[g];
@@ -239,7 +240,9 @@ __global__ void __launch_bounds__(kLayoutThreads) k_layout_slices(LearnLayoutArg
   };
   for (uint32_t i = threadIdx.x; i < n; i += kLayoutThreads) {
     const uint32_t k = A.key[n0 + i];
-    if (k != kNoEdge) atomicAdd(&bin[bin_of(k)], 1u);
+    if (k == kNoEdge) continue;
+    atomicAdd(&bin[bin_of(k)], 1u);
+    atomicAdd(&edges, k & 0x7FFFFFFFu);
   }
   __syncthreads();
   // ranks of the bins' first rows, from the last bin down
@@ -252,7 +255,7 @@ __global__ void __launch_bounds__(kLayoutThreads) k_layout_slices(LearnLayoutArg
     bin[b] = at;
     bin[b - 1] = at + c0;
     __syncthreads();
-    nh = bin[kLightEdges];  // (rows of more edges)
+    nh = bin[light_edges(edges, rows)];  // (rows of more edges)
     __syncthreads();
   }
   const uint32_t ns = nh + (rows - nh + 15u) / 16u;
