@@ -89,17 +89,17 @@ struct LearnSet {
 };
 constexpr uint32_t kNoRow = 0xFFFFu;
 
-// A workgroup's block of patterns: a row has `lanes` lanes, each with `groups` times four of them. The values
-// of a genome's nodes before a step lie in LDS, those after it and a third array (the input edges' sums, the
-// sum of the steps' derivatives) there too (local), or in memory.
+// A workgroup's block of patterns: a row has `lanes` lanes with four of them each. The values of a genome's
+// nodes before a step lie in LDS, those after it and a third array (the input edges' sums, the sum of the
+// steps' derivatives) there too (local), or in memory. With eight lanes a node's values are the 128 bytes
+// that LDS delivers at a time, whatever nodes a wave's rows read.
 struct LearnShape {
-  uint32_t lanes, groups, local;
+  uint32_t lanes, local;
 };
-constexpr LearnShape kLearnShapes[] = {{1, 1, 1}, {1, 1, 0}, {2, 1, 1}, {2, 1, 0},
-                                       {4, 1, 1}, {4, 1, 0}, {4, 2, 1}, {4, 2, 0}};
+constexpr LearnShape kLearnShapes[] = {{1, 1}, {1, 0}, {2, 1}, {2, 0}, {4, 1}, {4, 0}, {8, 1}, {8, 0}};
 constexpr uint32_t kLearnLds = 160u * 1024u;
 inline constexpr uint32_t learn_lds(uint32_t n, const LearnShape& S) {
-  return (n + 1u) * 16u * S.lanes * S.groups * (S.local ? 3u : 1u);
+  return (n + 1u) * 16u * S.lanes * (S.local ? 3u : 1u);
 }
 constexpr uint32_t kLearnNodes = kLearnLds / 16u - 1u;  // the most nodes of a genome that any shape takes
 
@@ -154,9 +154,10 @@ struct LearnWeightsArgs {
 // are summed at partial + part (places of kOutHid, then of kOutInp).
 struct LearnItem {
   uint32_t genome, b0, b1;
-  uint32_t alone;     // the genome has no other item: its derivatives go to grad_w directly
+  uint16_t shape;     // of kLearnShapes
+  uint16_t alone;     // the genome has no other item: its derivatives go to grad_w directly
   int64_t part;
-  int64_t values;     // (not local) in float4: [2][node][lanes * groups]
+  int64_t values;     // (not local) in float4: [2][node][lanes]
 };
 
 // The genomes of more than one item.
@@ -170,12 +171,12 @@ struct LearnFillArgs {
   int64_t n;
 };
 
-// A workgroup of a step's launch: every chunks-th unit of rows of a genome for one block of 4 `lanes` patterns.
+// A workgroup of a step's launch: every chunks-th unit of rows of a genome for the blocks b0 .. b1 - 1 of 4
+// `lanes` patterns.
 struct LearnStepItem {
-  uint32_t genome, block, chunk, chunks;
-  int64_t values;  // of the block, in float4: [node][lanes] in each of the three arrays
+  uint32_t genome, b0, b1, chunk, chunks, lanes;
+  int64_t values;  // of the genome's first block, in float4: [block][node][lanes] in each of the three arrays
   int64_t part;
-  uint32_t lanes, pad;
 };
 
 struct LearnArgs {
@@ -199,7 +200,6 @@ struct LearnArgs {
   uint32_t steps;
   uint32_t first_item, n_items, n_joins;
   uint32_t threads, lds_bytes;
-  uint32_t shape;              // of kLearnShapes
   float4* values;              // (not local)
   // a step's launch
   const LearnStepItem* step_items;

@@ -380,12 +380,13 @@ __device__ __forceinline__ float dpp_add(float v) {
   return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
                  0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
-constexpr int kDppXor2 = 0x4E, kDppXor1 = 0xB1;
-// The sum over a row's LN lanes.
+constexpr int kDppXor2 = 0x4E, kDppXor1 = 0xB1, kDppHalfMirror = 0x141;
+// The sum over a row's LN lanes. (The mirror of eight lanes pairs a lane with one of the other four.)
 template <int LN>
 __device__ __forceinline__ float row_sum(float v) {
   if constexpr (LN >= 2) v = dpp_add<kDppXor1>(v);
   if constexpr (LN >= 4) v = dpp_add<kDppXor2>(v);
+  if constexpr (LN >= 8) v = dpp_add<kDppHalfMirror>(v);
   return v;
 }
 __device__ __forceinline__ float dot4(const float4& a, const float4& b) {
@@ -410,10 +411,11 @@ __device__ __forceinline__ Rows rows_of(const LearnArgs& A, int which, uint32_t 
   return {reinterpret_cast<const uint64_t*>(S.ent + A.place[g]), S.slices + A.slice[g],
           S.rows + 16 * A.slice[g], S.n_slices[g], S.n_heavy[g]};
 }
-// A wave takes a heavy slice, or 4 / LN light ones, at a time: units of work.
+// A wave takes a heavy slice, or the rows of 64 / LN light places, at a time: units of work.
 template <int LN>
 __device__ __forceinline__ uint32_t units_of(const Rows& R) {
-  return R.heavy + (R.n - R.heavy + 4u / LN - 1u) / (4u / LN);
+  const uint32_t light = R.n - R.heavy;
+  return R.heavy + (LN > 4 ? light * (LN / 4) : (light + 4 / LN - 1) / (4 / LN));
 }
 
 // What a lane does of a unit: lane q of the LN of its row, edges off + step k, k < count.
@@ -438,22 +440,24 @@ __device__ __forceinline__ Place<LN> place_of(const Rows& R, uint32_t unit, uint
     P.step = each;
     P.full = 16u * S.len / each;
     P.count = FIRST ? (16u * S.first + each - 1u) / each : P.full;
-    if (LN == 4) P.count = padded(P.count);
+    if (LN >= 4) P.count = padded(P.count);
     P.most = P.count;
     P.row = R.rows[16u * unit];
     P.writes = lane < (uint32_t)LN;
     return P;
   }
-  const uint32_t r = lane / LN % 16u;
   P.step = 16;
-  if constexpr (LN == 4) {  // the wave's slice
-    const uint32_t s = unit;
+  if constexpr (LN >= 4) {  // the wave's slice (or half of one)
+    constexpr uint32_t parts = LN / 4;
+    const uint32_t s = R.heavy + (unit - R.heavy) / parts;
+    const uint32_t r = (unit - R.heavy) % parts * (16u / parts) + lane / LN;
     const LearnSlice S = R.slices[s];
     P.off = S.base + r;
     P.full = S.len;
     P.count = P.most = FIRST ? padded(S.first) : S.len;
     P.row = R.rows[16u * s + r];
   } else {
+    const uint32_t r = lane / LN % 16u;
     const uint32_t s0 = R.heavy + (unit - R.heavy) * (4u / LN);
     P.most = 0;
     for (uint32_t j = 0; j < 4u / LN && s0 + j < R.n; ++j) {
@@ -472,116 +476,109 @@ __device__ __forceinline__ Place<LN> place_of(const Rows& R, uint32_t unit, uint
   return P;
 }
 
-// Four of a lane's edges from the k-th on: with LN 4 all lanes of a wave have as many, a multiple of four;
-// else empty ones past a lane's own.
+// Four of a lane's edges from the k-th on: from four lanes to a row on, all lanes of a wave have as many, a
+// multiple of four; else empty ones past a lane's own. (The address is the wave's, but for a lane's constant
+// offsets.)
 template <int LN>
 __device__ __forceinline__ void edges_at(const uint64_t* __restrict__ e, uint32_t k, const Place<LN>& P,
                                          uint32_t n, uint64_t (&v)[kLearnPad]) {
+  const uint64_t* at = e + P.step * k;
 #pragma unroll
   for (uint32_t j = 0; j < kLearnPad; ++j) {
     v[j] = n;
-    if (LN == 4 || k + j < P.count) v[j] = e[P.off + P.step * (k + j)];
+    if (LN >= 4 || k + j < P.count) v[j] = at[P.off + P.step * j];
   }
 }
 
 // The sum over the lanes of a heavy slice.
-template <int LN, int K>
-__device__ __forceinline__ void heavy_sum(float4 (&a)[K]) {
+template <int LN>
+__device__ __forceinline__ void heavy_sum(float4& a) {
 #pragma unroll
-  for (int o = LN; o < kWave; o <<= 1)
-#pragma unroll
-    for (int g = 0; g < K; ++g) {
-      a[g].x += __shfl_xor(a[g].x, o, kWave);
-      a[g].y += __shfl_xor(a[g].y, o, kWave);
-      a[g].z += __shfl_xor(a[g].z, o, kWave);
-      a[g].w += __shfl_xor(a[g].w, o, kWave);
-    }
+  for (int o = LN; o < kWave; o <<= 1) {
+    a.x += __shfl_xor(a.x, o, kWave);
+    a.y += __shfl_xor(a.y, o, kWave);
+    a.z += __shfl_xor(a.z, o, kWave);
+    a.w += __shfl_xor(a.w, o, kWave);
+  }
 }
 
-// The weighted sums of a unit's rows over x (the values of the genome's nodes, K groups of LN float4 each).
-template <int LN, int K>
-__device__ __forceinline__ void row_sums(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* x,
-                                         uint32_t n, float4 (&acc)[K]) {
+// The loops below hold kAhead fours of edges: while one is worked on, the loads of the others are under way.
+
+// The weighted sums of a unit's rows over x (the values of the genome's nodes, LN float4 each).
+template <int LN>
+__device__ __forceinline__ float4 row_sums(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* x,
+                                           uint32_t n) {
+  constexpr uint32_t kAhead = 3;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  uint64_t a[kAhead][kLearnPad];
 #pragma unroll
-  for (int g = 0; g < K; ++g) acc[g] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (P.most > 0) {
-    uint64_t a[kLearnPad], b[kLearnPad];
-    edges_at<LN>(e, 0, P, n, a);
-    for (uint32_t k = kLearnPad;; k += kLearnPad) {
-      const bool more = k < P.most;
-      if (more) edges_at<LN>(e, k, P, n, b);
+  for (uint32_t i = 0; i < kAhead; ++i)
+    if (i * kLearnPad < P.most) edges_at<LN>(e, i * kLearnPad, P, n, a[i]);
+  for (uint32_t k = 0; k < P.most; k += kAhead * kLearnPad) {
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      if (k + i * kLearnPad >= P.most) break;
 #pragma unroll
       for (uint32_t j = 0; j < kLearnPad; ++j)
-#pragma unroll
-        for (int g = 0; g < K; ++g)
-          fma4(acc[g], __uint_as_float((uint32_t)(a[j] >> 32)), x[(uint32_t)a[j] * (LN * K) + g * LN + P.q]);
-      if (!more) break;
-#pragma unroll
-      for (uint32_t j = 0; j < kLearnPad; ++j) a[j] = b[j];
+        fma4(acc, __uint_as_float((uint32_t)(a[i][j] >> 32)), x[(uint32_t)a[i][j] * LN + P.q]);
+      if (k + (i + kAhead) * kLearnPad < P.most) edges_at<LN>(e, k + (i + kAhead) * kLearnPad, P, n, a[i]);
     }
   }
-  if (P.heavy) heavy_sum<LN, K>(acc);
+  if (P.heavy) heavy_sum<LN>(acc);
+  return acc;
 }
 
 // The same for derivatives gz, and beside it the derivatives of the edges' weights, gz times the row's
 // own states s summed over the patterns, added to `sum` at the edges' places (set: stored there, the first
 // time; with FIRST, zeros at the places past those). An edge's derivative, read once from LDS, serves both.
-template <int LN, int K>
-__device__ __forceinline__ void row_grads(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* gz,
-                                          uint32_t n, const float4 (&s)[K], float* __restrict__ sum, bool set,
-                                          float4 (&acc)[K]) {
+template <int LN>
+__device__ __forceinline__ float4 row_grads(const Place<LN>& P, const uint64_t* __restrict__ e, const float4* gz,
+                                            uint32_t n, const float4& s, float* __restrict__ sum, bool set) {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kAhead = 2;  // (three spill)
+  // a row's lanes (four of them) share the adding of four edges' derivatives
+  constexpr int four = LN < (int)kLearnPad ? LN : (int)kLearnPad, own = (int)kLearnPad / four;
+  uint64_t a[kAhead][kLearnPad];
+  float had[kAhead][own];
+  const uint32_t mine = P.off + P.step * P.q;
+  auto adds = [&](uint32_t k, int c) {
+    return LN >= 4 ? P.q < (uint32_t)four : k + (uint32_t)(c * four) + P.q < P.count;
+  };
+  auto load = [&](uint32_t k, int i) {
+    edges_at<LN>(e, k, P, n, a[i]);
 #pragma unroll
-  for (int g = 0; g < K; ++g) acc[g] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (P.most > 0) {
-    // each of a row's lanes adds the derivatives of one edge in LN
-    constexpr int own = (int)kLearnPad / LN;
-    uint64_t a[kLearnPad], b[kLearnPad];
-    float had[own], next[own];
-    auto sums_at = [&](uint32_t k, float (&v)[own]) {
+    for (int c = 0; c < own; ++c)
+      had[i][c] = !set && adds(k, c) ? (sum + P.step * k)[mine + P.step * (c * four)] : 0.0f;
+  };
 #pragma unroll
-      for (int c = 0; c < own; ++c) {
-        const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
-        v[c] = !set && (LN == 4 || kk < P.count) ? sum[P.off + P.step * kk] : 0.0f;
-      }
-    };
-    edges_at<LN>(e, 0, P, n, a);
-    sums_at(0, had);
-    for (uint32_t k = 0;; k += kLearnPad) {
-      const bool more = k + kLearnPad < P.most;
-      if (more) {
-        edges_at<LN>(e, k + kLearnPad, P, n, b);
-        sums_at(k + kLearnPad, next);
-      }
+  for (int i = 0; i < kAhead; ++i)
+    if ((uint32_t)i * kLearnPad < P.most) load((uint32_t)i * kLearnPad, i);
+  for (uint32_t k0 = 0; k0 < P.most; k0 += kAhead * kLearnPad) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t k = k0 + (uint32_t)i * kLearnPad;
+      if (k >= P.most) break;
       float d[kLearnPad];
 #pragma unroll
       for (uint32_t j = 0; j < kLearnPad; ++j) {
-        float t = 0.0f;
-#pragma unroll
-        for (int g = 0; g < K; ++g) {
-          const float4 v = gz[(uint32_t)a[j] * (LN * K) + g * LN + P.q];
-          fma4(acc[g], __uint_as_float((uint32_t)(a[j] >> 32)), v);
-          t = g == 0 ? dot4(v, s[g]) : t + dot4(v, s[g]);
-        }
-        d[j] = row_sum<LN>(t);
+        const float4 v = gz[(uint32_t)a[i][j] * LN + P.q];
+        fma4(acc, __uint_as_float((uint32_t)(a[i][j] >> 32)), v);
+        d[j] = row_sum<LN>(dot4(v, s));
       }
 #pragma unroll
       for (int c = 0; c < own; ++c) {
-        float v = d[c * LN];
+        float v = d[c * four];
 #pragma unroll
-        for (int j = 1; j < LN; ++j) v = P.q == (uint32_t)j ? d[c * LN + j] : v;
-        const uint32_t kk = k + (uint32_t)(c * LN) + P.q;
-        if (LN == 4 || kk < P.count) sum[P.off + P.step * kk] = had[c] + v;
+        for (int j = 1; j < four; ++j) v = P.q == (uint32_t)j ? d[c * four + j] : v;
+        if (adds(k, c)) (sum + P.step * k)[mine + P.step * (c * four)] = had[i][c] + v;
       }
-      if (!more) break;
-#pragma unroll
-      for (uint32_t j = 0; j < kLearnPad; ++j) a[j] = b[j];
-#pragma unroll
-      for (int c = 0; c < own; ++c) had[c] = next[c];
+      if (k + kAhead * kLearnPad < P.most) load(k + kAhead * kLearnPad, i);
     }
   }
   if (set)
     for (uint32_t k = P.count + P.q; k < P.full; k += LN) sum[P.off + P.step * k] = 0.0f;
-  if (P.heavy) heavy_sum<LN, K>(acc);
+  if (P.heavy) heavy_sum<LN>(acc);
+  return acc;
 }
 
 __device__ __forceinline__ float sigmoid_f(float z) { return 1.0f / (1.0f + expf(-z)); }
@@ -645,27 +642,21 @@ __device__ __forceinline__ void fill_outputs(const LearnArgs& A, uint32_t g, uin
   }
 }
 // A unit's rows of input nodes: their edges' derivatives, and their patterns'.
-template <int LN, int K>
+template <int LN>
 __device__ __forceinline__ void input_rows(const LearnArgs& A, const Rows& R, uint32_t unit, uint32_t g,
                                            int64_t n0, uint32_t n, uint32_t block, const float4* gz, float* sum,
                                            bool set) {
   const Place<LN> P = place_of<LN, false>(R, unit, threadIdx.x % kWave);
   const int32_t slot = P.row != kNoRow ? A.node_in[n0 + P.row] : -1;
-  float4 x[K], d[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-    x[k] = slot >= 0 ? pattern4(A, slot, block * (LN * K) + k * LN + P.q) : make_float4(0.f, 0.f, 0.f, 0.f);
-  row_grads<LN, K>(P, R.ent, gz, n, x, sum, set, d);
+  const uint32_t pg = block * LN + P.q;
+  const float4 x = slot >= 0 ? pattern4(A, slot, pg) : make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4 d = row_grads<LN>(P, R.ent, gz, n, x, sum, set);
   if (!A.grad_inputs || !P.writes) return;
+  const float v[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const float v[4] = {d[k].x, d[k].y, d[k].z, d[k].w};
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-      const uint32_t p = 4u * (block * (LN * K) + k * LN + P.q) + j;
-      if (p < A.n_patterns)
-        A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[j];
-    }
+  for (uint32_t j = 0; j < 4; ++j) {
+    const uint32_t p = 4u * pg + j;
+    if (p < A.n_patterns) A.grad_inputs[((int64_t)g * A.n_patterns + p) * A.n_inputs + (uint32_t)slot] = v[j];
   }
 }
 
@@ -687,124 +678,104 @@ __device__ __forceinline__ void advance(float4*& cur, float4*& nxt, uint32_t n) 
   }
 }
 
-// All steps of one genome for an item's blocks of 4 LN K patterns.
-template <int LN, int K, bool LOCAL>
+// All steps of one genome for an item's blocks of 4 LN patterns.
+template <int LN, bool LOCAL>
 __device__ __forceinline__ void keep_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
-  constexpr int W = LN * K;
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, {LN, K, LOCAL}) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, LOCAL}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const Rows H = rows_of(A, kInHid, g), E = rows_of(A, kInInp, g);
-  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * W : A.values + I.values, *held = nxt + (n + 1u) * W;
+  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * LN : A.values + I.values, *held = nxt + (n + 1u) * LN;
   if (LOCAL)
-    for (uint32_t i = threadIdx.x; i < W; i += blockDim.x) nxt[n * W + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i = threadIdx.x; i < LN; i += blockDim.x) nxt[n * LN + i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (uint32_t b = I.b0; b < I.b1; ++b) {
-    fill_patterns<W>(A, n0, n, b, true, cur);
+    fill_patterns<LN>(A, n0, n, b, true, cur);
     __syncthreads();
-    auto put = [&](uint32_t row, uint32_t q, uint32_t step, const float4 (&z)[K]) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const uint32_t i = row * W + k * LN + q, pg = b * W + k * LN + q;
-        const float4 s = sigmoid4(z[k]);
-        nxt[i] = s;
-        if (step < A.steps && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, step - 1, pg, n0 + row) = codes_of(s);
-      }
+    auto put = [&](uint32_t row, uint32_t q, uint32_t step, const float4& z) {
+      const uint32_t pg = b * LN + q;
+      const float4 s = sigmoid4(z);
+      nxt[row * LN + q] = s;
+      if (step < A.steps && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, step - 1, pg, n0 + row) = codes_of(s);
     };
     // the first step: the inputs' edges alone, whose sums stay (hidden states are 0)
     if (A.steps > 0)
       for (uint32_t u = wave; u < units_of<LN>(E); u += waves) {
         const Place<LN> P = place_of<LN, false>(E, u, lane);
-        float4 z[K];
-        row_sums<LN, K>(P, E.ent, cur, n, z);
+        const float4 z = row_sums<LN>(P, E.ent, cur, n);
         if (!P.writes) continue;
-#pragma unroll
-        for (int k = 0; k < K; ++k) held[P.row * W + k * LN + P.q] = z[k];
+        held[P.row * LN + P.q] = z;
         put(P.row, P.q, 1, z);
       }
     for (uint32_t step = 2; step <= A.steps; ++step) {
-      advance<W, LOCAL>(cur, nxt, n);
+      advance<LN, LOCAL>(cur, nxt, n);
       // the last step: output nodes alone, the first units
       const uint32_t end = step == A.steps ? A.n_outputs : units_of<LN>(H);
       for (uint32_t u = wave; u < end; u += waves) {
         const Place<LN> P = place_of<LN, false>(H, u, lane);
-        float4 z[K];
-        row_sums<LN, K>(P, H.ent, cur, n, z);
-        if (!P.writes) continue;
-#pragma unroll
-        for (int k = 0; k < K; ++k) z[k] = add4(z[k], held[P.row * W + k * LN + P.q]);
-        put(P.row, P.q, step, z);
+        const float4 z = row_sums<LN>(P, H.ent, cur, n);
+        if (P.writes) put(P.row, P.q, step, add4(z, held[P.row * LN + P.q]));
       }
     }
     __threadfence_block();
     __syncthreads();
     const float* c = reinterpret_cast<const float*>(nxt);
-    const uint32_t p0 = b * 4u * W, np = min(A.n_patterns - p0, 4u * W);
+    const uint32_t p0 = b * 4u * LN, np = min(A.n_patterns - p0, 4u * LN);
     for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += blockDim.x) {
       const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
       A.outputs[((int64_t)g * A.n_patterns + p0 + p) * A.n_outputs + o] =
-          A.steps > 0 ? c[(uint32_t)A.out_node[o] * 4u * W + p] : 0.0f;
+          A.steps > 0 ? c[(uint32_t)A.out_node[o] * 4u * LN + p] : 0.0f;
     }
     __syncthreads();
   }
 }
 
-template <int LN, int K, bool LOCAL>
+template <int LN, bool LOCAL>
 __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
-  constexpr int W = LN * K;
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, {LN, K, LOCAL}) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, LOCAL}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const Rows H = rows_of(A, kOutHid, g), E = rows_of(A, kOutInp, g);
   const uint32_t hp = A.set[kOutHid].n_places[g], ip = A.set[kOutInp].n_places[g];
   float *hsum = A.partial + I.part, *isum = hsum + hp;
-  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * W : A.values + I.values, *all = nxt + (n + 1u) * W;
+  float4 *cur = lds, *nxt = LOCAL ? lds + (n + 1u) * LN : A.values + I.values, *all = nxt + (n + 1u) * LN;
   if (LOCAL)
-    for (uint32_t i = threadIdx.x; i < W; i += blockDim.x)
-      nxt[n * W + i] = all[n * W + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t i = threadIdx.x; i < LN; i += blockDim.x)
+      nxt[n * LN + i] = all[n * LN + i] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (A.steps < 2)  // (no step of theirs)
     for (uint32_t i = threadIdx.x; i < hp; i += blockDim.x) hsum[i] = 0.0f;
   for (uint32_t b = I.b0; b < I.b1; ++b) {
-    fill_outputs<W>(A, g, n, b, cur);
+    fill_outputs<LN>(A, g, n, b, cur);
     __syncthreads();
     for (uint32_t step = A.steps; step >= 2; --step) {
       const bool last = step == A.steps;  // derivatives at the output nodes alone
       for (uint32_t u = wave; u < units_of<LN>(H); u += waves) {
         const Place<LN> P = last ? place_of<LN, true>(H, u, lane) : place_of<LN, false>(H, u, lane);
-        uint32_t c[K];
-        float4 s[K], d[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const uint32_t pg = b * W + k * LN + P.q;
-          c[k] = P.row != kNoRow && kept_in(A.kept, pg)
-                     ? *kept_at(A.kept, A.nodes, step - 2, pg, n0 + P.row) : 0u;
-          s[k] = states(c[k]);
-        }
-        row_grads<LN, K>(P, H.ent, cur, n, s, hsum, last && b == I.b0, d);
+        const uint32_t pg = b * LN + P.q;
+        const uint32_t c = P.row != kNoRow && kept_in(A.kept, pg)
+                               ? *kept_at(A.kept, A.nodes, step - 2, pg, n0 + P.row) : 0u;
+        const float4 d = row_grads<LN>(P, H.ent, cur, n, states(c), hsum, last && b == I.b0);
         if (!P.writes) continue;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const uint32_t i = P.row * W + k * LN + P.q;
-          const float4 v = slopes(d[k], c[k]);
-          nxt[i] = v;
-          all[i] = add4(last ? cur[i] : all[i], v);
-        }
+        const uint32_t i = P.row * LN + P.q;
+        const float4 v = slopes(d, c);
+        nxt[i] = v;
+        all[i] = add4(last ? cur[i] : all[i], v);
       }
-      advance<W, LOCAL>(cur, nxt, n);
+      advance<LN, LOCAL>(cur, nxt, n);
     }
     const float4* sum_gz = A.steps < 2 ? cur : all;
     if (!LOCAL && A.steps >= 2) {
-      for (uint32_t i = threadIdx.x; i < n * W; i += blockDim.x) cur[i] = all[i];
+      for (uint32_t i = threadIdx.x; i < n * LN; i += blockDim.x) cur[i] = all[i];
       __syncthreads();
       sum_gz = cur;
     }
     for (uint32_t u = wave; u < units_of<LN>(E); u += waves)
-      input_rows<LN, K>(A, E, u, g, n0, n, b, sum_gz, isum, b == I.b0);
+      input_rows<LN>(A, E, u, g, n0, n, b, sum_gz, isum, b == I.b0);
     __syncthreads();
   }
   if (!I.alone) return;
@@ -817,25 +788,19 @@ __device__ __forceinline__ void back_item(const LearnArgs& A, const LearnItem& I
     if (ii[i] != kNoEdge) A.grad_w[ii[i]] = isum[i];
 }
 
-template <bool BACK, int LN, int K, bool LOCAL>
+template <bool BACK>
 __global__ void __launch_bounds__(1024, 4) k_learn(LearnArgs A) {
   extern __shared__ float4 learn_lds_mem[];
   const LearnItem I = A.items[A.first_item + blockIdx.x];
-  if constexpr (BACK) back_item<LN, K, LOCAL>(A, I, learn_lds_mem);
-  else keep_item<LN, K, LOCAL>(A, I, learn_lds_mem);
-}
-
-template <bool BACK>
-hipError_t launch_learn(const LearnArgs& A, hipStream_t s) {
-  const dim3 grid(A.n_items), blk(A.threads);
   static_assert(sizeof kLearnShapes / sizeof kLearnShapes[0] == 8, "a case for each shape");
 #define EMR_LEARN_CASE(i)                                                                                   \
-  case i:                                                                                                   \
-    hipLaunchKernelGGL((k_learn<BACK, (int)kLearnShapes[i].lanes, (int)kLearnShapes[i].groups,             \
-                                kLearnShapes[i].local != 0>),                                               \
-                       grid, blk, A.lds_bytes, s, A);                                                       \
-    break;
-  switch (A.shape) {
+  case i: {                                                                                                 \
+    constexpr LearnShape S = kLearnShapes[i];                                                               \
+    if constexpr (BACK) back_item<(int)S.lanes, S.local != 0>(A, I, learn_lds_mem);          \
+    else keep_item<(int)S.lanes, S.local != 0>(A, I, learn_lds_mem);                         \
+    break;                                                                                                  \
+  }
+  switch (__builtin_amdgcn_readfirstlane(I.shape)) {
     EMR_LEARN_CASE(0)
     EMR_LEARN_CASE(1)
     EMR_LEARN_CASE(2)
@@ -844,10 +809,9 @@ hipError_t launch_learn(const LearnArgs& A, hipStream_t s) {
     EMR_LEARN_CASE(5)
     EMR_LEARN_CASE(6)
     EMR_LEARN_CASE(7)
-    default: return hipErrorInvalidValue;
+    default: break;
   }
 #undef EMR_LEARN_CASE
-  return hipSuccess;
 }
 
 // ----------------------------------------------------------------------------- a step of a genome
@@ -859,32 +823,35 @@ __device__ __forceinline__ void keep_step(const LearnArgs& A, const LearnStepIte
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, {LN, 1, 0}) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, 0}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const bool first = A.step == 1, last = A.step == A.steps;
-  const float4* cur = A.cur + I.values;
-  float4 *nxt = A.nxt + I.values, *held = A.held + I.values;
   const Rows R = rows_of(A, first ? kInInp : kInHid, g);
-  if (first) {
-    fill_patterns<LN>(A, n0, n, I.block, I.chunk == 0, lds);
-  } else {
-    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
-      lds[i] = i < n * LN ? cur[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  __syncthreads();
   const uint32_t end = last && !first ? A.n_outputs : units_of<LN>(R);
-  for (uint32_t u = wave * I.chunks + I.chunk; u < end; u += waves * I.chunks) {
-    const Place<LN> P = place_of<LN, false>(R, u, lane);
-    float4 z[1];
-    row_sums<LN, 1>(P, R.ent, lds, n, z);
-    if (!P.writes) continue;
-    const uint32_t i = P.row * LN + P.q, pg = I.block * LN + P.q;
-    if (first) held[i] = z[0];
-    else z[0] = add4(z[0], held[i]);
-    const float4 s = sigmoid4(z[0]);
-    nxt[i] = s;
-    if (!last && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, A.step - 1, pg, n0 + P.row) = codes_of(s);
+  for (uint32_t b = I.b0; b < I.b1; ++b) {
+    const int64_t v0 = I.values + (int64_t)b * n * LN;
+    const float4* cur = A.cur + v0;
+    float4 *nxt = A.nxt + v0, *held = A.held + v0;
+    if (first) {
+      fill_patterns<LN>(A, n0, n, b, I.chunk == 0, lds);
+    } else {
+      for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
+        lds[i] = i < n * LN ? cur[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncthreads();
+    for (uint32_t u = wave * I.chunks + I.chunk; u < end; u += waves * I.chunks) {
+      const Place<LN> P = place_of<LN, false>(R, u, lane);
+      float4 z = row_sums<LN>(P, R.ent, lds, n);
+      if (!P.writes) continue;
+      const uint32_t i = P.row * LN + P.q, pg = b * LN + P.q;
+      if (first) held[i] = z;
+      else z = add4(z, held[i]);
+      const float4 s = sigmoid4(z);
+      nxt[i] = s;
+      if (!last && kept_in(A.kept, pg)) *kept_at(A.kept, A.nodes, A.step - 1, pg, n0 + P.row) = codes_of(s);
+    }
+    __syncthreads();
   }
 }
 
@@ -893,43 +860,45 @@ __device__ __forceinline__ void back_step(const LearnArgs& A, const LearnStepIte
   const uint32_t g = I.genome;
   const int64_t n0 = A.node_offset[g];
   const uint32_t n = (uint32_t)(A.node_offset[g + 1] - n0);
-  if (learn_lds(n, {LN, 1, 0}) > A.lds_bytes) return;  // (host-checked)
+  if (learn_lds(n, {LN, 0}) > A.lds_bytes) return;  // (host-checked)
   const uint32_t lane = threadIdx.x % kWave;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const bool inputs = A.step == 1, last = A.step == A.steps;
   const uint32_t hp = A.set[kOutHid].n_places[g];
   const Rows R = rows_of(A, inputs ? kOutInp : kOutHid, g);
   float* sum = A.partial + I.part + (inputs ? hp : 0u);
-  const float4* from = (inputs ? A.held : A.cur) + I.values;
-  float4 *nxt = A.nxt + I.values, *all = A.held + I.values;
-  // the derivatives after the step (of all steps); those after the last are at the output nodes alone
-  if (last) {
-    fill_outputs<LN>(A, g, n, I.block, lds);
-  } else {
-    for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
-      lds[i] = i < n * LN ? from[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  __syncthreads();
   if (inputs && last)  // (one step: the other edges have no part)
     for (uint32_t i = I.chunk * blockDim.x + threadIdx.x; i < hp; i += I.chunks * blockDim.x)
       A.partial[I.part + i] = 0.0f;
-  for (uint32_t u = wave * I.chunks + I.chunk; u < units_of<LN>(R); u += waves * I.chunks) {
-    if (inputs) {
-      input_rows<LN, 1>(A, R, u, g, n0, n, I.block, lds, sum, true);
-      continue;
+  for (uint32_t b = I.b0; b < I.b1; ++b) {
+    const int64_t v0 = I.values + (int64_t)b * n * LN;
+    const float4* from = (inputs ? A.held : A.cur) + v0;
+    float4 *nxt = A.nxt + v0, *all = A.held + v0;
+    // the derivatives after the step (of all steps); those after the last are at the output nodes alone
+    if (last) {
+      fill_outputs<LN>(A, g, n, b, lds);
+    } else {
+      for (uint32_t i = threadIdx.x; i < (n + 1u) * LN; i += blockDim.x)
+        lds[i] = i < n * LN ? from[i] : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const Place<LN> P = last ? place_of<LN, true>(R, u, lane) : place_of<LN, false>(R, u, lane);
-    const uint32_t pg = I.block * LN + P.q;
-    const uint32_t c = P.row != kNoRow && kept_in(A.kept, pg)
-                           ? *kept_at(A.kept, A.nodes, A.step - 2, pg, n0 + P.row) : 0u;
-    const float4 s[1] = {states(c)};
-    float4 d[1];
-    row_grads<LN, 1>(P, R.ent, lds, n, s, sum, last, d);
-    if (!P.writes) continue;
-    const uint32_t i = P.row * LN + P.q;
-    const float4 v = slopes(d[0], c);
-    nxt[i] = v;
-    all[i] = add4(last ? lds[i] : all[i], v);
+    __syncthreads();
+    for (uint32_t u = wave * I.chunks + I.chunk; u < units_of<LN>(R); u += waves * I.chunks) {
+      if (inputs) {
+        input_rows<LN>(A, R, u, g, n0, n, b, lds, sum, b == I.b0);
+        continue;
+      }
+      const Place<LN> P = last ? place_of<LN, true>(R, u, lane) : place_of<LN, false>(R, u, lane);
+      const uint32_t pg = b * LN + P.q;
+      const uint32_t c = P.row != kNoRow && kept_in(A.kept, pg)
+                             ? *kept_at(A.kept, A.nodes, A.step - 2, pg, n0 + P.row) : 0u;
+      const float4 d = row_grads<LN>(P, R.ent, lds, n, states(c), sum, last && b == I.b0);
+      if (!P.writes) continue;
+      const uint32_t i = P.row * LN + P.q;
+      const float4 v = slopes(d, c);
+      nxt[i] = v;
+      all[i] = add4(last ? lds[i] : all[i], v);
+    }
+    __syncthreads();
   }
 }
 
@@ -937,10 +906,11 @@ template <bool BACK>
 __global__ void __launch_bounds__(1024, 4) k_learn_step(LearnArgs A) {
   extern __shared__ float4 learn_lds_mem[];
   const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
-  switch (I.lanes) {
+  switch (__builtin_amdgcn_readfirstlane(I.lanes)) {
     case 1: BACK ? back_step<1>(A, I, learn_lds_mem) : keep_step<1>(A, I, learn_lds_mem); break;
     case 2: BACK ? back_step<2>(A, I, learn_lds_mem) : keep_step<2>(A, I, learn_lds_mem); break;
-    default: BACK ? back_step<4>(A, I, learn_lds_mem) : keep_step<4>(A, I, learn_lds_mem); break;
+    case 4: BACK ? back_step<4>(A, I, learn_lds_mem) : keep_step<4>(A, I, learn_lds_mem); break;
+    default: BACK ? back_step<8>(A, I, learn_lds_mem) : keep_step<8>(A, I, learn_lds_mem); break;
   }
 }
 
@@ -948,12 +918,16 @@ __global__ void __launch_bounds__(1024, 4) k_learn_step(LearnArgs A) {
 __global__ void __launch_bounds__(kNetThreads) k_step_outputs(LearnArgs A) {
   const LearnStepItem I = A.step_items[A.first_item + blockIdx.x];
   if (I.chunk != 0) return;
-  const float* v = reinterpret_cast<const float*>(A.cur + I.values);
-  const uint32_t wide = 4u * I.lanes, p0 = I.block * wide, np = min(A.n_patterns - p0, wide);
-  for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += kNetThreads) {
-    const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
-    A.outputs[((int64_t)I.genome * A.n_patterns + p0 + p) * A.n_outputs + o] =
-        A.steps ? v[(uint32_t)A.out_node[o] * wide + p] : 0.0f;
+  const int64_t n = A.node_offset[I.genome + 1] - A.node_offset[I.genome];
+  const uint32_t wide = 4u * I.lanes;
+  for (uint32_t b = I.b0; b < I.b1; ++b) {
+    const float* v = reinterpret_cast<const float*>(A.cur + I.values + b * n * I.lanes);
+    const uint32_t p0 = b * wide, np = min(A.n_patterns - p0, wide);
+    for (uint32_t i = threadIdx.x; i < np * A.n_outputs; i += kNetThreads) {
+      const uint32_t p = i / A.n_outputs, o = i % A.n_outputs;
+      A.outputs[((int64_t)I.genome * A.n_patterns + p0 + p) * A.n_outputs + o] =
+          A.steps ? v[(uint32_t)A.out_node[o] * wide + p] : 0.0f;
+    }
   }
 }
 
@@ -1039,8 +1013,10 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       if (A.n_items == 0) return hipSuccess;
       if (A.lds_bytes > kLearnLds || A.threads == 0 || A.threads > 1024u || A.threads % kWave != 0)
         return hipErrorInvalidValue;
-      const hipError_t e = step == 4 ? launch_learn<false>(A, s) : launch_learn<true>(A, s);
-      if (e != hipSuccess) return e;
+      if (step == 4)
+        hipLaunchKernelGGL(k_learn<false>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      else
+        hipLaunchKernelGGL(k_learn<true>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
       break;
     }
     case 6: {

@@ -303,7 +303,7 @@ struct emr_networks {
     Dev place, slice, fits, large, edge_dst, out_offset, out_edge;
     std::vector<uint32_t> fit, big;
     struct Run {
-      uint32_t first, count, threads, lds, shape;
+      uint32_t first, count, threads, lds;
     };
     struct Plan {
       int32_t patterns = 0;
@@ -1067,9 +1067,12 @@ emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps,
   return EMR_OK;
 }
 
-// Waves of a call's items over all genomes, about: sixteen times what the chip holds, so that the items' ends
-// fall together (150 networks on 1000 patterns, gradients: 2.56 ms at 16384, 2.36 at 32768, 2.06 at 65536).
-constexpr double kLearnWaves = 65536.0;
+// Items of a call over all genomes, about: many times what the chip holds, so that their ends fall together (150
+// networks on 1000 patterns, gradients: 1.10 ms at 4096, 0.98 at 16384, 0.97 at 65536).
+constexpr double kLearnItems = 32768.0;
+// Copies of a stepped genome's sums, at most. (Three of 5000 to 9000 nodes, a step: 50 us with a copy for each of
+// 16 blocks of patterns, 58 with eight, 67 with four: fewer leave longer workgroups.)
+constexpr uint32_t kStepGroups = 64;
 constexpr size_t kLearnPlans = 64;  // numbers of patterns whose items a handle keeps
 
 void learn_sets(emr_networks& N, emr::LearnSet* out) {
@@ -1202,70 +1205,67 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   auto plan = std::make_unique<emr_networks::Learning::Plan>();
   plan->patterns = n_patterns;
   struct Shape {
-    uint32_t id, lds, blocks, threads;
+    uint32_t id, lds, blocks;
   };
   auto nodes = [&](uint32_t g) { return N.node_off[g + 1] - N.node_off[g]; };
   auto edges = [&](uint32_t g) { return N.edge_off[g + 1] - N.edge_off[g]; };
-  auto shape_of = [&](uint32_t g, uint32_t id) {
+  auto shape_of = [&](uint32_t g, int id) {
     const emr::LearnShape& f = emr::kLearnShapes[id];
-    const uint32_t wide = 4 * f.lanes * f.groups;
-    Shape S{id, emr::learn_lds((uint32_t)nodes(g), f), ((uint32_t)n_patterns + wide - 1) / wide, 0};
-    S.threads = S.lds > emr::kLearnLds / 2 ? 1024 : (S.lds > emr::kLearnLds / 4 ? 512 : 256);
-    return S;
+    const uint32_t wide = 4 * f.lanes;
+    return Shape{(uint32_t)id, emr::learn_lds((uint32_t)nodes(g), f), ((uint32_t)n_patterns + wide - 1) / wide};
   };
-  // As many patterns beside each other as there are (an edge is read once for them), all arrays in LDS where
-  // two workgroups still share a compute unit.
-  auto shape = [&](uint32_t g) {
+  // As many patterns beside each other as there are (an edge is read once for them) and as let two workgroups
+  // share a compute unit; all arrays in LDS where that still holds.
+  constexpr uint32_t kHalf = emr::kLearnLds / 2;
+  auto shape = [&](uint32_t g, uint32_t most = kHalf) {
     int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
-    while (id > 1 && shape_of(g, (uint32_t)id).lds > emr::kLearnLds) id -= 2;
-    const Shape local = shape_of(g, (uint32_t)id - 1);
-    return local.lds <= emr::kLearnLds / 2 ? local : shape_of(g, (uint32_t)id);
+    while (id > 1 && shape_of(g, id).lds > most) id -= 2;
+    const Shape local = shape_of(g, id - 1);
+    return local.lds <= most ? local : shape_of(g, id);
   };
   auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
   double total = 0.0;
   for (uint32_t g : L.fit) total += load(g) * shape(g).blocks;
-  // A genome is stepped of which one block is longer work than four times a compute unit's share of all,
+  // A genome is stepped of which one block is longer work than a compute unit's share of all,
   // and than its steps' launches (8192 edges: about 12 us a step).
-  auto stepped = [&](uint32_t g) { return load(g) > std::max(4.0 * total / 256.0, 8192.0); };
+  auto stepped = [&](uint32_t g) { return load(g) > std::max(total / 256.0, 8192.0); };
   std::vector<emr::LearnItem> items;
   std::vector<emr::LearnJoin> joins;
   int64_t part = 0;
-  // runs of one shape and workgroup size, the largest workgroups first, the heaviest genomes of a run first
-  std::map<std::pair<int, int>, std::vector<std::pair<double, uint32_t>>> by;
-  for (uint32_t g : L.fit) {
-    if (stepped(g)) continue;
-    const Shape S = shape(g);
-    by[{-(int)S.threads, -(int)S.id}].emplace_back(-load(g) * S.blocks, g);
-  }
-  for (auto& kv : by) {
-    std::stable_sort(kv.second.begin(), kv.second.end());
-    emr_networks::Learning::Run run{(uint32_t)items.size(), 0, (uint32_t)-kv.first.first, 0,
-                                    (uint32_t)-kv.first.second};
-    for (const auto& e : kv.second) {
-      const uint32_t g = e.second;
+  // genomes that leave no room for a second workgroup, then the others, the longest items first
+  for (const bool whole : {true, false}) {
+    std::vector<std::pair<double, emr::LearnItem>> by;
+    emr_networks::Learning::Run run{(uint32_t)items.size(), 0, 1024, 0};
+    for (uint32_t g : L.fit) {
       const Shape S = shape(g);
+      if (stepped(g) || (S.lds > kHalf) != whole) continue;
       const emr::LearnShape& f = emr::kLearnShapes[S.id];
       run.lds = std::max(run.lds, S.lds);
       const uint32_t n = (uint32_t)std::min<double>(
-          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnWaves /
-                                            (std::max(total, 1.0) * (S.threads / 64)))));
+          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnItems / std::max(total, 1.0))));
       const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
       if (n > 1) joins.push_back({g, n, part, stride});
       for (uint32_t k = 0; k < n; ++k, part += stride) {
-        items.push_back({g, (uint32_t)((uint64_t)S.blocks * k / n), (uint32_t)((uint64_t)S.blocks * (k + 1) / n),
-                         n == 1 ? 1u : 0u, part, plan->scratch});
-        if (!f.local) plan->scratch += 2 * (nodes(g) + 1) * f.lanes * f.groups;
+        const uint32_t b0 = (uint32_t)((uint64_t)S.blocks * k / n), b1 = (uint32_t)((uint64_t)S.blocks * (k + 1) / n);
+        by.push_back({-load(g) * f.lanes * (b1 - b0),
+                      {g, b0, b1, (uint16_t)S.id, (uint16_t)(n == 1), part, plan->scratch}});
+        if (!f.local) plan->scratch += 2 * (nodes(g) + 1) * f.lanes;
       }
     }
+    if (by.empty()) continue;
+    std::stable_sort(by.begin(), by.end(), [](const auto& a, const auto& b) { return a.first < b.first; });
+    for (const auto& e : by) items.push_back(e.second);
     run.count = (uint32_t)items.size() - run.first;
+    // (16 waves to a compute unit are what the registers leave)
+    run.threads = whole ? 1024 : (run.lds > emr::kLearnLds / 8 ? 512 : 256);
     plan->runs.push_back(run);
   }
-  // stepped genomes: about two workgroups for each compute unit
+  // Stepped genomes: a workgroup for each compute unit (its LDS holds no second one), no more.
   std::vector<emr::LearnStepItem> steps;
   auto step_shape = [&](uint32_t g) {
-    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : 5);
-    while (id > 1 && shape_of(g, (uint32_t)id).lds > emr::kLearnLds) id -= 2;
-    return shape_of(g, (uint32_t)id);
+    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
+    while (id > 1 && shape_of(g, id).lds > emr::kLearnLds) id -= 2;
+    return shape_of(g, id);
   };
   double all = 0.0;
   for (uint32_t g : L.fit)
@@ -1274,16 +1274,17 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
     if (!stepped(g)) continue;
     const Shape S = step_shape(g);
     const uint32_t lanes = emr::kLearnShapes[S.id].lanes;
-    const uint32_t waves = ((uint32_t)nodes(g) / 16 + 1) * lanes / 4 + 1;
-    const uint32_t chunks = (uint32_t)std::min<double>(
-        std::max(1u, waves / 16), std::max(1.0, std::ceil(load(g) * 512.0 / std::max(all, 1.0))));
+    const uint32_t units = (uint32_t)(nodes(g) * lanes / 64) + 1;
+    const double share = 256.0 * load(g) * S.blocks / std::max(all, 1.0);
+    const uint32_t groups = std::min(S.blocks, kStepGroups);
+    const uint32_t chunks = (uint32_t)std::min<double>(std::max(1u, units / 8), std::max(1.0, share / groups));
     const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
-    joins.push_back({g, S.blocks, part, stride});
+    joins.push_back({g, groups, part, stride});
     plan->steps.lds = std::max(plan->steps.lds, S.lds);
-    for (uint32_t b = 0; b < S.blocks; ++b, part += stride) {
-      for (uint32_t c = 0; c < chunks; ++c) steps.push_back({g, b, c, chunks, plan->values, part, lanes, 0});
-      plan->values += nodes(g) * lanes;
-    }
+    for (uint32_t k = 0; k < groups; ++k, part += stride)
+      for (uint32_t c = 0; c < chunks; ++c)
+        steps.push_back({g, S.blocks * k / groups, S.blocks * (k + 1) / groups, c, chunks, lanes, plan->values, part});
+    plan->values += nodes(g) * lanes * S.blocks;
   }
   plan->steps.threads = 1024;
   plan->steps.count = (uint32_t)steps.size();
@@ -1357,7 +1358,6 @@ emr_status run_items(const emr_networks::Learning::Plan& plan, emr::LearnArgs& A
     A.n_items = r.count;
     A.threads = r.threads;
     A.lds_bytes = r.lds;
-    A.shape = r.shape;
     NET_HIP(emr_launch_net(step, &A, s));
   }
   return EMR_OK;
