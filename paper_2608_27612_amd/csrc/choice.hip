@@ -76,12 +76,12 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v, uint32_t lane) {  // i
   return v;
 }
 
-// Four entries of a row from i on (a multiple of four, at which the row's memory is aligned to four entries),
-// none above the largest float: those outside lo .. n - 1 as -inf. A NaN stays one: every comparison below
-// leaves it out, as it does -inf.
+// Four entries of a row from i on (a multiple of four, at which the row's memory is aligned to four entries):
+// those outside lo .. n - 1 as -inf; with `cap`, none above the largest float. A NaN stays one: every
+// comparison below leaves it out, as it does -inf.
 template <int TYPE>
 __device__ __forceinline__ void load4(const typename Score<TYPE>::T* row, uint32_t i, uint32_t lo, uint32_t n,
-                                      float (&v)[4]) {
+                                      bool cap, float (&v)[4]) {
   using T = typename Score<TYPE>::T;
   struct alignas(4 * sizeof(T)) Four {
     T v[4];
@@ -89,11 +89,15 @@ __device__ __forceinline__ void load4(const typename Score<TYPE>::T* row, uint32
   if (i >= lo && i + 4u <= n) {
     const Four f = *reinterpret_cast<const Four*>(row + i);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = capped(Score<TYPE>::get(f.v[j]));
+    for (int j = 0; j < 4; ++j) v[j] = Score<TYPE>::get(f.v[j]);
   } else {
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j)
-      v[j] = i + j >= lo && i + j < n ? capped(Score<TYPE>::get(row[i + j])) : -INFINITY;
+      v[j] = i + j >= lo && i + j < n ? Score<TYPE>::get(row[i + j]) : -INFINITY;
+  }
+  if (cap) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = capped(v[j]);
   }
 }
 
@@ -121,9 +125,10 @@ __device__ __forceinline__ RowRule row_rule(const SampleArgs& A, int64_t r, uint
   R.least = mp > 0.0f ? (uint32_t)ceil((double)fminf(mp, 1.0f) * (double)kOne) : 0u;
   return R;
 }
+__device__ __forceinline__ float exponent_of(float x, const RowRule& R) { return (x - R.m) * R.inv; }
 // (x: not a NaN)
 __device__ __forceinline__ uint32_t weight_of(float x, const RowRule& R) {
-  return (uint32_t)(expf((x - R.m) * R.inv) * kOne);
+  return (uint32_t)(expf(exponent_of(x, R)) * kOne);
 }
 // Which part of the running sum u draws.
 __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
@@ -132,7 +137,7 @@ __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
   return k < total ? k : total - 1;
 }
 __device__ __forceinline__ float logp_of(float x, const RowRule& R, uint64_t total) {
-  return (float)((double)((x - R.m) * R.inv) - log((double)total * (1.0 / 2147483648.0)));
+  return (float)((double)exponent_of(x, R) - log((double)total * (1.0 / 2147483648.0)));
 }
 
 // How many of the equal weights q, ranking after a sum of `before`, top-p's target needs (at least one).
@@ -212,7 +217,8 @@ __global__ void __launch_bounds__(256) k_sample_short(SampleArgs A) {
 
 // ----------------------------------------------------------------------------- a workgroup for a row
 
-constexpr uint32_t kFew = 64;     // entries that a wave ranks among themselves
+constexpr uint32_t kFew = 256;    // entries that threads rank among themselves, one each
+constexpr uint32_t kPairs = 128;  // entries of a list that is short enough for that from the start
 constexpr uint32_t kList = 2048;  // entries of a row that a list holds
 
 // A workgroup's memory: NT threads, bins of scores, and the row's parts.
@@ -310,7 +316,7 @@ __device__ __forceinline__ uint32_t find_part(const SH& S, uint32_t parts, uint6
 }
 
 // Whether an entry weighs anything that counts: 2^-31 of the largest is at an exponent of -31 ln 2 = -21.49.
-__device__ __forceinline__ bool weighs(float x, const RowRule& R) { return (x - R.m) * R.inv > -21.5f; }
+__device__ __forceinline__ bool weighs(float x, const RowRule& R) { return exponent_of(x, R) > -21.5f; }
 
 // A register's value that the compiler does not follow: what a pass over a row in registers computes from it
 // is not kept for the next pass, which would take more registers than the row.
@@ -329,6 +335,7 @@ struct Row {
   const SampleArgs& A;
   const T* row;
   uint32_t lo, n;
+  bool cap = false;  // scores above the largest float count as that
   static constexpr bool kWeights = NT * J <= 2048;  // (more do not fit the registers beside the scores)
   RowRule R;
   float x[4 * J + 1];
@@ -340,7 +347,7 @@ struct Row {
     n = a.n + lo;
   }
   __device__ uint32_t parts() const { return J > 0 ? (n + 3u) / 4u : (n + A.part - 1u) / A.part; }
-  // The maximum.
+  // The thread's maximum (uncapped).
   __device__ __forceinline__ float load() {
     float best = -INFINITY;
     if constexpr (J > 0) {
@@ -348,7 +355,7 @@ struct Row {
       for (int j = 0; j < J; ++j) {
         const uint32_t i = 4u * ((uint32_t)j * NT + threadIdx.x);
         float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (i < n) load4<TYPE>(row, i, lo, n, v);
+        if (i < n) load4<TYPE>(row, i, lo, n, cap, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[4 * j + c] = v[c];
       }
@@ -401,17 +408,24 @@ struct Row {
     for (; (uint64_t)i + (U - 1) * step < n; i += U * step) {
       float v[U][4];
 #pragma unroll
-      for (uint32_t k = 0; k < U; ++k) load4<TYPE>(row, i + k * step, lo, n, v[k]);
+      for (uint32_t k = 0; k < U; ++k) load4<TYPE>(row, i + k * step, lo, n, cap, v[k]);
 #pragma unroll
       for (uint32_t k = 0; k < U; ++k) f(i + k * step, v[k]);
     }
     for (; i < n; i += step) {
       float v[4];
-      load4<TYPE>(row, i, lo, n, v);
+      load4<TYPE>(row, i, lo, n, cap, v);
       f(i, v);
     }
   }
   __device__ __forceinline__ uint32_t weight(float v) const { return v > -INFINITY ? weight_of(v, R) : 0u; }
+  __device__ __forceinline__ void cap_all() {
+    cap = true;
+    if constexpr (J > 0) {
+#pragma unroll
+      for (int j = 0; j < 4 * J; ++j) x[j] = capped(x[j]);
+    }
+  }
   __device__ __forceinline__ void weigh(const RowRule& rule) {
     R = rule;
     if constexpr (J > 0 && kWeights) {
@@ -476,7 +490,7 @@ struct Row {
           for (uint32_t k = 0; k < U; ++k) {
             const uint32_t i = (p + k * W) * A.part + 4u * lane;
             if (p + k * W < parts_ && i < n) {
-              load4<TYPE>(row, i, lo, n, v[k]);
+              load4<TYPE>(row, i, lo, n, cap, v[k]);
             } else {
               v[k][0] = v[k][1] = v[k][2] = v[k][3] = NAN;
             }
@@ -493,7 +507,7 @@ struct Row {
           uint64_t sum = 0;
           for (uint32_t b = 4u * lane; b < A.part && (uint64_t)p * A.part + b < n; b += 4u * kWave) {
             float v[4];
-            load4<TYPE>(row, p * A.part + b, lo, n, v);
+            load4<TYPE>(row, p * A.part + b, lo, n, cap, v);
             sum += four(p * A.part + b, v);
           }
           if (__ballot(sum != 0) != 0) sum = wave_sum(sum);
@@ -509,7 +523,7 @@ struct Row {
   __device__ __forceinline__ uint32_t find_entry(uint32_t s, uint64_t before, uint64_t target, F&& w) {
     if constexpr (J > 0) {
       float v[4];
-      load4<TYPE>(row, 4u * s, lo, n, v);
+      load4<TYPE>(row, 4u * s, lo, n, cap, v);
       uint32_t j = 0;
 #pragma unroll
       for (uint32_t c = 0; c < 3; ++c) {
@@ -526,7 +540,7 @@ struct Row {
         uint64_t p[4], sum = 0;
         const uint32_t i = b + 4u * lane;
         if (i < end) {
-          load4<TYPE>(row, i, lo, n, v);
+          load4<TYPE>(row, i, lo, n, cap, v);
         } else {
           v[0] = v[1] = v[2] = v[3] = -INFINITY;
         }
@@ -580,19 +594,19 @@ struct List {
 };
 
 // The entries whose exponent is above -21.5, in bins of falling score: entries and weights of each bin, as
-// running sums (MASS false: all entries above -inf, and no weights). BIN(i, x): a bin, or kBins for none, rising as x falls.
-template <bool MASS, int NT, typename ROW, typename SH, typename BIN>
+// running sums (MASS false: all entries above -inf, and no weights; COUNT false: weights alone). BIN(i, x): a bin, or kBins for none, rising as x falls.
+template <bool MASS, bool COUNT, int NT, typename ROW, typename SH, typename BIN>
 __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
   for (uint32_t i = threadIdx.x; i < SH::kBins; i += NT) {
-    S.count[i] = 0;
-    S.mass[i] = 0;
+    if (COUNT) S.count[i] = 0;
+    if (MASS) S.mass[i] = 0;
   }
   __syncthreads();
   if constexpr (MASS) {
     row.each([&](uint32_t i, float x, uint32_t q) {
       const uint32_t b = bin(i, x);
       if (b >= (uint32_t)SH::kBins) return;
-      atomicAdd(&S.count[b], 1u);
+      if (COUNT) atomicAdd(&S.count[b], 1u);
       atomicAdd((unsigned long long*)&S.mass[b], (unsigned long long)q);
     });
   } else {
@@ -603,14 +617,17 @@ __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
   }
   __syncthreads();
   const uint32_t lane = threadIdx.x % kWave, wv = threadIdx.x / kWave, b = 2u * threadIdx.x;
-  const uint32_t c0 = S.count[b], c1 = S.count[b + 1];
-  uint32_t c = c0 + c1;
+  uint32_t c = 0, c1 = 0;
+  if constexpr (COUNT) {
+    c1 = S.count[b + 1];
+    c = S.count[b] + c1;
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const uint32_t w = (uint32_t)__shfl_up((int)c, o, kWave);
-    if (lane >= (uint32_t)o) c += w;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t w = (uint32_t)__shfl_up((int)c, o, kWave);
+      if (lane >= (uint32_t)o) c += w;
+    }
+    if (lane == kWave - 1) S.wcount[wv] = c;
   }
-  if (lane == kWave - 1) S.wcount[wv] = c;
   if constexpr (MASS) {
     uint64_t m[2] = {S.mass[b], S.mass[b + 1]};
     block_scan<NT, 2>(m, S);
@@ -618,11 +635,13 @@ __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
     S.mass[b + 1] = m[1];
   }
   __syncthreads();
+  if constexpr (COUNT) {
 #pragma unroll
-  for (uint32_t i = 0; i < NT / kWave; ++i) c += i < wv ? S.wcount[i] : 0u;
-  S.count[b] = c - c1;
-  S.count[b + 1] = c;
-  __syncthreads();
+    for (uint32_t i = 0; i < NT / kWave; ++i) c += i < wv ? S.wcount[i] : 0u;
+    S.count[b] = c - c1;
+    S.count[b + 1] = c;
+    __syncthreads();
+  }
 }
 
 // The bin in which the running count (mass) reaches `target`, or the last one.
@@ -642,14 +661,35 @@ __device__ __forceinline__ uint32_t reach_bin(SH& S, double target) {
   return b;
 }
 
+// Among the S.n <= kFew entries of S.cand, which rank after `count` others of weight `mass`: the one at which the
+// target is reached.
+template <bool BY_MASS, typename SH>
+__device__ __forceinline__ uint64_t rank_few(SH& S, uint64_t count, uint64_t mass, double target) {
+  const uint32_t n = S.n < kFew ? S.n : kFew;
+  if (threadIdx.x < n) {
+    const uint64_t mine = S.cand[threadIdx.x];
+    const uint32_t q = S.cq[threadIdx.x];
+    uint64_t before = mass, rank = count;
+    for (uint32_t j = 0; j < n; ++j) {
+      const bool a = S.cand[j] > mine;
+      if (BY_MASS) before += a ? S.cq[j] : 0u;
+      else rank += a ? 1u : 0u;
+    }
+    if (BY_MASS ? (double)before < target && (double)(before + q) >= target : (double)(rank + 1) == target)
+      S.cut = mine;
+  }
+  __syncthreads();
+  const uint64_t cut = S.cut;
+  __syncthreads();
+  return cut;
+}
+
 // The rank at which the entries ranking at `from` or above reach `target` by count (by weight), counted by
-// falling rank; *below receives the weight at and before it (by count: not meant without weights in the
-// bins). The bins are filled by `first`; a bin of many entries is divided again, evenly over its scores'
+// falling rank. The bins are filled by `first`; a bin of many entries is divided again, evenly over its scores'
 // bits, until few are left or all are equal. `some`: the row, or a list that holds every entry ranking
 // as high; `row`: the row.
 template <bool BY_MASS, bool MASS, int NT, int PARTS, typename SOME, typename ROW, typename SH, typename BIN>
-__device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t from, double target, BIN&& first,
-                                          uint64_t* below) {
+__device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t from, double target, BIN&& first) {
   uint32_t b = reach_bin<BY_MASS, NT>(S, target);
   uint64_t count = b ? S.count[b - 1] : 0, mass = MASS && b ? S.mass[b - 1] : 0;  // before the bin
   uint32_t inside = S.count[b] - (uint32_t)count;
@@ -702,7 +742,6 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
       const uint32_t s = find_part(S, row.parts(), m - 1);
       const uint32_t i = row.find_entry(s, s ? S.part[s - 1] : 0, m - 1, is);
       __syncthreads();
-      *below = mass + m * q;
       return (uint64_t)hi << 32 | (uint32_t)~i;
     }
     const uint32_t at = lo, width = hi - lo + 1u;  // (0: all 2^32)
@@ -711,7 +750,7 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
       if (k < lo || k > hi || rank_of(x, i) < from) return (uint32_t)SH::kBins;
       return SH::kBins - 1u - (uint32_t)((uint64_t)(k - at) * SH::kBins / (width ? width : 1ull << 32));
     };
-    bin_row<MASS, NT>(some, S, bin);
+    bin_row<MASS, true, NT>(some, S, bin);
     b = reach_bin<BY_MASS, NT>(S, BY_MASS ? target - (double)mass : target - (double)count);
     inside = S.count[b] - (b ? S.count[b - 1] : 0u);
     if (b) {
@@ -735,32 +774,58 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
     }
   });
   __syncthreads();
-  if (threadIdx.x < kWave) {
-    const uint32_t n = S.n < kFew ? S.n : kFew;
-    const uint64_t mine = threadIdx.x < n ? S.cand[threadIdx.x] : 0;
-    const uint32_t q = threadIdx.x < n ? S.cq[threadIdx.x] : 0;
-    uint64_t before = mass, rank = count;
+  return rank_few<BY_MASS>(S, count, mass, target);
+}
+
+// The draws of a row of which at most kPairs entries can be left by top-k: each thread holds one and compares
+// it with all others, for its rank and the weight before it by rank, then for the weight before it by index.
+template <int NT, typename SH>
+__device__ __forceinline__ void draw_listed(const SampleArgs& A, const RowRule& R, SH& S, uint32_t lo, int64_t d0) {
+  const uint32_t n = S.listed;
+  const bool in = threadIdx.x < n;
+  const uint64_t mine = in ? S.list[threadIdx.x] : 0;
+  const float x = key_score((uint32_t)(mine >> 32));
+  uint32_t q = in ? weight_of(x, R) : 0u, rank = 0;
+  if (in) S.cq[threadIdx.x] = q;
+  __syncthreads();
+  uint64_t above = 0, total = 0;
+  if (in)
     for (uint32_t j = 0; j < n; ++j) {
-      const bool a = S.cand[j] > mine;
-      before += a ? S.cq[j] : 0u;
+      const bool a = S.list[j] > mine;
       rank += a ? 1u : 0u;
+      above += a ? S.cq[j] : 0u;
     }
-    const bool hit = threadIdx.x < n && (BY_MASS ? (double)before < target && (double)(before + q) >= target
-                                                 : (double)(rank + 1) == target);
-    if (hit) {
-      S.cut = mine;
-      S.below = before + q;
-    }
+  if (rank >= R.k) q = 0;
+  __syncthreads();
+  if (in) S.cq[threadIdx.x] = q;
+  __syncthreads();
+  if (R.p < 1.0) {
+    for (uint32_t j = 0; j < n; ++j) total += S.cq[j];
+    if (above != 0 && !((double)above < R.p * (double)total)) q = 0;
   }
+  if (q < R.least) q = 0;
   __syncthreads();
-  *below = S.below;
-  const uint64_t cut = S.cut;
+  if (in) S.cq[threadIdx.x] = q;
   __syncthreads();
-  return cut;
+  uint64_t before = 0;
+  total = 0;
+  for (uint32_t j = 0; j < n; ++j) {
+    const uint32_t w = S.cq[j];
+    total += w;
+    before += (uint32_t)~(uint32_t)S.list[j] < (uint32_t)~(uint32_t)mine ? w : 0u;
+  }
+  if (q == 0) return;
+  for (int64_t d = blockIdx.y; d < A.draws; d += gridDim.y) {
+    const uint64_t target = target_of(A.u[d0 + d], total);
+    if (target < before || target >= before + q) continue;
+    A.index[d0 + d] = (int32_t)(~(uint32_t)mine - lo);
+    if (A.logp) A.logp[d0 + d] = logp_of(x, R, total);
+  }
 }
 
 // A workgroup for a row (blockIdx.x), and for a share of its draws (blockIdx.y). Memory: the row once
-// (J > 0); else three times, and once more for each refinement of a crowded bin.
+// (J > 0); else for its maximum, for the limits' bins and for the parts' sums, and once more for each division of
+// a crowded bin.
 template <int TYPE, int NT, int J>
 __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   using T = typename Score<TYPE>::T;
@@ -770,7 +835,11 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   const uint32_t lane = threadIdx.x % kWave;
   const int64_t r = blockIdx.x, d0 = r * A.draws;
   Row<TYPE, NT, J> row(A, static_cast<const T*>(A.x) + r * A.stride);
-  const float m = block_max<NT>(row.load(), S);
+  float m = block_max<NT>(row.load(), S);
+  if (m > 3.402823466e38f) {
+    row.cap_all();
+    m = capped(m);
+  }
   RowRule R = row_rule(A, r, (uint64_t)key_of(m) << 32);
   if (!(m > -INFINITY) || R.greedy) {
     const bool none = !(m > -INFINITY);
@@ -783,17 +852,16 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   }
   row.weigh(R);
   uint64_t from = 0;  // the least rank that is left
-  bool listed = false;
+  bool listed = false, summed = false;
   // even bins of the exponent: weights fall to 0 at 31 ln 2 = 21.5
   constexpr float kPer = (float)kBins / 21.5f;
   auto bin = [&](uint32_t, float x) {
-    const float b = (R.m - x) * R.inv * kPer;
+    const float b = exponent_of(x, R) * -kPer;
     return b < (float)kBins ? (uint32_t)b : (uint32_t)kBins - 1u;
   };
   List<NT, decltype(S)> list{S, R};
   if (R.k > 0) {
-    uint64_t below;
-    bin_row<false, NT>(row, S, bin);
+    bin_row<false, true, NT>(row, S, bin);
     if (S.count[kBins - 1] > R.k) {
       // what can be among the k: with few others, all that follows is done on a list of it
       const uint32_t b = reach_bin<false, NT>(S, (double)R.k);
@@ -805,33 +873,68 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
           if (bin(i, x) <= b) S.list[atomicAdd(&S.listed, 1u)] = rank_of(x, i);
         });
         __syncthreads();
-        from = reach<false, false, NT, PARTS>(list, row, S, 0, (double)R.k, bin, &below);
+        if (S.listed <= kPairs) {
+          draw_listed<NT>(A, R, S, row.lo, d0);
+          return;
+        }
+        from = reach<false, false, NT, PARTS>(list, row, S, 0, (double)R.k, bin);
       } else {
-        from = reach<false, false, NT, PARTS>(row, row, S, 0, (double)R.k, bin, &below);
+        from = reach<false, false, NT, PARTS>(row, row, S, 0, (double)R.k, bin);
       }
     }
   }
-  if (R.p < 1.0) {
-    auto left = [&](uint32_t i, float x) { return rank_of(x, i) < from ? (uint32_t)kBins : bin(i, x); };
-    uint64_t below;
-    if (listed) {
-      bin_row<true, NT>(list, S, left);
-      from = reach<true, true, NT, PARTS>(list, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin,
-                                          &below);
-    } else {
-      bin_row<true, NT>(row, S, left);
-      from = reach<true, true, NT, PARTS>(row, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin,
-                                          &below);
-    }
-  }
-  const float least = from ? key_score((uint32_t)(from >> 32)) : -INFINITY;
-  const uint32_t last = ~(uint32_t)from;  // the last of those equal to it
   auto kept = [&](uint32_t i, float x) {
-    if (x < least || (x == least && from != 0 && i > last)) return (uint64_t)0;
+    if (from != 0 && rank_of(x, i) < from) return (uint64_t)0;
     const uint32_t q = weight_of(x, R);
     return (uint64_t)(q >= R.least ? q : 0u);
   };
-  row.sum_parts(S, least, kept);
+  if (R.p < 1.0) {
+    auto left = [&](uint32_t i, float x) { return from != 0 && rank_of(x, i) < from ? (uint32_t)kBins : bin(i, x); };
+    if (listed) {
+      bin_row<true, true, NT>(list, S, left);
+      from = reach<true, true, NT, PARTS>(list, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin);
+    } else if constexpr (J == 0) {
+      // with the limit's bin known, one more reading gives the parts' sums of the bins before it and the
+      // entries in it, of which those that stay are added to their parts
+      bin_row<true, false, NT>(row, S, left);
+      const double target = fmax(R.p * (double)S.mass[kBins - 1], 1.0);
+      const uint32_t b = reach_bin<true, NT>(S, target);
+      const uint64_t mass = b ? S.mass[b - 1] : 0;
+      if (threadIdx.x == 0) S.n = 0;
+      __syncthreads();
+      // (a score of a later bin is below any of this one's, by more than the exponent's rounding)
+      const float low = R.m - ((float)(b + 1u) + 0.5f) / (kPer * R.inv) - fabsf(R.m) * 1e-6f;
+      row.sum_parts(S, low, [&](uint32_t i, float x) {
+        if (!weighs(x, R)) return (uint64_t)0;
+        const uint32_t at = left(i, x);
+        if (at > b) return (uint64_t)0;
+        const uint32_t q = weight_of(x, R);
+        if (at < b) return (uint64_t)(q >= R.least ? q : 0u);
+        const uint32_t k = atomicAdd(&S.n, 1u);
+        if (k < kFew) {
+          S.cand[k] = rank_of(x, i);
+          S.cq[k] = q;
+        }
+        return (uint64_t)0;
+      });
+      summed = S.n <= kFew;
+      __syncthreads();
+      if (summed) {
+        from = rank_few<true>(S, 0, mass, target);
+        if (threadIdx.x < S.n && S.cand[threadIdx.x] >= from && S.cq[threadIdx.x] >= R.least)
+          atomicAdd((unsigned long long*)&S.part[~(uint32_t)S.cand[threadIdx.x] / A.part],
+                    (unsigned long long)S.cq[threadIdx.x]);
+        __syncthreads();
+      } else {
+        bin_row<true, true, NT>(row, S, left);
+        from = reach<true, true, NT, PARTS>(row, row, S, from, target, bin);
+      }
+    } else {
+      bin_row<true, true, NT>(row, S, left);
+      from = reach<true, true, NT, PARTS>(row, row, S, from, fmax(R.p * (double)S.mass[kBins - 1], 1.0), bin);
+    }
+  }
+  if (!summed) row.sum_parts(S, from ? key_score((uint32_t)(from >> 32)) : -INFINITY, kept);
   const uint32_t parts = row.parts();
   const uint64_t total = scan_parts<NT, PARTS>(S, parts);
   if constexpr (J > 0) {
