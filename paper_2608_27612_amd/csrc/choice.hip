@@ -104,6 +104,7 @@ __device__ __forceinline__ void load4(const typename Score<TYPE>::T* row, uint32
 // What a row's draws go by.
 struct RowRule {
   float m, inv;      // maximum, 1 / temperature
+  float per;         // bins of the exponent for a unit of score (negative)
   uint32_t first;    // index of the first maximum
   uint32_t k;        // entries that top-k leaves (0: all)
   double p;          // top-p (1: all)
@@ -315,8 +316,13 @@ __device__ __forceinline__ uint32_t find_part(const SH& S, uint32_t parts, uint6
   return lo;
 }
 
-// Whether an entry weighs anything that counts: 2^-31 of the largest is at an exponent of -31 ln 2 = -21.49.
-__device__ __forceinline__ bool weighs(float x, const RowRule& R) { return exponent_of(x, R) > -21.5f; }
+// Even bins of the exponent, rising as a score falls, over the scores that weigh anything: 2^-31 of the largest
+// weight is at an exponent of -31 ln 2 = -21.49. The bin of lower scores, of -inf and of NaN is BINS.
+constexpr float kSpan = 21.5f;
+template <int BINS>
+__device__ __forceinline__ uint32_t bin_of(float x, const RowRule& R) {
+  return (uint32_t)fminf((x - R.m) * R.per, (float)BINS);
+}
 
 // A register's value that the compiler does not follow: what a pass over a row in registers computes from it
 // is not kept for the next pass, which would take more registers than the row.
@@ -377,6 +383,24 @@ struct Row {
     });
     return best;
   }
+  // f(i, score) for all entries, and places past them (-inf).
+  template <typename F>
+  __device__ __forceinline__ void each_entry(F&& f) {
+    if constexpr (J > 0) {
+      const uint32_t i = fresh(4u * threadIdx.x);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if ((uint32_t)j * 4u * NT >= n) break;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) f(i + (uint32_t)(4 * j * NT + c), fresh(x[4 * j + c]));
+      }
+    } else {
+      each_score([&](uint32_t i, const float (&v)[4]) {
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) f(i + c, v[c]);
+      });
+    }
+  }
   // f(i, score) for the entries of at least `least` (and above -inf).
   template <typename F>
   __device__ __forceinline__ void each_above(float least, F&& f) {
@@ -433,7 +457,7 @@ struct Row {
       for (int j = 0; j < 4 * J; ++j) q[j] = weight(x[j]);
     }
   }
-  // f(i, score, weight) for the entries whose exponent is above -21.5
+  // f(i, score, weight) for the entries in a bin of the exponent
   template <typename F>
   __device__ __forceinline__ void each(F&& f) {
     if constexpr (J > 0) {
@@ -444,7 +468,7 @@ struct Row {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float v = fresh(x[4 * j + c]);
-          if (weighs(v, R))
+          if (bin_of<2 * NT>(v, R) < 2 * NT)
             f(i + (uint32_t)(4 * j * NT + c), v, kWeights ? fresh(q[kWeights ? 4 * j + c : 0]) : weight_of(v, R));
         }
       }
@@ -452,7 +476,7 @@ struct Row {
       each_score([&](uint32_t i, const float (&v)[4]) {
 #pragma unroll
         for (uint32_t c = 0; c < 4; ++c)
-          if (weighs(v[c], R)) f(i + c, v[c], weight_of(v[c], R));
+          if (bin_of<2 * NT>(v[c], R) < 2 * NT) f(i + c, v[c], weight_of(v[c], R));
       });
     }
   }
@@ -580,8 +604,12 @@ struct List {
     for (uint32_t k = threadIdx.x; k < S.listed; k += NT) {
       const uint64_t r = S.list[k];
       const float x = key_score((uint32_t)(r >> 32));
-      if (weighs(x, R)) f(~(uint32_t)r, x, weight_of(x, R));
+      if (bin_of<2 * NT>(x, R) < 2 * NT) f(~(uint32_t)r, x, weight_of(x, R));
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each_entry(F&& f) {
+    each_above(-INFINITY, f);
   }
   template <typename F>
   __device__ __forceinline__ void each_above(float least, F&& f) {
@@ -593,8 +621,9 @@ struct List {
   }
 };
 
-// The entries whose exponent is above -21.5, in bins of falling score: entries and weights of each bin, as
-// running sums (MASS false: all entries above -inf, and no weights; COUNT false: weights alone). BIN(i, x): a bin, or kBins for none, rising as x falls.
+// The entries in a bin of the exponent, in bins of falling score: entries and weights of each bin, as running
+// sums (without MASS no weights, without COUNT weights alone). BIN(i, x): a bin, or kBins for none, rising as x
+// falls.
 template <bool MASS, bool COUNT, int NT, typename ROW, typename SH, typename BIN>
 __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
   for (uint32_t i = threadIdx.x; i < SH::kBins; i += NT) {
@@ -610,7 +639,7 @@ __device__ __forceinline__ void bin_row(ROW& row, SH& S, BIN&& bin) {
       atomicAdd((unsigned long long*)&S.mass[b], (unsigned long long)q);
     });
   } else {
-    row.each_above(-INFINITY, [&](uint32_t i, float x) {
+    row.each_entry([&](uint32_t i, float x) {
       const uint32_t b = bin(i, x);
       if (b < (uint32_t)SH::kBins) atomicAdd(&S.count[b], 1u);
     });
@@ -701,7 +730,7 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
       const uint32_t k = key_of(x);
       if (k < lo || k > hi) return false;
     }
-    return rank_of(x, i) >= from && (!MASS || weighs(x, some.R));
+    return bin_of<2 * NT>(x, some.R) < 2 * NT && rank_of(x, i) >= from;
   };
   while (inside > kFew) {
     // the bin's least and largest keys
@@ -747,7 +776,8 @@ __device__ __forceinline__ uint64_t reach(SOME& some, ROW& row, SH& S, uint64_t 
     const uint32_t at = lo, width = hi - lo + 1u;  // (0: all 2^32)
     auto bin = [&](uint32_t i, float x) {
       const uint32_t k = key_of(x);
-      if (k < lo || k > hi || rank_of(x, i) < from) return (uint32_t)SH::kBins;
+      if (k < lo || k > hi || bin_of<2 * NT>(x, some.R) >= 2 * NT || rank_of(x, i) < from)
+        return (uint32_t)SH::kBins;
       return SH::kBins - 1u - (uint32_t)((uint64_t)(k - at) * SH::kBins / (width ? width : 1ull << 32));
     };
     bin_row<MASS, true, NT>(some, S, bin);
@@ -841,6 +871,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
     m = capped(m);
   }
   RowRule R = row_rule(A, r, (uint64_t)key_of(m) << 32);
+  R.per = -R.inv * ((float)kBins / kSpan);
   if (!(m > -INFINITY) || R.greedy) {
     const bool none = !(m > -INFINITY);
     if (!none) R.first = ~(uint32_t)block_max<NT>(row.first_best(), S);
@@ -853,12 +884,9 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   row.weigh(R);
   uint64_t from = 0;  // the least rank that is left
   bool listed = false, summed = false;
-  // even bins of the exponent: weights fall to 0 at 31 ln 2 = 21.5
-  constexpr float kPer = (float)kBins / 21.5f;
-  auto bin = [&](uint32_t, float x) {
-    const float b = exponent_of(x, R) * -kPer;
-    return b < (float)kBins ? (uint32_t)b : (uint32_t)kBins - 1u;
-  };
+  auto bin = [&](uint32_t, float x) { return bin_of<kBins>(x, R); };
+  // A score below any of bin b's, by more than the bins' rounding.
+  auto below_bin = [&](uint32_t b) { return R.m + ((float)(b + 1u) + 0.5f) / R.per - fabsf(R.m) * 1e-6f; };
   List<NT, decltype(S)> list{S, R};
   if (R.k > 0) {
     bin_row<false, true, NT>(row, S, bin);
@@ -869,7 +897,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
       if (listed) {
         if (threadIdx.x == 0) S.listed = 0;
         __syncthreads();
-        row.each_above(-INFINITY, [&](uint32_t i, float x) {
+        row.each_above(below_bin(b), [&](uint32_t i, float x) {
           if (bin(i, x) <= b) S.list[atomicAdd(&S.listed, 1u)] = rank_of(x, i);
         });
         __syncthreads();
@@ -902,10 +930,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
       const uint64_t mass = b ? S.mass[b - 1] : 0;
       if (threadIdx.x == 0) S.n = 0;
       __syncthreads();
-      // (a score of a later bin is below any of this one's, by more than the exponent's rounding)
-      const float low = R.m - ((float)(b + 1u) + 0.5f) / (kPer * R.inv) - fabsf(R.m) * 1e-6f;
-      row.sum_parts(S, low, [&](uint32_t i, float x) {
-        if (!weighs(x, R)) return (uint64_t)0;
+      row.sum_parts(S, below_bin(b), [&](uint32_t i, float x) {
         const uint32_t at = left(i, x);
         if (at > b) return (uint64_t)0;
         const uint32_t q = weight_of(x, R);
@@ -1116,7 +1141,6 @@ __global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A)
     double all = 0.0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      if ((uint32_t)j * NT * V >= n) break;
 #pragma unroll
       for (uint32_t k = 0; k < V; ++k) {
         x[j][k] = x[j][k] != -INFINITY ? power(x[j][k] - m, factor) : 0.0f;
@@ -1129,7 +1153,6 @@ __global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A)
     if (!A.grad) return;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      if ((uint32_t)j * NT * V >= n) break;
       const uint32_t i = V * ((uint32_t)j * NT + tid);
       if (i < n) store(i, x[j], sum, some);
     }
