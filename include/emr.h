@@ -552,6 +552,10 @@ emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t s
 emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32_t n_patterns,
                              int32_t steps, float* outputs, uint8_t* kept, int64_t kept_bytes,
                              void* stream);
+/* Kept states as numbers c / 255 of a type (EMR_F32, EMR_BF16, EMR_F16): out (device, caller-owned,
+ * [steps - 1][nodes][n_patterns]), from the codes of an emr_activate_keep on networks of `nodes` nodes. */
+emr_status emr_kept_values(const uint8_t* kept, int64_t nodes, int32_t n_patterns, int32_t steps,
+                           int32_t type, void* out, void* stream);
 emr_status emr_activate_backward(const emr_networks* net, const float* inputs, int32_t n_patterns,
                                  int32_t steps, const float* outputs, const uint8_t* kept,
                                  int64_t kept_bytes, const float* grad_outputs, float* grad_w,

@@ -179,6 +179,15 @@ struct LearnStepItem {
   int64_t part;
 };
 
+// Kept states as numbers.
+struct KeptValuesArgs {
+  NetKept kept;
+  int64_t nodes;
+  uint32_t n_patterns;
+  int32_t type;   // EMR_F32, EMR_BF16, EMR_F16
+  void* out;      // [planes][nodes][n_patterns]
+};
+
 struct LearnArgs {
   LearnSet set[kSets];
   const LearnItem* items;

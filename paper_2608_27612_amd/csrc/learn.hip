@@ -955,6 +955,45 @@ __global__ void __launch_bounds__(kNetThreads) k_learn_join(LearnArgs A) {
   }
 }
 
+// ----------------------------------------------------------------------------- kept states
+
+// A state's number in a type: float, or 16 bits (bfloat16 to nearest, ties to even).
+__device__ __forceinline__ float as(float v, float) { return v; }
+__device__ __forceinline__ _Float16 as(float v, _Float16) { return (_Float16)v; }
+__device__ __forceinline__ uint16_t as(float v, uint16_t) {
+  const uint32_t b = __float_as_uint(v);
+  return (uint16_t)((b + 0x7FFFu + ((b >> 16) & 1u)) >> 16);
+}
+
+// A lane for a node's block of codes; a wave for eight blocks of eight nodes, so that both the codes read and
+// the numbers written lie side by side in runs of 128 bytes and more. (blockIdx.y: plane.)
+template <typename T>
+__global__ void __launch_bounds__(kNetThreads) k_kept_values(KeptValuesArgs A) {
+  const uint32_t b = 4u * A.kept.q, tiles = (A.kept.blocks + 7u) / 8u;
+  const int64_t groups = (A.nodes + 7) / 8, all = groups * tiles;
+  const uint32_t lane = threadIdx.x % kWave;
+  const bool wide = (uint64_t)A.n_patterns * sizeof(T) % 16 == 0 && (uintptr_t)A.out % 16 == 0;
+  for (int64_t w = grid_thread() / kWave; w < all; w += grid_threads() / kWave) {
+    const int64_t node = w / tiles * 8 + lane % 8u;
+    const uint32_t block = (uint32_t)(w % tiles) * 8u + lane / 8u;
+    if (node >= A.nodes || block >= A.kept.blocks) continue;
+    const uint8_t* c = A.kept.codes + (((int64_t)blockIdx.y * A.kept.blocks + block) * A.nodes + node) * b;
+    const uint32_t p0 = block * b, n = min(b, A.n_patterns - p0);
+    T* out = static_cast<T*>(A.out) + ((int64_t)blockIdx.y * A.nodes + node) * A.n_patterns + p0;
+    for (uint32_t k = 0; k < n; k += 4) {
+      const float4 s = states(*reinterpret_cast<const uint32_t*>(c + k));
+      struct alignas(4 * sizeof(T)) Four {
+        T v[4];
+      } f = {{as(s.x, T()), as(s.y, T()), as(s.z, T()), as(s.w, T())}};
+      if (wide && k + 4 <= n) {
+        *reinterpret_cast<Four*>(out + k) = f;
+      } else {
+        for (uint32_t j = 0; j < 4 && k + j < n; ++j) out[k + j] = f.v[j];
+      }
+    }
+  }
+}
+
 uint32_t stride_blocks(int64_t n) {
   const int64_t b = (n + kNetThreads - 1) / kNetThreads;
   return (uint32_t)(b < 1 ? 1 : (b > 16384 ? 16384 : b));
@@ -965,7 +1004,7 @@ uint32_t stride_blocks(int64_t n) {
 
 // Steps: 0 the edges' keys by source, 1 their offsets (after the sort), 2 a layout, 3 its weights; all steps
 // of the genomes in LDS: 4 activation, 5 gradients, 6 their joined sums; one step of others: 11 activation, 12
-// gradients, 13 the outputs; a genome larger than the LDS: 7 the derivatives by
+// gradients, 13 the outputs; 14 kept states as numbers; a genome larger than the LDS: 7 the derivatives by
 // the outputs' sums into gz_before (the other half behind it cleared), 8 one step's weight derivatives, 9 one
 // step backwards; 10 zeros.
 extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s) {
@@ -1054,6 +1093,22 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       const auto& A = *static_cast<const LearnFillArgs*>(args);
       if (A.n <= 0) return hipSuccess;
       hipLaunchKernelGGL(k_back_clear, dim3(stride_blocks(A.n)), blk, 0, s, A);
+      break;
+    }
+    case 14: {
+      const auto& A = *static_cast<const KeptValuesArgs*>(args);
+      const int64_t waves = (A.nodes + 7) / 8 * ((A.kept.blocks + 7) / 8);
+      for (uint32_t a = 0; a < A.kept.planes; a += 65535u) {
+        KeptValuesArgs B = A;
+        const int64_t plane = (int64_t)A.kept.blocks * A.nodes * (4 * A.kept.q);
+        B.kept.codes = A.kept.codes + a * plane;
+        B.out = static_cast<char*>(A.out) + (int64_t)a * A.nodes * A.n_patterns * (A.type == 0 ? 4 : 2);
+        const uint32_t y = A.kept.planes - a < 65535u ? A.kept.planes - a : 65535u;
+        const dim3 grid(stride_blocks(waves * kWave), y);
+        if (A.type == 0) hipLaunchKernelGGL(k_kept_values<float>, grid, blk, 0, s, B);
+        else if (A.type == 1) hipLaunchKernelGGL(k_kept_values<uint16_t>, grid, blk, 0, s, B);
+        else hipLaunchKernelGGL(k_kept_values<_Float16>, grid, blk, 0, s, B);
+      }
       break;
     }
     case 11:

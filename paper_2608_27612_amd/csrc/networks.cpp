@@ -1051,7 +1051,7 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
 }
 
 // Bytes of the codes that `steps` steps on n_patterns patterns keep, and their layout.
-emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps, uint8_t* codes,
+emr_status kept_layout(int64_t nodes, int32_t n_patterns, int32_t steps, uint8_t* codes,
                        emr::NetKept* K, int64_t* bytes) {
   if (n_patterns < 1 || n_patterns > kMaxPatterns)
     return failf(EMR_E_INVAL, "networks: n_patterns %d outside [1, %d]", n_patterns, kMaxPatterns);
@@ -1061,9 +1061,9 @@ emr_status kept_layout(const emr_networks* N, int32_t n_patterns, int32_t steps,
   K->blocks = ((uint32_t)n_patterns + 4 * K->q - 1) / (4 * K->q);
   K->planes = steps > 0 ? (uint32_t)steps - 1 : 0;
   K->codes = codes;
-  const double all = (double)K->planes * K->blocks * 4.0 * K->q * (double)N->nodes;
+  const double all = (double)K->planes * K->blocks * 4.0 * K->q * (double)nodes;
   if (all > 9e15) return failf(EMR_E_LIMIT, "networks: too many steps x nodes x patterns to keep");
-  *bytes = (int64_t)K->planes * K->blocks * N->nodes * (4 * K->q);
+  *bytes = (int64_t)K->planes * K->blocks * nodes * (4 * K->q);
   return EMR_OK;
 }
 
@@ -1217,11 +1217,11 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   // As many patterns beside each other as there are (an edge is read once for them) and as let two workgroups
   // share a compute unit; all arrays in LDS where that still holds.
   constexpr uint32_t kHalf = emr::kLearnLds / 2;
-  auto shape = [&](uint32_t g, uint32_t most = kHalf) {
+  auto shape = [&](uint32_t g) {
     int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
-    while (id > 1 && shape_of(g, id).lds > most) id -= 2;
+    while (id > 1 && shape_of(g, id).lds > kHalf) id -= 2;
     const Shape local = shape_of(g, id - 1);
-    return local.lds <= most ? local : shape_of(g, id);
+    return local.lds <= kHalf ? local : shape_of(g, id);
   };
   auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
   double total = 0.0;
@@ -1777,7 +1777,27 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
 emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes) {
   if (!net || !bytes) return failf(EMR_E_INVAL, "networks: NULL argument");
   emr::NetKept K{};
-  return kept_layout(net, n_patterns, steps, nullptr, &K, bytes);
+  return kept_layout(net->nodes, n_patterns, steps, nullptr, &K, bytes);
+}
+
+emr_status emr_kept_values(const uint8_t* kept, int64_t nodes, int32_t n_patterns, int32_t steps,
+                           int32_t type, void* out, void* stream) {
+  if (nodes < 0 || nodes > (int64_t)UINT32_MAX)
+    return failf(EMR_E_INVAL, "networks: %lld nodes", (long long)nodes);
+  if (type != EMR_F32 && type != EMR_BF16 && type != EMR_F16)
+    return failf(EMR_E_INVAL, "networks: type %d of kept states", type);
+  emr::KeptValuesArgs a{};
+  int64_t need = 0;
+  NET_TRY(kept_layout(nodes, n_patterns, steps, const_cast<uint8_t*>(kept), &a.kept, &need));
+  if (need == 0) return EMR_OK;
+  if (!kept || (uintptr_t)kept % 16 != 0 || !out || (uintptr_t)out % (uintptr_t)type_size(type) != 0)
+    return failf(EMR_E_INVAL, "networks: kept or out is NULL or not aligned");
+  a.nodes = nodes;
+  a.n_patterns = (uint32_t)n_patterns;
+  a.type = type;
+  a.out = out;
+  NET_HIP(emr_launch_net(34, &a, (hipStream_t)stream));
+  return EMR_OK;
 }
 
 emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32_t n_patterns,
@@ -1786,7 +1806,7 @@ emr_status emr_activate_keep(const emr_networks* net, const float* inputs, int32
   if (!net || !inputs || !outputs) return failf(EMR_E_INVAL, "networks: NULL argument");
   emr::NetKept K{};
   int64_t need = 0;
-  NET_TRY(kept_layout(net, n_patterns, steps, kept, &K, &need));
+  NET_TRY(kept_layout(net->nodes, n_patterns, steps, kept, &K, &need));
   if (need > 0 && (!kept || (uintptr_t)kept % 16 != 0))
     return failf(EMR_E_INVAL, "networks: kept is NULL or not aligned to 16 bytes");
   if (kept_bytes < need)
@@ -1807,7 +1827,7 @@ emr_status emr_activate_backward(const emr_networks* net, const float* inputs, i
     return failf(EMR_E_INVAL, "networks: NULL argument");
   emr::NetKept K{};
   int64_t need = 0;
-  NET_TRY(kept_layout(net, n_patterns, steps, const_cast<uint8_t*>(kept), &K, &need));
+  NET_TRY(kept_layout(net->nodes, n_patterns, steps, const_cast<uint8_t*>(kept), &K, &need));
   if (need > 0 && (!kept || (uintptr_t)kept % 16 != 0))
     return failf(EMR_E_INVAL, "networks: kept is NULL or not aligned to 16 bytes");
   if (kept_bytes < need)

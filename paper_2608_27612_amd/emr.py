@@ -34,6 +34,7 @@ ABI_FUNCTIONS = [
     "emr_networks_phase", "emr_activate", "emr_xor_fitness", "emr_free_networks",
     "emr_copy_to_host", "emr_sample", "emr_answer_loss", "emr_load_networks",
     "emr_networks_set_weights", "emr_kept_bytes", "emr_activate_keep", "emr_activate_backward",
+    "emr_kept_values",
 ]
 EMR_CONN_FORWARD, EMR_CONN_BACKWARD, EMR_CONN_LATERAL, EMR_CONN_SELF, EMR_CONN_ALL = 1, 2, 4, 8, 15
 EMR_F32, EMR_BF16, EMR_F16 = 0, 1, 2
@@ -175,6 +176,7 @@ def lib():
             "emr_kept_bytes": (I32, [P, I32, I32, P]),
             "emr_activate_keep": (I32, [P, P, I32, I32, P, P, I64, P]),
             "emr_activate_backward": (I32, [P, P, I32, I32, P, P, I64, P, P, P, P]),
+            "emr_kept_values": (I32, [P, I64, I32, I32, I32, P, P]),
             "emr_sample": (I32, [P, P, P, I64, P, P, P]),
             "emr_answer_loss": (I32, [P, P, P, F32, P, P, I64, P]),
         }
@@ -1104,13 +1106,19 @@ class Kept:
     def __init__(self, codes, patterns: int):
         self.codes, self.patterns = codes, patterns
 
-    def values(self, dtype=None):
-        """The states, [steps - 1, nodes, patterns] (a strided view)."""
+    def values(self, dtype=None, stream=None):
+        """The states as numbers of a type (float32, bfloat16 or float16), [steps - 1, nodes, patterns]; see
+        emr_kept_values in include/emr.h. Not synchronized."""
         import torch
-        t, blocks, nodes, b = self.codes.shape
-        out = torch.empty((t, nodes, blocks, b), dtype=dtype or torch.float32, device=self.codes.device)
-        torch.mul(self.codes.transpose(1, 2), 1.0 / 255.0, out=out)
-        return out.view(t, nodes, blocks * b)[:, :, :self.patterns]
+        planes, _, nodes, _ = self.codes.shape
+        dtype = dtype or torch.float32
+        if _score_type(dtype) is None:
+            raise ValueError("dtype: float32, bfloat16 or float16 is needed")
+        with _On(stream) as raw:
+            out = torch.empty((planes, nodes, self.patterns), dtype=dtype, device=self.codes.device)
+            _check(lib().emr_kept_values(self.codes.data_ptr(), nodes, self.patterns, planes + 1,
+                                         _score_type(dtype), out.data_ptr(), raw))
+            return out
 
 
 def kept_from_codes(codes) -> Kept:
@@ -1198,13 +1206,18 @@ class _On:
 _SCORE_TYPES = {}
 
 
-def _scores(x):
-    """emr_scores of a device tensor [rows, n] (a copy where its last dimension is strided), and the
-    tensor that holds them."""
+def _score_type(dtype):
+    """EMR_F32, EMR_BF16 or EMR_F16 of a torch type, or None."""
     if not _SCORE_TYPES:
         import torch
         _SCORE_TYPES.update({torch.float32: EMR_F32, torch.bfloat16: EMR_BF16, torch.float16: EMR_F16})
-    kind = _SCORE_TYPES.get(getattr(x, "dtype", None))
+    return _SCORE_TYPES.get(dtype)
+
+
+def _scores(x):
+    """emr_scores of a device tensor [rows, n] (a copy where its last dimension is strided), and the
+    tensor that holds them."""
+    kind = _score_type(getattr(x, "dtype", None))
     if kind is None or x.dim() != 2:
         raise ValueError("scores: a device tensor [rows, n] of float32, bfloat16 or float16 is needed")
     rows, n = x.shape

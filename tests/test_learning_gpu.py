@@ -171,7 +171,7 @@ def check(emr, net, a, x, steps, seed=0, codes=None):
                                    grad_inputs=True)
     gw2, none = net.activate_backward(xd, steps, out, kept, torch.tensor(grad_out, device="cuda"))
     assert none is None and torch.equal(gw, gw2)
-    c = np.rint(kept.values(torch.float64).cpu().numpy() * 255)
+    c = np.rint(kept.values().double().cpu().numpy() * 255)
     ww, wx, aw, ax = backward64(a, x, steps, out.cpu().numpy(), c, grad_out)
     terms = int(max(deg, len(x), np.bincount(a["src"]).max() if len(a["src"]) else 0))
     eps = unit(steps, terms)
@@ -264,7 +264,7 @@ def test_gradient_against_differences(emr):
         s = forward64(dict(a, w=w), x, steps)[-1]
         return (s[output_nodes(a)].transpose(0, 2, 1) * grad_out).sum()
 
-    c = np.rint(kept.values(torch.float64).cpu().numpy() * 255)
+    c = np.rint(kept.values().double().cpu().numpy() * 255)
     _, _, aw, _ = backward64(a, x, steps, out.cpu().numpy(), c, grad_out)
     w = a["w"].astype(np.float64)
     # sizes of the terms at the steepest slope (1 / 4) instead of the codes' own
@@ -331,6 +331,20 @@ def test_streams_and_graph(emr):
         assert all(torch.equal(p, q) for p, q in zip(got, want[k][1]))
         eager, _ = net.activate_keep(xs[k], 4)
         assert torch.equal(eager, out)
+
+
+@pytest.mark.parametrize("patterns", [1, 4, 7, 8, 13, 16, 40, 100, 1000])
+def test_kept_values(emr, patterns):
+    """Codes to numbers of each type and back: what torch makes of them, to the bit."""
+    g = torch.Generator(device="cuda").manual_seed(patterns)
+    codes = torch.randint(0, 256, (2, 37, patterns), generator=g, device="cuda").to(torch.uint8)
+    kept = emr.kept_from_codes(codes)
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        got = kept.values(dtype)
+        want = (codes.float() * (1.0 / 255.0)).to(dtype)
+        assert got.shape == codes.shape and torch.equal(got, want)
+    with pytest.raises(ValueError):
+        kept.values(torch.float64)
 
 
 def test_refusals(emr):
