@@ -1126,9 +1126,10 @@ def kept_from_codes(codes) -> Kept:
     import torch
     t, nodes, P = codes.shape
     b = _kept_width(P)
-    full = torch.zeros((t, nodes, -(-P // b) * b), dtype=torch.uint8, device=codes.device)
+    blocks = -(-P // b)
+    full = torch.zeros((t, nodes, blocks * b), dtype=torch.uint8, device=codes.device)
     full[:, :, :P] = codes
-    return Kept(full.view(t, nodes, -1, b).transpose(1, 2).contiguous(), P)
+    return Kept(full.view(t, nodes, blocks, b).transpose(1, 2).contiguous(), P)
 
 
 def emr_load_networks(substrate, node_offset, in_offset, in_src, in_w, node_cell=None, depth: int = 0,

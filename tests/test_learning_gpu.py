@@ -333,6 +333,20 @@ def test_streams_and_graph(emr):
         assert torch.equal(eager, out)
 
 
+def test_one_step_keeps_nothing(emr):
+    a = random_nets(3, [7, 20], 2, 2, 6)
+    net = load(emr, a)
+    nodes = int(a["node_offset"][-1])
+    x = torch.rand((5, 2), device="cuda")
+    out, kept = net.activate_keep(x, 1)
+    none = emr.kept_from_codes(torch.zeros((0, nodes, 5), dtype=torch.uint8, device="cuda"))
+    assert kept.codes.shape == none.codes.shape and kept.values().shape == (0, nodes, 5)
+    g = torch.randn_like(out)
+    one, _ = net.activate_backward(x, 1, out, kept, g)
+    two, _ = net.activate_backward(x, 1, out, none, g)
+    assert torch.equal(one, two)
+
+
 @pytest.mark.parametrize("patterns", [1, 4, 7, 8, 13, 16, 40, 100, 1000])
 def test_kept_values(emr, patterns):
     """Codes to numbers of each type and back: what torch makes of them, to the bit."""
