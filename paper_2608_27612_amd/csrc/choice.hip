@@ -871,7 +871,9 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
     m = capped(m);
   }
   RowRule R = row_rule(A, r, (uint64_t)key_of(m) << 32);
-  R.per = -R.inv * ((float)kBins / kSpan);
+  // (bounded for the least temperatures, whose bins then cover fewer scores than weigh nothing: the maximum's
+  // difference of 0 times an infinity would be in no bin)
+  R.per = fmaxf(-R.inv * ((float)kBins / kSpan), -3.402823466e38f);
   if (!(m > -INFINITY) || R.greedy) {
     const bool none = !(m > -INFINITY);
     if (!none) R.first = ~(uint32_t)block_max<NT>(row.first_best(), S);

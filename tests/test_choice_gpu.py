@@ -201,6 +201,16 @@ def test_special_values(emr, n):
     check(emr, half, u, k=2, p=0.9)
 
 
+@pytest.mark.parametrize("n", [64, 300, 3000, 12000, 50000])
+@pytest.mark.parametrize("t", [1.2e-38, 2e-38, 1e-37, 2.7e-37])
+def test_least_temperatures(emr, n, t):
+    """Temperatures whose reciprocal times the bins of the exponent is past the largest float."""
+    for spread in (3.0, 1e-37):
+        x, u = scores(n, 12, n, spread=spread)
+        for rule in (dict(), dict(k=3), dict(p=0.6), dict(k=200, p=0.9), dict(p=0.95, min_p=0.01)):
+            check(emr, x, u, t=t, **rule)
+
+
 def test_many_draws_of_one_row_follow_their_probabilities(emr):
     """Parents: 200000 draws from 1000 scores; each index as often as its probability says, within five
     standard deviations and one."""
