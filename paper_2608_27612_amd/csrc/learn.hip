@@ -678,7 +678,9 @@ __device__ __forceinline__ void advance(float4*& cur, float4*& nxt, uint32_t n) 
   }
 }
 
-// All steps of one genome for an item's blocks of 4 LN patterns.
+// All steps of one genome for an item's blocks of 4 LN patterns. Bound by LDS reads, 16 bytes for each edge,
+// step and four patterns: 150 networks of up to 773 hidden nodes, 1000 patterns, 4 steps take 638 us with the
+// kept states as numbers, their gradients (below) 1015 us.
 template <int LN, bool LOCAL>
 __device__ __forceinline__ void keep_item(const LearnArgs& A, const LearnItem& I, float4* lds) {
   const uint32_t g = I.genome;
