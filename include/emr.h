@@ -543,9 +543,10 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  *   - A weight that `steps` steps do not let reach an output has derivative 0. A node that no derivative
  *     reaches adds nothing, whatever its states.
  * Enqueued on `stream`, but for a handle's first call of the two, and its first on a number of patterns (of
- * the last 64 such numbers), which lay out edges and work and wait for the stream: not under capture. A call
- * on more patterns than before may replace buffers that a captured call uses: capture after it. Calls on
- * one handle must be ordered on one stream, as emr_activate's.
+ * the last 64 such numbers), which lay out edges and work and wait for the stream. Under capture a call that
+ * would do that, or that needs a larger buffer, is refused (EMR_E_DEVICE): make the same call once before.
+ * The tables and buffers that a captured call uses stay as they are until emr_free_networks, whatever is
+ * called after it. Calls on one handle must be ordered on one stream, as emr_activate's.
  * EMR_E_INVAL, EMR_E_CAPACITY (kept_bytes too small), EMR_E_LIMIT, EMR_E_NOMEM, EMR_E_DEVICE.
  */
 emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes);

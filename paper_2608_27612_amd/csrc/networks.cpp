@@ -19,6 +19,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <list>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -163,6 +164,7 @@ struct Dev {
   size_t cap = 0;     // the buffer's size
   int dev = 0;
   hipStream_t s = nullptr;  // the stream its users run on
+  bool captured = false;    // a captured call names it: it stays with its handle (grow)
   Dev() = default;
   Dev(const Dev&) = delete;
   Dev& operator=(const Dev&) = delete;
@@ -178,8 +180,10 @@ struct Dev {
     cap = o.cap;
     dev = o.dev;
     s = o.s;
+    captured = o.captured;
     o.p = nullptr;
     o.bytes = o.cap = 0;
+    o.captured = false;
   }
   template <class T>
   T* as() const {
@@ -191,6 +195,7 @@ struct Dev {
     if (p) cache_give(dev, p, cap, s, idle);
     p = nullptr;
     bytes = cap = 0;
+    captured = false;
   }
 };
 
@@ -294,6 +299,7 @@ struct emr_networks {
   Dev d_out_node;  // [n_out] substrate index of output o
   int64_t nodes = 0, edges = 0;
   Dev state, patterns;
+  std::list<Dev> retired;  // replaced buffers that captured calls name
   // learning, from its first call on: the edges' layouts of the genomes that fit a workgroup (learn.h), by
   // genome the first place and slice; the others, whose edges by source lie in out_edge; the items by
   // number of patterns; partial sums, and a larger genome's derivatives
@@ -314,8 +320,9 @@ struct emr_networks {
       int64_t values = 0;         // float4 of each of their three arrays
       int64_t scratch = 0;        // float4 of the items' values outside LDS
       int64_t partial_floats = 0;
+      bool captured = false;      // a captured call names its tables: it stays
     };
-    std::vector<std::unique_ptr<Plan>> plans;  // by number of patterns, the oldest first
+    std::vector<std::unique_ptr<Plan>> plans;  // by number of patterns, the one used longest ago first
     Dev partial, back, values;
     void release_idle() {
       for (int k = 0; k < emr::kSets; ++k)
@@ -361,6 +368,7 @@ struct emr_networks {
     for (Dev* d : {&known, &node_offset, &node_cell, &node_in, &in_offset, &in_src, &in_w,
                    &d_slots, &d_out_node, &state, &patterns, &order})
       d->reset_idle();
+    for (Dev& d : retired) d.reset_idle();
     learn.release_idle();
   }
 };
@@ -915,6 +923,37 @@ emr_status check_device(const emr_networks* N) {
   return EMR_OK;
 }
 
+// Whether work enqueued on s goes into a graph instead of running now.
+bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) != hipSuccess) (void)hipGetLastError();
+  return st != hipStreamCaptureStatusNone;
+}
+
+// At least `bytes` in one of a handle's buffers, for work on `s`. What a captured call names stays as it is
+// until the handle goes: its replays name it too.
+emr_status grow(emr_networks& M, Dev& d, size_t bytes, const char* what, hipStream_t s) {
+  if (d.bytes < bytes) {
+    if (d.captured) {
+      M.retired.emplace_back();
+      M.retired.back().take(d);
+    }
+    d.s = s;  // (the calls before this one are ordered before it)
+    NET_TRY(alloc(d, bytes, what, s));
+  }
+  d.s = s;
+  return EMR_OK;
+}
+
+// The same for a call that may be under capture, which gets no new buffer.
+emr_status grow_outside(emr_networks& M, Dev& d, size_t bytes, const char* what, hipStream_t s, bool captured) {
+  if (captured && d.bytes < bytes)
+    return failf(EMR_E_DEVICE, "networks: the call needs new %s: not under capture before it has run once", what);
+  NET_TRY(grow(M, d, bytes, what, s));
+  d.captured |= captured;
+  return EMR_OK;
+}
+
 // The end of the work queued on `s`, which the handle's buffers outlive.
 emr_status mark_done(emr_networks& M, hipStream_t s) {
   if (!M.done) NET_HIP(hipEventCreateWithFlags(&M.done, hipEventDisableTiming));
@@ -1003,7 +1042,8 @@ emr_status run_forward(const emr_networks* N, const float* patterns, int32_t n_p
   if (list.total > 0) {
     // two state buffers of [pblocks][nodes] float4
     const size_t half = (size_t)pblocks * (size_t)(N->nodes ? N->nodes : 1) * 16;
-    if (M.state.bytes < 2 * half) NET_TRY(alloc(M.state, 2 * half, "node states", s));
+    NET_TRY(grow(M, M.state, 2 * half, "node states", s));
+    M.state.captured |= capturing(s);
     float* buf[2] = {M.state.as<float>(), reinterpret_cast<float*>(M.state.as<char>() + half)};
     // (a launch covers at most 65535 genomes)
     const emr::NetList whole = list;
@@ -1086,10 +1126,12 @@ void learn_sets(emr_networks& N, emr::LearnSet* out) {
 
 // The edges by source and the layouts of the genomes that fit a workgroup, on the first learning call's
 // stream.
-emr_status lay_out(emr_networks& N, hipStream_t s) {
+emr_status lay_out(emr_networks& N, hipStream_t s, bool captured) {
   auto& L = N.learn;
   const size_t G = (size_t)N.n_genomes, E = (size_t)N.edges;
   if (!L.laid) {
+    if (captured)
+      return failf(EMR_E_DEVICE, "networks: the first learning call lays the edges out: not under capture");
     if (N.edges > (int64_t)UINT32_MAX - 1) return failf(EMR_E_LIMIT, "networks: too many edges");
     L.fit.clear();
     L.big.clear();
@@ -1195,13 +1237,17 @@ emr_status lay_weights(emr_networks& N, hipStream_t s) {
 // The workgroups' shares of a call on this number of patterns: each genome's blocks in as many items as its
 // load asks for, the heaviest genomes first, in runs of one shape.
 emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learning::Plan** out,
-                      hipStream_t s) {
+                      hipStream_t s, bool captured) {
   auto& L = N.learn;
-  for (auto& p : L.plans)
-    if (p->patterns == n_patterns) {
-      *out = p.get();
+  for (auto p = L.plans.begin(); p != L.plans.end(); ++p)
+    if ((*p)->patterns == n_patterns) {
+      std::rotate(p, p + 1, L.plans.end());
+      *out = L.plans.back().get();
+      (*out)->captured |= captured;
       return EMR_OK;
     }
+  if (captured)
+    return failf(EMR_E_DEVICE, "networks: the first learning call on %d patterns: not under capture", n_patterns);
   auto plan = std::make_unique<emr_networks::Learning::Plan>();
   plan->patterns = n_patterns;
   struct Shape {
@@ -1299,7 +1345,13 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   NET_HIP(hipStreamSynchronize(s));  // (the tables above are the host's)
   plan->n_joins = (uint32_t)joins.size();
   plan->partial_floats = part;
-  if (L.plans.size() >= kLearnPlans) L.plans.erase(L.plans.begin());
+  if (L.plans.size() >= kLearnPlans) {
+    const auto old = std::find_if(L.plans.begin(), L.plans.end(), [](const auto& p) { return !p->captured; });
+    if (old != L.plans.end()) {
+      for (Dev* d : {&(*old)->items, &(*old)->joins, &(*old)->step_items}) d->s = s;  // (its last use is before this)
+      L.plans.erase(old);
+    }
+  }
   L.plans.push_back(std::move(plan));
   *out = L.plans.back().get();
   return EMR_OK;
@@ -1308,19 +1360,19 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
 // Every learning call's arguments, its layouts and items made.
 emr_status learn_args(emr_networks& N, const float* inputs, int32_t n_patterns, int32_t steps,
                       float* outputs, const emr::NetKept& K, emr::LearnArgs* A,
-                      emr_networks::Learning::Plan** plan, hipStream_t s) {
+                      emr_networks::Learning::Plan** plan, hipStream_t s, bool captured) {
   NET_TRY(check_device(&N));
   if ((int64_t)((n_patterns + 15) / 16) * (N.nodes ? N.nodes : 1) > ((int64_t)1 << 38))
     return failf(EMR_E_LIMIT, "networks: too many nodes x patterns");
-  NET_TRY(lay_out(N, s));
-  NET_TRY(plan_items(N, n_patterns, plan, s));
+  NET_TRY(lay_out(N, s, captured));
+  NET_TRY(plan_items(N, n_patterns, plan, s, captured));
   learn_sets(N, A->set);
   A->items = (*plan)->items.as<emr::LearnItem>();
   A->joins = (*plan)->joins.as<emr::LearnJoin>();
   A->n_joins = (*plan)->n_joins;
   A->step_items = (*plan)->step_items.as<emr::LearnStepItem>();
   const size_t need = ((size_t)(*plan)->values * 3 + (size_t)(*plan)->scratch) * 16;
-  if (N.learn.values.bytes < need) NET_TRY(alloc(N.learn.values, need, "learning values", s));
+  NET_TRY(grow_outside(N, N.learn.values, need, "learning values", s, captured));
   A->values = N.learn.values.as<float4>() + 3 * (*plan)->values;
   A->place = N.learn.place.as<int64_t>();
   A->slice = N.learn.slice.as<int64_t>();
@@ -1367,7 +1419,12 @@ emr_status run_keep(emr_networks& N, const float* inputs, int32_t n_patterns, in
                     float* outputs, const emr::NetKept& K, hipStream_t s) {
   emr::LearnArgs A{};
   emr_networks::Learning::Plan* plan;
-  NET_TRY(learn_args(N, inputs, n_patterns, steps, outputs, K, &A, &plan, s));
+  const bool captured = capturing(s);
+  NET_TRY(learn_args(N, inputs, n_patterns, steps, outputs, K, &A, &plan, s, captured));
+  const auto& big = N.learn.big;
+  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
+  const size_t half = (size_t)pblocks * (size_t)N.nodes * 16;
+  if (!big.empty()) NET_TRY(grow_outside(N, N.state, 2 * half, "node states", s, captured));
   NET_TRY(run_items(*plan, A, 24, s));
   if (plan->steps.count > 0) {
     int swap = 0;
@@ -1379,10 +1436,6 @@ emr_status run_keep(emr_networks& N, const float* inputs, int32_t n_patterns, in
     step_args(N, *plan, swap, A);
     NET_HIP(emr_launch_net(33, &A, s));
   }
-  const auto& big = N.learn.big;
-  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
-  const size_t half = (size_t)pblocks * (size_t)N.nodes * 16;
-  if (!big.empty() && N.state.bytes < 2 * half) NET_TRY(alloc(N.state, 2 * half, "node states", s));
   float* buf[2] = {N.state.as<float>(), reinterpret_cast<float*>(N.state.as<char>() + half)};
   for (size_t done = 0; done < big.size(); done += 65535) {  // (a launch covers at most 65535 genomes)
     emr::NetList list{};
@@ -1429,10 +1482,15 @@ emr_status run_backward(emr_networks& N, const float* inputs, int32_t n_patterns
   }
   emr::LearnArgs A{};
   emr_networks::Learning::Plan* plan;
-  NET_TRY(learn_args(N, inputs, n_patterns, steps, const_cast<float*>(outputs), K, &A, &plan, s));
+  const bool captured = capturing(s);
+  NET_TRY(learn_args(N, inputs, n_patterns, steps, const_cast<float*>(outputs), K, &A, &plan, s, captured));
   auto& L = N.learn;
-  const size_t need = (size_t)plan->partial_floats * 4;
-  if (L.partial.bytes < need) NET_TRY(alloc(L.partial, need, "partial derivatives", s));
+  NET_TRY(grow_outside(N, L.partial, (size_t)plan->partial_floats * 4, "partial derivatives", s, captured));
+  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
+  size_t half = 0;
+  for (uint32_t g : L.big)
+    half = std::max(half, (size_t)pblocks * (size_t)(N.node_off[g + 1] - N.node_off[g]) * 16);
+  NET_TRY(grow_outside(N, L.back, 2 * half, "derivatives", s, captured));
   A.partial = L.partial.as<float>();
   A.grad_outputs = grad_outputs;
   A.grad_w = grad_w;
@@ -1447,11 +1505,6 @@ emr_status run_backward(emr_networks& N, const float* inputs, int32_t n_patterns
     }
   }
   NET_HIP(emr_launch_net(26, &A, s));
-  const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
-  size_t half = 0;
-  for (uint32_t g : L.big)
-    half = std::max(half, (size_t)pblocks * (size_t)(N.node_off[g + 1] - N.node_off[g]) * 16);
-  if (L.back.bytes < 2 * half) NET_TRY(alloc(L.back, 2 * half, "derivatives", s));
   for (uint32_t g : L.big) {
     emr::NetBackArgs B{};
     B.genome = g;

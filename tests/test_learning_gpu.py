@@ -394,3 +394,45 @@ def test_refusals(emr):
     with pytest.raises(emr.EmrError) as e:
         emr.emr_load_networks(a["subs"], a["node_offset"], into_input, a["src"], a["w"])
     assert e.value.status == emr.EMR_E_INVAL
+
+
+def test_graph_beside_other_calls(emr):
+    """A captured call's replays give the same bits after calls on fewer and on more patterns, on more than 64
+    numbers of them, on other handles; a call under capture that would lay out or allocate is refused, and
+    the capture goes on."""
+    a = random_nets(11, [900] + [60] * 40, 2, 1, 60)
+    a = dict(a, w=a["w"] * np.float32(0.5))
+    net, fresh = load(emr, a), load(emr, a)
+    x = torch.rand((96, 2), device="cuda")
+    g = torch.randn((41, 96, 1), device="cuda")
+    want_out, kept = net.activate_keep(x, 3)
+    want, _ = net.activate_backward(x, 3, want_out, kept, g)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(emr.EmrError) as e:
+            fresh.activate_keep(x, 3)
+        assert e.value.status == emr.EMR_E_DEVICE
+        with pytest.raises(emr.EmrError):
+            net.activate_keep(x[:95], 3)
+        out, kept = net.activate_keep(x, 3)
+        got, _ = net.activate_backward(x, 3, out, kept, g)
+
+    def others():
+        for handle in (net, fresh):
+            for patterns in [64, 700] + list(range(1, 70)):
+                y = torch.rand((patterns, 2), device="cuda")
+                o, k = handle.activate_keep(y, 2)
+                handle.activate_backward(y, 2, o, k, torch.ones_like(o))
+
+    for _ in range(2):
+        out.zero_()
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want_out) and torch.equal(got, want)
+        others()
+        torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want_out) and torch.equal(got, want)

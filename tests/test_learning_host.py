@@ -1,0 +1,204 @@
+"""The learning calls' host code without a GPU: networks.cpp linked with the stand-in runtime
+(tests/shim/fake_hip.cpp) and launchers that write down what they are given (tests/shim/fake_learn.cpp), for
+which buffers a call uses, keeps and replaces."""
+
+import ctypes as C
+import gc
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2608_27612_amd import emr as E
+from paper_2608_27612_amd import workloads as W
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(os.path.dirname(HERE), "paper_2608_27612_amd", "csrc")
+FLAGS = ["g++", "-std=c++17", "-O1", "-fPIC", "-w", "-pthread", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include"]
+FIELDS = ("step", "items", "joins", "step_items", "values", "partial", "state", "count", "first", "at")
+MB = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def built(tmp_path_factory):
+    at = tmp_path_factory.mktemp("fake")
+    path, plain = str(at / "libfake.so"), str(at / "fake_hip.o")
+    subprocess.check_call(FLAGS + ["-Demr_launch_net=emr_launch_net_of_no_kernel", "-c",
+                                   os.path.join(HERE, "shim", "fake_hip.cpp"), "-o", plain])
+    subprocess.check_call(FLAGS + ["-shared", "-Wl,-Bsymbolic", plain, os.path.join(HERE, "shim", "fake_learn.cpp")]
+                          + [os.path.join(CSRC, s) for s in ("runtime.cpp", "networks.cpp", "plan.cpp", "pack.cpp",
+                                                             "sched.cpp", "jit.cpp", "record_file.cpp")]
+                          + ["-o", path])
+    return path
+
+
+@pytest.fixture
+def lib(built, tmp_path):
+    """The binding on a copy of the stand-in library, and the stand-in's own calls."""
+    path = str(tmp_path / "libfake.so")
+    shutil.copy(built, path)
+    keep = E._lib, E.LIB_PATH
+    E._lib, E.LIB_PATH = None, path
+    L = E.lib()
+    for name, (res, args) in {"fake_capturing": (None, [C.c_int]), "fake_held": (C.c_int64, []),
+                              "fake_hold_events": (None, [C.c_int]), "fake_counts": (None, [C.c_void_p]),
+                              "fake_size": (C.c_int64, [C.c_void_p]), "fake_launches": (C.c_int64, []),
+                              "fake_launch": (None, [C.c_int64, C.c_void_p])}.items():
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = res, args
+    yield L
+    gc.collect()
+    E._lib, E.LIB_PATH = keep
+
+
+def launches(lib, first=0):
+    out = []
+    for i in range(first, lib.fake_launches()):
+        v = (C.c_int64 * len(FIELDS))()
+        lib.fake_launch(i, v)
+        out.append(dict(zip(FIELDS, v)))
+    return out
+
+
+def networks(nodes, edges):
+    """A handle of genomes of one input, one output, and these numbers of nodes and edges (spread evenly over
+    the nodes but the input, from node 0 on)."""
+    src = W.sources_array([(0.0, -1.0, 0), (0.0, 1.0, 1)])
+    node_offset, degrees, ins = [0], [], []
+    for n, e in zip(nodes, edges):
+        d = np.full(n, e // (n - 1))
+        d[0] = 0
+        d[1] += e - d.sum()
+        degrees.append(d)
+        ins.append(node_offset[-1] + np.arange(e) % n)
+        node_offset.append(node_offset[-1] + n)
+    in_offset = np.concatenate([[0], np.cumsum(np.concatenate(degrees))]).astype(np.int64)
+    ins = np.concatenate(ins).astype(np.uint32)
+    w = np.zeros(len(ins), np.float32)
+    node_offset = np.array(node_offset, np.int64)
+    h = C.c_void_p()
+    assert E.lib().emr_load_networks(src.ctypes.data, 2, 0, len(nodes), node_offset.ctypes.data, None,
+                                     in_offset.ctypes.data, ins.ctypes.data, w.ctypes.data, C.byref(h), None) == 0
+    return h
+
+
+ANY = 1 << 20  # an aligned address that nothing reads
+
+
+def keep(h, patterns, steps=3):
+    return E.lib().emr_activate_keep(h, ANY, patterns, steps, ANY, ANY, 1 << 50, None)
+
+
+def back(h, patterns, steps=3):
+    return E.lib().emr_activate_backward(h, ANY, patterns, steps, ANY, ANY, 1 << 50, ANY, ANY, None, None)
+
+
+def buffers(logged):
+    return {l[k] for l in logged for k in ("items", "joins", "step_items", "values", "partial", "state") if l[k]}
+
+
+# one genome that is stepped at 64 patterns and not at 96, among smaller ones
+STEPPED = ([1000] + [200] * 100, [100000] + [9000] * 100)
+
+
+def contents(lib, p):
+    return C.string_at(p, min(lib.fake_size(p), MB))
+
+
+@pytest.mark.parametrize("later", ["fewer patterns", "more patterns", "many numbers of patterns"])
+def test_what_a_captured_call_uses_stays(lib, later):
+    """A captured call names its tables and buffers in every replay: no later call on the handle replaces or
+    rewrites them, whether it needs larger ones (which calls on fewer patterns may) or leaves more than 64
+    numbers of patterns behind, and none serves another handle."""
+    h = networks(*STEPPED)
+    for f in (keep, back):
+        assert f(h, 96) == 0, lib.emr_last_error()
+    at = lib.fake_launches()
+    lib.fake_capturing(1)
+    for f in (keep, back):
+        assert f(h, 96) == 0, lib.emr_last_error()
+    lib.fake_capturing(0)
+    used = buffers(launches(lib, at))
+    tables = {l[k] for l in launches(lib, at) for k in ("items", "joins", "step_items") if l[k]}
+    assert len(used) >= 5
+    was = {p: contents(lib, p) for p in tables}
+    for patterns in {"fewer patterns": [64], "more patterns": [3000],
+                     "many numbers of patterns": range(1, 80)}[later]:
+        for f in (keep, back):
+            assert f(h, patterns) == 0, lib.emr_last_error()
+    other = networks(*STEPPED)
+    at = lib.fake_launches()
+    for patterns in (96, 64, 20):
+        for f in (keep, back):
+            assert f(other, patterns) == 0, lib.emr_last_error()
+    assert not used & buffers(launches(lib, at))
+    for p in used & tables:
+        assert contents(lib, p) == was[p]
+    # and the same call again names the same tables
+    at = lib.fake_launches()
+    assert keep(h, 96) == 0 and back(h, 96) == 0
+    assert {l[k] for l in launches(lib, at) for k in ("items", "joins", "step_items") if l[k]} == tables
+    for x in (other, h):
+        lib.emr_free_networks(x)
+
+
+def test_states_that_a_captured_activation_uses_stay(lib):
+    """emr_activate's stepwise states, and the kept activation's of genomes larger than a workgroup's memory,
+    are one buffer of the handle."""
+    h = networks([20000], [19999])
+    x = np.zeros((8, 1), np.float32)
+    for capture in (0, 1):
+        lib.fake_capturing(capture)
+        at = lib.fake_launches()
+        assert lib.emr_activate(h, x.ctypes.data, 8, 2, ANY, None) == 0
+    lib.fake_capturing(0)
+    used = {l["state"] for l in launches(lib, at) if l["step"] == 9}
+    assert len(used) == 1
+    assert keep(h, 100) == 0
+    other = networks([20000], [19999])
+    at = lib.fake_launches()
+    assert lib.emr_activate(other, x.ctypes.data, 8, 2, ANY, None) == 0
+    assert not used & buffers(launches(lib, at))
+    for v in (other, h):
+        lib.emr_free_networks(v)
+
+
+def test_a_capture_that_would_need_new_buffers_is_refused(lib):
+    """Under capture a call lays nothing out and allocates nothing: it is refused, with nothing enqueued, until
+    the same call has run once."""
+    h = networks(STEPPED[0] + [20000], STEPPED[1] + [30000])
+    lib.fake_capturing(1)
+    for f in (keep, back):
+        held, at = lib.fake_held(), lib.fake_launches()
+        assert f(h, 96) == E.EMR_E_DEVICE
+        assert b"capture" in lib.emr_last_error()
+        assert (lib.fake_held(), lib.fake_launches()) == (held, at)
+    lib.fake_capturing(0)
+    assert keep(h, 96) == 0
+    lib.fake_capturing(1)
+    held, at = lib.fake_held(), lib.fake_launches()
+    assert keep(h, 97) == E.EMR_E_DEVICE  # another number of patterns
+    assert back(h, 96) == E.EMR_E_DEVICE  # the derivatives' buffers
+    assert (lib.fake_held(), lib.fake_launches()) == (held, at)
+    lib.fake_capturing(0)
+    assert back(h, 96) == 0
+    lib.fake_capturing(1)
+    assert keep(h, 96) == 0 and back(h, 96) == 0
+    lib.fake_capturing(0)
+    lib.emr_free_networks(h)
+
+
+def test_the_plan_in_use_stays_among_many(lib):
+    """Of more than 64 numbers of patterns, the one used longest ago is laid out anew, not the oldest."""
+    h = networks([30], [100])
+    out = (C.c_int32 * 3)()
+    for patterns in range(1, 120):
+        assert keep(h, patterns) == 0
+        lib.fake_counts(out)
+        waits = out[0]
+        assert keep(h, 1) == 0
+        lib.fake_counts(out)
+        assert out[0] == waits
+    lib.emr_free_networks(h)
