@@ -521,7 +521,7 @@ emr_status emr_load_networks(const emr_source* substrate, int32_t n_substrate, i
                              emr_networks** out, void* stream);
 
 /* The weights of every edge (device, [edges], in the order of in_w) for the calls after this one on
- * `stream`. Enqueued. */
+ * `stream`. Enqueued; captured, every replay sets them. */
 emr_status emr_networks_set_weights(const emr_networks* net, const float* w, void* stream);
 
 /*

@@ -305,6 +305,7 @@ struct emr_networks {
   // number of patterns; partial sums, and a larger genome's derivatives
   struct Learning {
     bool laid = false;
+    bool weights_apart = false;  // a graph of before sets the handle's weights, not the layouts' copies
     Dev ent[emr::kSets], edge[emr::kSets], slices[emr::kSets], rows[emr::kSets], n_slices, n_heavy, n_places;
     Dev place, slice, fits, large, edge_dst, out_offset, out_edge;
     std::vector<uint32_t> fit, big;
@@ -1404,7 +1405,9 @@ void step_args(const emr_networks& N, const emr_networks::Learning::Plan& plan, 
 }
 
 // The items' launches (step: 24 activation, 25 gradients).
-emr_status run_items(const emr_networks::Learning::Plan& plan, emr::LearnArgs& A, int step, hipStream_t s) {
+emr_status run_items(emr_networks& N, const emr_networks::Learning::Plan& plan, emr::LearnArgs& A, int step,
+                     hipStream_t s) {
+  if (N.learn.weights_apart) NET_TRY(lay_weights(N, s));
   for (const auto& r : plan.runs) {
     A.first_item = r.first;
     A.n_items = r.count;
@@ -1425,7 +1428,7 @@ emr_status run_keep(emr_networks& N, const float* inputs, int32_t n_patterns, in
   const uint32_t pblocks = ((uint32_t)n_patterns + 3) / 4;
   const size_t half = (size_t)pblocks * (size_t)N.nodes * 16;
   if (!big.empty()) NET_TRY(grow_outside(N, N.state, 2 * half, "node states", s, captured));
-  NET_TRY(run_items(*plan, A, 24, s));
+  NET_TRY(run_items(N, *plan, A, 24, s));
   if (plan->steps.count > 0) {
     int swap = 0;
     for (int32_t t = 1; t <= steps; ++t, swap ^= 1) {
@@ -1495,7 +1498,7 @@ emr_status run_backward(emr_networks& N, const float* inputs, int32_t n_patterns
   A.grad_outputs = grad_outputs;
   A.grad_w = grad_w;
   A.grad_inputs = grad_inputs;
-  NET_TRY(run_items(*plan, A, 25, s));
+  NET_TRY(run_items(N, *plan, A, 25, s));
   if (plan->steps.count > 0) {
     int swap = 0;
     for (int32_t t = steps; t >= 1; --t, swap ^= 1) {
@@ -1823,6 +1826,7 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
   hipStream_t s = (hipStream_t)stream;
   if (net->edges > 0)
     NET_HIP(hipMemcpyAsync(M.in_w.p, w, (size_t)net->edges * 4, hipMemcpyDeviceToDevice, s));
+  if (!M.learn.laid && capturing(s)) M.learn.weights_apart = true;
   NET_TRY(lay_weights(M, s));
   return mark_done(M, s);
 }

@@ -436,3 +436,42 @@ def test_graph_beside_other_calls(emr):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want_out) and torch.equal(got, want)
+
+
+def test_weights_set_by_a_graph(emr):
+    """A graph that sets the weights, captured before and after the handle's first learning call: its replays
+    count in the learning calls after them, captured ones too."""
+    a = random_nets(12, [5, 40, 300], 3, 2, 9)
+    x = torch.rand((9, 3), device="cuda")
+    g = torch.randn((3, 9, 2), device="cuda")
+    ws = [torch.tensor(a["w"] * np.float32(f), device="cuda") for f in (1.0, 0.5, -0.25)]
+    want = []
+    for w in ws:
+        net = load(emr, dict(a, w=w.cpu().numpy()))
+        out, kept = net.activate_keep(x, 3)
+        want.append((out, net.activate_backward(x, 3, out, kept, g)[0]))
+    for laid in (False, True):
+        net = load(emr, a)
+        if laid:
+            net.activate_keep(x, 3)
+        w = ws[0].clone()
+        sets, learns = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(sets):
+            net.set_weights(w)
+        out, kept = net.activate_keep(x, 3)
+        net.activate_backward(x, 3, out, kept, g)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(learns):
+            out_g, kept_g = net.activate_keep(x, 3)
+            grad_g, _ = net.activate_backward(x, 3, out_g, kept_g, g)
+        for k in (1, 2, 0, 1):
+            w.copy_(ws[k])
+            sets.replay()
+            out, kept = net.activate_keep(x, 3)
+            grad, _ = net.activate_backward(x, 3, out, kept, g)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[k][0]) and torch.equal(grad, want[k][1])
+            learns.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out_g, want[k][0]) and torch.equal(grad_g, want[k][1])

@@ -85,6 +85,7 @@ def networks(nodes, edges):
 
 
 ANY = 1 << 20  # an aligned address that nothing reads
+ANY_W = np.zeros(1000, np.float32)
 
 
 def keep(h, patterns, steps=3):
@@ -202,3 +203,20 @@ def test_the_plan_in_use_stays_among_many(lib):
         lib.fake_counts(out)
         assert out[0] == waits
     lib.emr_free_networks(h)
+
+
+def test_weights_set_by_a_graph_captured_before_the_layout(lib):
+    """The layouts hold copies of the weights. A graph captured before there were any sets the handle's
+    weights alone, in every replay: the learning calls of that handle then copy them anew."""
+    for first in ("captured", "eager"):
+        h = networks([30, 40], [100, 90])
+        lib.fake_capturing(first == "captured")
+        assert lib.emr_networks_set_weights(h, ANY_W.ctypes.data, None) == 0
+        lib.fake_capturing(0)
+        for f in (keep, back, keep):
+            at = lib.fake_launches()
+            assert f(h, 20) == 0
+            steps = [l["step"] for l in launches(lib, at)]
+            assert (23 in steps) == (first == "captured")
+            assert 23 not in steps or steps.index(23) < steps.index(25 if f is back else 24)
+        lib.emr_free_networks(h)
