@@ -546,7 +546,8 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  * the last 64 such numbers), which lay out edges and work and wait for the stream. Under capture a call that
  * would do that, or that needs a larger buffer, is refused (EMR_E_DEVICE): make the same call once before.
  * The tables and buffers that a captured call uses stay as they are until emr_free_networks, whatever is
- * called after it. Calls on one handle must be ordered on one stream, as emr_activate's.
+ * called after it; the handle must outlive the replays. Calls on one handle must be ordered on one stream, as
+ * emr_activate's.
  * EMR_E_INVAL, EMR_E_CAPACITY (kept_bytes too small), EMR_E_LIMIT, EMR_E_NOMEM, EMR_E_DEVICE.
  */
 emr_status emr_kept_bytes(const emr_networks* net, int32_t n_patterns, int32_t steps, int64_t* bytes);

@@ -955,8 +955,10 @@ emr_status grow_outside(emr_networks& M, Dev& d, size_t bytes, const char* what,
   return EMR_OK;
 }
 
-// The end of the work queued on `s`, which the handle's buffers outlive.
+// The end of the work queued on `s`, which the handle's buffers outlive. (Under capture nothing runs, and an event
+// recorded into the graph could not be waited for: the end of the calls before stays the one that counts.)
 emr_status mark_done(emr_networks& M, hipStream_t s) {
+  if (capturing(s)) return EMR_OK;
   if (!M.done) NET_HIP(hipEventCreateWithFlags(&M.done, hipEventDisableTiming));
   NET_HIP(hipEventRecord(M.done, s));
   M.done_pending = true;

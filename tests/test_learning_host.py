@@ -25,7 +25,8 @@ MB = 1 << 20
 def built(tmp_path_factory):
     at = tmp_path_factory.mktemp("fake")
     path, plain = str(at / "libfake.so"), str(at / "fake_hip.o")
-    subprocess.check_call(FLAGS + ["-Demr_launch_net=emr_launch_net_of_no_kernel", "-c",
+    subprocess.check_call(FLAGS + ["-Demr_launch_net=emr_launch_net_of_no_kernel", "-DhipEventRecord=plain_hipEventRecord",
+                                   "-DhipEventSynchronize=plain_hipEventSynchronize", "-c",
                                    os.path.join(HERE, "shim", "fake_hip.cpp"), "-o", plain])
     subprocess.check_call(FLAGS + ["-shared", "-Wl,-Bsymbolic", plain, os.path.join(HERE, "shim", "fake_learn.cpp")]
                           + [os.path.join(CSRC, s) for s in ("runtime.cpp", "networks.cpp", "plan.cpp", "pack.cpp",
@@ -220,3 +221,22 @@ def test_weights_set_by_a_graph_captured_before_the_layout(lib):
             assert (23 in steps) == (first == "captured")
             assert 23 not in steps or steps.index(23) < steps.index(25 if f is back else 24)
         lib.emr_free_networks(h)
+
+
+def test_a_freed_handle_waits_for_the_calls_before_a_capture(lib):
+    """The handle's buffers go back to the cache once the last call that ran has ended, whatever was captured
+    after it (an event recorded into a graph cannot be waited for)."""
+    h = networks([30], [100])
+    assert keep(h, 5) == 0
+    lib.fake_hold_events(1)
+    assert keep(h, 5) == 0
+    lib.fake_capturing(1)
+    assert keep(h, 5) == 0
+    lib.fake_capturing(0)
+    out = (C.c_int32 * 3)()
+    lib.fake_counts(out)
+    waits = out[0]
+    lib.emr_free_networks(h)
+    lib.fake_counts(out)
+    assert out[0] == waits + 1
+    lib.fake_hold_events(0)
