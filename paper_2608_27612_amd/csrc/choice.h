@@ -32,6 +32,7 @@ struct SampleArgs {
   int32_t* index;       // [rows * draws]
   float* logp;          // [rows * draws] or NULL
   uint32_t part;        // entries of a part of a row
+  int64_t first;        // a launch's first row
 };
 
 struct LossArgs {

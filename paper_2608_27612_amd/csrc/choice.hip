@@ -853,7 +853,7 @@ __device__ __forceinline__ void draw_listed(const SampleArgs& A, const RowRule& 
   }
 }
 
-// A workgroup for a row (blockIdx.x), and for a share of its draws (blockIdx.y). Memory: the row once
+// A workgroup for a row (blockIdx.x, from A.first on), and for a share of its draws (blockIdx.y). Memory: the row once
 // (J > 0); else for its maximum, for the limits' bins and for the parts' sums, and once more for each division of
 // a crowded bin. 256 rows of 131072 float scores, top-p: 109 us, 1.2 TB/s of the scores read once (each is read
 // three times); 256 rows of 2485, all filters: 15 us, latency.
@@ -864,7 +864,7 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   __shared__ RowShared<NT, PARTS> S;
   constexpr int kBins = 2 * NT;
   const uint32_t lane = threadIdx.x % kWave;
-  const int64_t r = blockIdx.x, d0 = r * A.draws;
+  const int64_t r = A.first + blockIdx.x, d0 = r * A.draws;
   Row<TYPE, NT, J> row(A, static_cast<const T*>(A.x) + r * A.stride);
   float m = block_max<NT>(row.load(), S);
   if (m > 3.402823466e38f) {
@@ -1190,6 +1190,9 @@ __global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A)
   }
 }
 
+// Workgroups of a launch, at most: its threads in a dimension are a 32-bit number.
+constexpr int64_t most_groups(int threads) { return 0xFFFFFFFFll / threads; }
+
 template <int TYPE, int G>
 void launch_short(const SampleArgs& A, hipStream_t s) {
   const int64_t b = (A.rows + 256 / G - 1) / (256 / G);
@@ -1198,9 +1201,12 @@ void launch_short(const SampleArgs& A, hipStream_t s) {
 template <int TYPE, int NT, int J>
 void launch_row(const SampleArgs& A, hipStream_t s) {
   // (every workgroup of a row finds its limits anew: shares of several draws for each thread, or wave)
-  const int64_t per = J > 0 ? 8 * NT : 4 * NT, y = (A.draws + per - 1) / per;
-  hipLaunchKernelGGL((k_sample_row<TYPE, NT, J>), dim3((uint32_t)A.rows, (uint32_t)(y < 256 ? y : 256)), dim3(NT),
-                     0, s, A);
+  const int64_t per = J > 0 ? 8 * NT : 4 * NT, y = (A.draws + per - 1) / per, most = most_groups(NT);
+  for (SampleArgs B = A; B.first < A.rows; B.first += most) {
+    const int64_t rows = A.rows - B.first < most ? A.rows - B.first : most;
+    hipLaunchKernelGGL((k_sample_row<TYPE, NT, J>), dim3((uint32_t)rows, (uint32_t)(y < 256 ? y : 256)), dim3(NT), 0,
+                       s, B);
+  }
 }
 template <int TYPE>
 void launch_sample(const SampleArgs& A, hipStream_t s) {

@@ -248,6 +248,28 @@ def test_strides_and_shared_rows(emr):
     check(emr, long.expand(9, 6000), v.expand(9, 3).contiguous(), k=30)
 
 
+@pytest.mark.parametrize("n,rows", [(65, (1 << 24) + 5), (8190, (1 << 22) + 5)])
+def test_more_rows_than_a_launch_takes(emr, n, rows):
+    """Rows (all the same one) beyond what workgroups of 256 and of 1024 threads in one launch cover: each
+    draws as the row alone does."""
+    x, _ = scores(n, 1, n)
+    u = torch.rand((rows, 1), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    index, logp = emr.emr_sample(x.expand(rows, n), u, top_p=0.9)
+    _, q, y = whole(x, u[:1], p=0.9)
+    run = q[0].cumsum(0)
+    want = torch.searchsorted(run, (u[:, 0].double() * run[-1].double()).long().clamp(max=int(run[-1]) - 1),
+                              right=True)
+    assert torch.equal(index[:, 0], want.int())
+    lp = (y[0].double() - torch.log(run[-1].double() / 2.0 ** 31))[want]
+    assert ((logp[:, 0].double() - lp).abs() <= 1e-12 + 2.0 ** -23 * lp.abs()).all()
+    k = torch.full((rows,), 1, dtype=torch.int32, device="cuda")  # (settings by row: the last one is its own)
+    k[-1] = 0
+    index, _ = emr.emr_sample(x.expand(rows, n), u.fill_(1 - 2.0 ** -24), top_k=k)
+    _, q, _ = whole(x, u[:1])
+    assert (index[:-1] == x[0].argmax()).all()
+    assert int(index[-1]) == int(q[0].nonzero().max())
+
+
 def test_another_stream_and_graph(emr):
     """On a stream of its own, and captured: replays draw from what the scores then hold."""
     s = torch.cuda.Stream()
