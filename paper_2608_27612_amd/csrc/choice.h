@@ -46,6 +46,7 @@ struct LossArgs {
   float* loss;           // [rows] or NULL
   void* grad;            // [rows] rows of n, grad_stride entries apart, of x's type; or NULL
   int64_t grad_stride;
+  int64_t first;         // a launch's first row
 };
 
 }  // namespace emr

@@ -1082,7 +1082,7 @@ __global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A)
   __shared__ float mpart[NT / kWave];
   __shared__ double spart[NT / kWave];
   const uint32_t tid = threadIdx.x % NT;
-  const int64_t r = (int64_t)blockIdx.x * (NT == kWave ? 4 : 1) + threadIdx.x / NT;
+  const int64_t r = A.first + (int64_t)blockIdx.x * (NT == kWave ? 4 : 1) + threadIdx.x / NT;
   if (r >= A.rows) return;  // (a wave's row)
   const T* row = static_cast<const T*>(A.x) + r * A.stride;
   T* grad = A.grad ? static_cast<T*>(A.grad) + r * A.grad_stride : const_cast<T*>(row);  // (unused)
@@ -1229,8 +1229,12 @@ void launch_loss_short(const LossArgs& A, hipStream_t s) {
 }
 template <int TYPE, int NT, int J>
 void launch_loss_row(const LossArgs& A, hipStream_t s) {
-  const int64_t b = NT == kWave ? (A.rows + 3) / 4 : A.rows;
-  hipLaunchKernelGGL((k_loss_row<TYPE, NT, J>), dim3((uint32_t)b), dim3(NT == kWave ? 256 : NT), 0, s, A);
+  constexpr int threads = NT == kWave ? 256 : NT, each = threads / NT;
+  constexpr int64_t most = most_groups(threads) * each;
+  for (LossArgs B = A; B.first < A.rows; B.first += most) {
+    const int64_t rows = A.rows - B.first < most ? A.rows - B.first : most;
+    hipLaunchKernelGGL((k_loss_row<TYPE, NT, J>), dim3((uint32_t)((rows + each - 1) / each)), dim3(threads), 0, s, B);
+  }
 }
 template <int TYPE>
 void launch_loss(const LossArgs& A, hipStream_t s) {

@@ -414,3 +414,26 @@ def test_loss_nothing_and_in_place(emr):
                                              emr._stream_ptr()))
         torch.cuda.synchronize()
         assert torch.equal(y, grad) and torch.equal(out, loss)
+
+
+@pytest.mark.parametrize("n,rows", [(65, (1 << 26) + 5), (2000, (1 << 24) + 5), (20000, (1 << 23) + 5),
+                                    (33000, (1 << 22) + 5)])
+def test_loss_of_more_rows_than_a_launch_takes(emr, n, rows):
+    """Rows (all the same one) beyond what one launch covers by waves, workgroups of 256, of 512 and of 1024
+    threads: each row's loss is the one of a few rows alone, for its own index."""
+    import ctypes as C
+    x, _ = scores(n, 1, n, "bf16", mask=False)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    picks = torch.randint(0, n, (7,), generator=g, device="cuda", dtype=torch.int32)
+    few, grad = emr.emr_answer_loss(x.expand(7, n), picks, temperature=0.5)
+    want, _ = loss64(x.expand(7, n), picks, torch.ones(7, device="cuda"), 0.5)
+    bound, _ = loss_bounds(x.expand(7, n), n, torch.ones(7, device="cuda"), 0.5, want, grad.double(), "bf16")
+    assert ((few.double() - want).abs() <= bound).all()
+    at = torch.arange(rows, device="cuda") % 7
+    index = picks[at]
+    index[1::1000] = -1
+    loss = torch.full((rows,), -1.0, device="cuda")
+    st = emr.emr_scores(x.data_ptr(), emr.EMR_BF16, rows, n, 0)
+    emr._check(emr.lib().emr_answer_loss(C.byref(st), index.data_ptr(), None, C.c_float(0.5), loss.data_ptr(), None,
+                                         0, emr._stream_ptr()))
+    assert torch.equal(loss, torch.where(index < 0, 0.0, few[at]))
