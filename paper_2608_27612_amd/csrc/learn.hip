@@ -996,6 +996,12 @@ __global__ void __launch_bounds__(kNetThreads) k_kept_values(KeptValuesArgs A) {
   }
 }
 
+// f(first, count) for shares of n workgroups: a launch's threads in a dimension are a 32-bit number.
+template <typename F>
+void launches(uint32_t n, uint32_t threads, F&& f) {
+  const uint32_t most = 0xFFFFFFFFu / threads;
+  for (uint64_t a = 0; a < n; a += most) f((uint32_t)a, n - (uint32_t)a < most ? n - (uint32_t)a : most);
+}
 uint32_t stride_blocks(int64_t n) {
   const int64_t b = (n + kNetThreads - 1) / kNetThreads;
   return (uint32_t)(b < 1 ? 1 : (b > 16384 ? 16384 : b));
@@ -1027,7 +1033,11 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       const auto& A = *static_cast<const LearnLayoutArgs*>(args);
       if (A.count == 0) return hipSuccess;
       hipLaunchKernelGGL(k_layout_degrees, dim3(stride_blocks(A.nodes * kWave)), blk, 0, s, A);
-      hipLaunchKernelGGL(k_layout_slices, dim3(A.count), dim3(kLayoutThreads), 0, s, A);
+      launches(A.count, kLayoutThreads, [&](uint32_t a, uint32_t n) {
+        LearnLayoutArgs B = A;
+        B.genomes = A.genomes + a;
+        hipLaunchKernelGGL(k_layout_slices, dim3(n), dim3(kLayoutThreads), 0, s, B);
+      });
       // (about 4096 workgroups over the genomes, a wave to a node)
       const uint32_t x = A.count < 4096u ? 4096u / A.count : 1u;
       for (uint32_t a = 0; a < A.count; a += 65535u) {
@@ -1054,10 +1064,14 @@ extern "C" hipError_t emr_launch_learn(int step, const void* args, hipStream_t s
       if (A.n_items == 0) return hipSuccess;
       if (A.lds_bytes > kLearnLds || A.threads == 0 || A.threads > 1024u || A.threads % kWave != 0)
         return hipErrorInvalidValue;
-      if (step == 4)
-        hipLaunchKernelGGL(k_learn<false>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
-      else
-        hipLaunchKernelGGL(k_learn<true>, dim3(A.n_items), dim3(A.threads), A.lds_bytes, s, A);
+      launches(A.n_items, A.threads, [&](uint32_t a, uint32_t n) {
+        LearnArgs B = A;
+        B.first_item = A.first_item + a;
+        if (step == 4)
+          hipLaunchKernelGGL(k_learn<false>, dim3(n), dim3(A.threads), A.lds_bytes, s, B);
+        else
+          hipLaunchKernelGGL(k_learn<true>, dim3(n), dim3(A.threads), A.lds_bytes, s, B);
+      });
       break;
     }
     case 6: {

@@ -475,3 +475,21 @@ def test_weights_set_by_a_graph(emr):
             learns.replay()
             torch.cuda.synchronize()
             assert torch.equal(out_g, want[k][0]) and torch.equal(grad_g, want[k][1])
+
+
+def test_more_genomes_than_a_launch_takes(emr):
+    """2^23 + 3 genomes of one edge, beyond what workgroups of one launch cover: their layouts, activation and
+    gradients (sigmoid(w x), whatever the steps)."""
+    G = (1 << 23) + 3
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("not enough free device memory")
+    w = np.linspace(-2, 2, G).astype(np.float32)
+    net = emr.emr_load_networks(substrate(1, 1), 2 * np.arange(G + 1), np.arange(2 * G + 1) // 2, 2 * np.arange(G), w)
+    x = torch.tensor([[0.5], [-1.0]], device="cuda")
+    out, kept = net.activate_keep(x, 2)
+    want = torch.sigmoid(torch.tensor(w, device="cuda").double()[:, None, None] * x.double())
+    # (the product's rounding, times the slope of at most 1 / 4, and the sigmoid's few of its own)
+    assert (out.double() - want).abs().max() < 2.0 ** -21
+    grad, _ = net.activate_backward(x, 2, out, kept, torch.ones_like(out))
+    want = (want * (1 - want) * x.double()).sum((1, 2))
+    assert (grad.double() - want).abs().max() < 2.0 ** -20
