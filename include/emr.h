@@ -540,6 +540,10 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  *   - The gradient is the one of the activation with each state replaced by c / 255 in both places where it
  *     occurs (the product with a weight's derivative, and s (1 - s)), in fp32; every sum has a fixed
  *     order, so a handle's gradients are the same bits on every call.
+ *   - Memory that a handle keeps from its first call of the two on: the edges laid out four times (about 100
+ *     bytes an edge, and at least 10 KB a genome); partial sums and states, 2 GiB at most beyond one copy of
+ *     each genome's (about 8 bytes an edge), whatever the number of patterns; for networks too large or too few
+ *     for that, three floats (four, above 10239 nodes) for each of their nodes and patterns.
  *   - A weight that `steps` steps do not let reach an output has derivative 0. A node that no derivative
  *     reaches adds nothing, whatever its states.
  * Enqueued on `stream`, but for a handle's first call of the two, and its first on a number of patterns (of

@@ -1116,6 +1116,11 @@ constexpr double kLearnItems = 32768.0;
 // Copies of a stepped genome's sums, at most. (Three of 5000 to 9000 nodes, a step: 50 us with a copy for each of
 // 16 blocks of patterns, 58 with eight, 67 with four: fewer leave longer workgroups.)
 constexpr uint32_t kStepGroups = 64;
+// Bytes of the items' sums and of their values outside LDS, beyond the one item that a genome has at least: where
+// more items would take more, there are fewer, longer ones. (Gradients of 150 networks of up to 773 hidden nodes on
+// 10000 patterns: 22.9 ms at 64 MiB, 10.9 at 256 MiB, 8.8 at 2 GiB, 8.6 at 4 GiB; of 300 of 4000 on 100 patterns 13.7,
+// 13.7, 10.1 and 10.3.)
+constexpr double kLearnBytes = 2147483648.0;
 constexpr size_t kLearnPlans = 64;  // numbers of patterns whose items a handle keeps
 
 void learn_sets(emr_networks& N, emr::LearnSet* out) {
@@ -1272,12 +1277,46 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
     const Shape local = shape_of(g, id - 1);
     return local.lds <= kHalf ? local : shape_of(g, id);
   };
+  auto step_shape = [&](uint32_t g) {
+    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
+    while (id > 1 && shape_of(g, id).lds > emr::kLearnLds) id -= 2;
+    return shape_of(g, id);
+  };
   auto load = [&](uint32_t g) { return (double)edges(g) + 8.0 * (double)nodes(g); };
+  auto stride_of = [&](uint32_t g) { return emr::learn_sums(nodes(g), edges(g)); };
+  auto values_of = [&](uint32_t g, const Shape& S) {
+    const emr::LearnShape& f = emr::kLearnShapes[S.id];
+    return f.local ? 0 : 2 * (nodes(g) + 1) * (int64_t)f.lanes;
+  };
+  struct Share {
+    uint32_t g;
+    Shape S;
+    uint32_t n;    // items of it (stepped: groups of blocks, each with sums of its own)
+    bool stepped;
+  };
+  std::vector<Share> fit;
   double total = 0.0;
-  for (uint32_t g : L.fit) total += load(g) * shape(g).blocks;
-  // A genome is stepped of which one block is longer work than a compute unit's share of all,
-  // and than its steps' launches (8192 edges: about 12 us a step).
-  auto stepped = [&](uint32_t g) { return load(g) > std::max(total / 256.0, 8192.0); };
+  for (uint32_t g : L.fit) {
+    fit.push_back({g, shape(g), 1, false});
+    total += load(g) * fit.back().S.blocks;
+  }
+  // As many items as a genome's load asks for, and as there is memory for.
+  double bytes = 0.0;
+  for (Share& f : fit) {
+    f.n = (uint32_t)std::min<double>(
+        f.S.blocks, std::max(1.0, std::ceil(load(f.g) * f.S.blocks * kLearnItems / std::max(total, 1.0))));
+    bytes += (f.n - 1.0) * (4.0 * (double)stride_of(f.g) + 16.0 * (double)values_of(f.g, f.S));
+  }
+  const double part_of = bytes > kLearnBytes ? kLearnBytes / bytes : 1.0;
+  for (Share& f : fit) {
+    f.n = 1u + (uint32_t)((f.n - 1.0) * part_of);
+    // A genome is stepped of which one item is longer work than a compute unit's share of all,
+    // and than its steps' launches (8192 edges: about 12 us a step).
+    f.stepped = load(f.g) * f.S.blocks > f.n * std::max(total / 256.0, 8192.0);
+    if (!f.stepped) continue;
+    f.S = step_shape(f.g);
+    f.n = std::min({f.n, f.S.blocks, kStepGroups});
+  }
   std::vector<emr::LearnItem> items;
   std::vector<emr::LearnJoin> joins;
   int64_t part = 0;
@@ -1285,20 +1324,17 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   for (const bool whole : {true, false}) {
     std::vector<std::pair<double, emr::LearnItem>> by;
     emr_networks::Learning::Run run{(uint32_t)items.size(), 0, 1024, 0};
-    for (uint32_t g : L.fit) {
-      const Shape S = shape(g);
-      if (stepped(g) || (S.lds > kHalf) != whole) continue;
-      const emr::LearnShape& f = emr::kLearnShapes[S.id];
+    for (const auto& [g, S, n, stepped] : fit) {
+      if (stepped || (S.lds > kHalf) != whole) continue;
       run.lds = std::max(run.lds, S.lds);
-      const uint32_t n = (uint32_t)std::min<double>(
-          S.blocks, std::max(1.0, std::ceil(load(g) * S.blocks * kLearnItems / std::max(total, 1.0))));
-      const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
+      const uint32_t lanes = emr::kLearnShapes[S.id].lanes;
+      const int64_t stride = stride_of(g);
       if (n > 1) joins.push_back({g, n, part, stride});
       for (uint32_t k = 0; k < n; ++k, part += stride) {
         const uint32_t b0 = (uint32_t)((uint64_t)S.blocks * k / n), b1 = (uint32_t)((uint64_t)S.blocks * (k + 1) / n);
-        by.push_back({-load(g) * f.lanes * (b1 - b0),
+        by.push_back({-load(g) * lanes * (b1 - b0),
                       {g, b0, b1, (uint16_t)S.id, (uint16_t)(n == 1), part, plan->scratch}});
-        if (!f.local) plan->scratch += 2 * (nodes(g) + 1) * f.lanes;
+        plan->scratch += values_of(g, S);
       }
     }
     if (by.empty()) continue;
@@ -1311,23 +1347,16 @@ emr_status plan_items(emr_networks& N, int32_t n_patterns, emr_networks::Learnin
   }
   // Stepped genomes: a workgroup for each compute unit (its LDS holds no second one), no more.
   std::vector<emr::LearnStepItem> steps;
-  auto step_shape = [&](uint32_t g) {
-    int id = n_patterns <= 4 ? 1 : (n_patterns <= 8 ? 3 : (n_patterns <= 16 ? 5 : 7));
-    while (id > 1 && shape_of(g, id).lds > emr::kLearnLds) id -= 2;
-    return shape_of(g, id);
-  };
   double all = 0.0;
-  for (uint32_t g : L.fit)
-    if (stepped(g)) all += load(g) * step_shape(g).blocks;
-  for (uint32_t g : L.fit) {
-    if (!stepped(g)) continue;
-    const Shape S = step_shape(g);
+  for (const Share& f : fit)
+    if (f.stepped) all += load(f.g) * f.S.blocks;
+  for (const auto& [g, S, groups, stepped] : fit) {
+    if (!stepped) continue;
     const uint32_t lanes = emr::kLearnShapes[S.id].lanes;
     const uint32_t units = (uint32_t)(nodes(g) * lanes / 64) + 1;
     const double share = 256.0 * load(g) * S.blocks / std::max(all, 1.0);
-    const uint32_t groups = std::min(S.blocks, kStepGroups);
     const uint32_t chunks = (uint32_t)std::min<double>(std::max(1u, units / 8), std::max(1.0, share / groups));
-    const int64_t stride = 2 * emr::learn_places(nodes(g), edges(g), N.n_out);
+    const int64_t stride = stride_of(g);
     joins.push_back({g, groups, part, stride});
     plan->steps.lds = std::max(plan->steps.lds, S.lds);
     for (uint32_t k = 0; k < groups; ++k, part += stride)

@@ -38,6 +38,9 @@ void fake_launch(int64_t i, int64_t* out) {
   for (int k = 0; k < 10; ++k) out[k] = v[k];
 }
 
+int64_t fake_sums(int64_t n, int64_t e) { return emr::learn_sums(n, e); }
+uint32_t fake_light_edges(uint32_t edges, uint32_t rows) { return emr::light_edges(edges, rows); }
+
 hipError_t plain_hipEventRecord(hipEvent_t e, hipStream_t s);
 hipError_t plain_hipEventSynchronize(hipEvent_t e);
 hipError_t hipEventRecord(hipEvent_t e, hipStream_t s) {

@@ -493,3 +493,54 @@ def test_more_genomes_than_a_launch_takes(emr):
     grad, _ = net.activate_backward(x, 2, out, kept, torch.ones_like(out))
     want = (want * (1 - want) * x.double()).sum((1, 2))
     assert (grad.double() - want).abs().max() < 2.0 ** -20
+
+
+def test_many_patterns_of_large_genomes(emr):
+    """More items than their sums' memory leaves room for (40 genomes of 4000 hidden nodes, 6000 patterns): the
+    gradients of the first and the last genome against 64 bits."""
+    G, m, deg, P, steps = 40, 4000, 60, 6000, 3
+    n = m + 3
+    rng = np.random.default_rng(0)
+    d = np.array([0, 0, m] + [deg] * m)
+    src = [np.concatenate([g * n + 3 + np.arange(m), g * n + np.sort(rng.integers(0, n, (m, deg)), axis=1).ravel()])
+           for g in range(G)]
+    a = {"subs": substrate(2, 1), "node_offset": n * np.arange(G + 1),
+         "in_offset": np.concatenate([[0], np.cumsum(np.tile(d, G))]), "src": np.concatenate(src),
+         "w": (rng.standard_normal(G * d.sum()) / 8).astype(np.float32)}
+    net = load(emr, a)
+    x = torch.rand((P, 2), device="cuda") * 2 - 1
+    out, kept = net.activate_keep(x, steps)
+    grad_out = torch.randn((G, P, 1), device="cuda") / P
+    gw, gx = net.activate_backward(x, steps, out, kept, grad_out, grad_inputs=True)
+    again, _ = net.activate_backward(x, steps, out, kept, grad_out)
+    assert torch.equal(gw, again)
+    e = int(d.sum())
+    eps = unit(steps, max(P, m))
+    to = torch.tensor(np.repeat(np.arange(n), d), device="cuda")
+    for g in (0, G - 1):
+        own = torch.tensor(src[g] - g * n, device="cuda")
+        w = torch.zeros((n, n), dtype=torch.float64, device="cuda")
+        w.index_put_((to, own), torch.tensor(a["w"][g * e:(g + 1) * e], device="cuda").double(), accumulate=True)
+        # (the sizes of an edge's terms: of each of several edges between the same two nodes apart)
+        size = torch.zeros_like(w).index_put_((to, own), torch.tensor(np.abs(a["w"][g * e:(g + 1) * e]),
+                                                                     device="cuda").double(), accumulate=True)
+        codes = kept.values()[:, g * n:(g + 1) * n].double()
+        z = torch.zeros((n, P), dtype=torch.float64, device="cuda")
+        o = out[g, :, 0].double()
+        z[2] = grad_out[g, :, 0].double() * o * (1 - o)
+        za, gm, ga = z.abs(), torch.zeros_like(w), torch.zeros_like(w)
+        xs = torch.zeros((2, P), dtype=torch.float64, device="cuda")
+        xa = xs.clone()
+        for t in range(steps, 0, -1):
+            s = codes[t - 2].clone() if t > 1 else torch.zeros_like(z)
+            s[:2] = x.double().t()
+            gm += z @ s.t().contiguous()
+            ga += za @ s.abs().t().contiguous()
+            back, size_back = w.t().contiguous() @ z, size.t().contiguous() @ za
+            xs += back[:2]
+            xa += size_back[:2]
+            z, za = back * s * (1 - s), size_back * s * (1 - s)
+            z[:2], za[:2] = 0, 0
+        got = gw[g * e:(g + 1) * e].double()
+        assert ((got - gm[to, own]).abs() <= eps * ga[to, own] + 1e-30).all()
+        assert ((gx[g].double().t() - xs).abs() <= eps * xa + 1e-30).all()

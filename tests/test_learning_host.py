@@ -46,7 +46,9 @@ def lib(built, tmp_path):
     for name, (res, args) in {"fake_capturing": (None, [C.c_int]), "fake_held": (C.c_int64, []),
                               "fake_hold_events": (None, [C.c_int]), "fake_counts": (None, [C.c_void_p]),
                               "fake_size": (C.c_int64, [C.c_void_p]), "fake_launches": (C.c_int64, []),
-                              "fake_launch": (None, [C.c_int64, C.c_void_p])}.items():
+                              "fake_launch": (None, [C.c_int64, C.c_void_p]),
+                              "fake_sums": (C.c_int64, [C.c_int64, C.c_int64]),
+                              "fake_light_edges": (C.c_uint32, [C.c_uint32, C.c_uint32])}.items():
         fn = getattr(L, name)
         fn.restype, fn.argtypes = res, args
     yield L
@@ -240,3 +242,60 @@ def test_a_freed_handle_waits_for_the_calls_before_a_capture(lib):
     lib.fake_counts(out)
     assert out[0] == waits + 1
     lib.fake_hold_events(0)
+
+
+@pytest.mark.parametrize("nodes,edges,patterns", [
+    ([4000] * 40, [240000] * 40, 10000), ([4000] * 40, [240000] * 40, 65536), ([773] * 150, [40000] * 150, 65536),
+    ([5000], [20000000], 65536), ([5000], [20000000], 600), ([1000] + [200] * 100, [100000] + [9000] * 100, 64)])
+def test_workspaces_have_a_bound(lib, nodes, edges, patterns):
+    """The gradients' partial sums and the states outside LDS take 2 GiB and a copy of the genomes' own at most
+    (the states of genomes with a launch for each step: three float arrays), however many patterns there are."""
+    h = networks(nodes, edges)
+    at = lib.fake_launches()
+    assert back(h, patterns) == 0, lib.emr_last_error()
+    logged = launches(lib, at)
+    partial, = {l["partial"] for l in logged if l["partial"]}
+    one = sum(4 * lib.fake_sums(n, e) for n, e in zip(nodes, edges))
+    values = sum(3 * 4 * n * -(-patterns // 32) * 32 + 2 * 16 * 8 * (n + 1) for n in nodes)
+    # (the stand-in hands out whole pages, the cache buffers of up to twice the size)
+    assert 0 < lib.fake_size(partial) <= (2 << 30) + one + 4096
+    if any(l["step"] == 32 for l in logged):
+        v, = {l["values"] for l in logged if l["step"] == 32}
+        assert lib.fake_size(v) <= values + (2 << 30) + 4096
+    assert sum(l["count"] for l in logged if l["step"] in (25, 32)) >= 256 or patterns < 256
+    lib.emr_free_networks(h)
+
+
+def places(degrees, light_edges):
+    """Places of one layout by source (rows of these numbers of edges), as the slices' kernel lays it out."""
+    d = np.sort(np.asarray(degrees))[::-1]
+    light = light_edges(int(d.sum()), len(d))
+    heavy, rest = d[d > light], d[d <= light]
+    four = lambda v: -(-v // 4) * 4  # noqa: E731
+    return int((16 * four(-(-heavy // 16))).sum() + sum(16 * four(int(rest[i])) for i in range(0, len(rest), 16)))
+
+
+@pytest.mark.parametrize("seed", range(200))
+def test_an_items_sums_hold_both_layouts(lib, seed):
+    """Rows of even, falling, few and single hub degrees, around the borders of the light rows."""
+    rng = np.random.default_rng(seed)
+    sets = []
+    for _ in range(2):
+        n = int(np.exp(rng.uniform(0, np.log(3000))))
+        kind = rng.integers(0, 6)
+        if kind == 0:
+            d = rng.integers(0, rng.choice([2, 20, 70, 2000]), n)
+        elif kind == 1:
+            d = np.minimum(rng.pareto(rng.uniform(0.3, 2.0), n) * 10, 10000).astype(int)
+        elif kind == 2:
+            d = np.zeros(n, int)
+            d[: max(1, n // 100)] = rng.choice([65, 66, 1021, 1022, 5000])
+        elif kind == 3:
+            d = np.full(n, rng.choice([0, 1, 4, 5, 64, 65, 300, 1021, 1022, 1025]))
+        elif kind == 4:
+            d = np.where(np.arange(n) % 16 == 0, rng.choice([17, 64, 65, 400]), rng.choice([0, 1, 16, 64]))
+        else:
+            d = np.where(rng.random(n) < 0.25, 65, 16)
+        sets.append(d)
+    n, e = sum(len(d) for d in sets), int(sum(d.sum() for d in sets))
+    assert sum(places(d, lib.fake_light_edges) for d in sets) <= lib.fake_sums(n, e)
