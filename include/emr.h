@@ -627,7 +627,8 @@ emr_status emr_sample(const emr_scores* scores, const emr_sampling* rule, const 
  * apart, or NULL) its gradient, scale[r] / temperature (softmax(x / temperature) - 1 at index[r]).
  * scale: device, [rows] (an advantage, a weight, a mean's factor), or NULL for 1. Computed in fp32,
  * the gradient rounded once. A row whose index lies outside [0, n), or whose scores are all -inf, has no
- * answer: its loss and gradient are 0. grad may be the scores' own memory. Enqueued on `stream`.
+ * answer: its loss and gradient are 0. grad may be the scores' own memory row by row (the same address and
+ * grad_stride = stride); it must share no entry with them otherwise. Enqueued on `stream`.
  * EMR_E_INVAL, EMR_E_LIMIT, EMR_E_DEVICE.
  */
 emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const float* scale,

@@ -1662,6 +1662,22 @@ emr_status check_scores(const char* who, const emr_scores* S) {
   return EMR_OK;
 }
 
+// Whether `rows` rows of n entries, s apart from 0 on, share an entry with as many from d on, t >= n apart.
+bool rows_meet(int64_t d, int64_t rows, int64_t n, int64_t s, int64_t t) {
+  const int64_t end = (rows - 1) * s + n, last = d + (rows - 1) * t;
+  if (d >= end || last + n <= 0) return false;
+  auto near = [&](int64_t a, int64_t step, int64_t lo, int64_t hi) {  // |a - k step| < n for a k of lo .. hi
+    const int64_t k = a / step - (a % step < 0 ? 1 : 0);
+    for (int64_t j = k; j <= k + 1; ++j)
+      if (j >= lo && j <= hi && a - j * step < n && j * step - a < n) return true;
+    return false;
+  };
+  if (s == t) return near(d, s, 1 - rows, rows - 1);
+  for (int64_t r = 0; r < (s > 0 ? rows : 1); ++r)
+    if (near(r * s - d, t, 0, rows - 1)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1985,6 +2001,10 @@ emr_status emr_answer_loss(const emr_scores* scores, const int32_t* index, const
   if (grad && (uintptr_t)grad % (uintptr_t)type_size(scores->type) != 0)
     return failf(EMR_E_INVAL, "loss: grad is not aligned to its type");
   if (!index) return failf(EMR_E_INVAL, "loss: index is NULL");
+  const int64_t apart = ((intptr_t)grad - (intptr_t)scores->x) / type_size(scores->type);
+  if (grad && !(apart == 0 && (scores->rows == 1 || grad_stride == scores->stride)) &&
+      rows_meet(apart, scores->rows, scores->n, scores->stride, grad_stride))
+    return failf(EMR_E_INVAL, "loss: grad lies over the scores, other than row by row");
   emr::LossArgs a{};
   a.x = scores->x;
   a.stride = scores->stride;

@@ -299,3 +299,22 @@ def test_an_items_sums_hold_both_layouts(lib, seed):
         sets.append(d)
     n, e = sum(len(d) for d in sets), int(sum(d.sum() for d in sets))
     assert sum(places(d, lib.fake_light_edges) for d in sets) <= lib.fake_sums(n, e)
+
+
+@pytest.mark.parametrize("rows,n", [(1, 1), (1, 4), (2, 3), (5, 1), (4, 3), (7, 2)])
+def test_a_gradient_over_the_scores_is_theirs_row_by_row(lib, rows, n):
+    """Every place of the gradient's rows beside the scores' (in entries): refused where an entry of the two is the
+    same one, but for rows that lie on each other. (No kernel runs.)"""
+    x = 1 << 20
+    for type, size in ((E.EMR_F32, 4), (E.EMR_BF16, 2)):
+        for stride in (0, 1, n - 1, n, n + 1, 2 * n, 2 * n + 1, 3 * n):
+            scores = E.emr_scores(x, type, rows, n, stride)
+            mine = {r * stride + k for r in range(rows) for k in range(n)}
+            for grad_stride in (n, n + 1, 2 * n, 3 * n):
+                rest = {r * grad_stride + k for r in range(rows) for k in range(n)}
+                for d in range(-3 * n * rows - 2, 3 * n * rows + 3):
+                    st = lib.emr_answer_loss(C.byref(scores), ANY, None, C.c_float(1.0), ANY, x + d * size,
+                                             grad_stride, None)
+                    same = d == 0 and (rows == 1 or stride == grad_stride)
+                    fits = same or not any(k - d in rest for k in mine)
+                    assert st == (E.EMR_OK if fits else E.EMR_E_INVAL), (stride, grad_stride, d)
