@@ -1034,19 +1034,19 @@ class Networks:
     def set_weights(self, w, stream=None):
         """The weight of every edge (a float32 device tensor in the order of in_w) for later calls."""
         import torch
-        with _On(stream) as raw:
-            w = _on_device("w", w, torch.float32, (self._sizes()[2],)).contiguous()
-            _check(lib().emr_networks_set_weights(self.handle, w.data_ptr(), raw))
+        with _On(stream) as on:
+            w = _on_device(on, "w", w, torch.float32, (self._sizes()[2],)).contiguous()
+            _check(lib().emr_networks_set_weights(self.handle, w.data_ptr(), on.raw))
 
     def weights(self, stream=None):
         """A copy of the edges' weights (numpy, in the order of in_w)."""
         i = self.info()
         return _dev_to_host(i.in_w, i.edges, np.float32, stream)
 
-    def _patterns(self, inputs):
+    def _patterns(self, on, inputs):
         import torch
         n_in = self._sizes()[3]
-        _on_device("inputs", inputs, torch.float32)
+        _on_device(on, "inputs", inputs, torch.float32)
         if inputs.dim() != 2 or inputs.shape[1] != n_in:
             raise ValueError("inputs: shape (patterns, %d) is needed, not %s" % (n_in, tuple(inputs.shape)))
         return inputs.contiguous()
@@ -1055,16 +1055,16 @@ class Networks:
         """Outputs (float32 device tensor [n_genomes, n_patterns, n_outputs]) of emr_activate_keep for
         `inputs` (float32 device tensor [n_patterns, n_inputs]), and the Kept states; not synchronized."""
         import torch
-        with _On(stream) as raw:
+        with _On(stream) as on:
             G, nodes, edges, n_in, n_out = self._sizes()
-            x = self._patterns(inputs)
+            x = self._patterns(on, inputs)
             P = x.shape[0]
             out = torch.empty((G, P, n_out), dtype=torch.float32, device=x.device)
             b = _kept_width(P)
             codes = torch.empty((max(steps - 1, 0), -(-P // b), nodes, b), dtype=torch.uint8,
                                 device=x.device)
             _check(lib().emr_activate_keep(self.handle, x.data_ptr(), P, steps, out.data_ptr(),
-                                           codes.data_ptr(), codes.numel(), raw))
+                                           codes.data_ptr(), codes.numel(), on.raw))
             return out, Kept(codes, P)
 
     def activate_backward(self, inputs, steps: int, outputs, kept, grad_outputs, grad_inputs: bool = False,
@@ -1074,15 +1074,15 @@ class Networks:
         activate_keep's inputs, outputs and Kept and the derivatives by the outputs; see
         emr_activate_backward in include/emr.h. Not synchronized."""
         import torch
-        with _On(stream) as raw:
+        with _On(stream) as on:
             G, nodes, edges, n_in, n_out = self._sizes()
-            x = self._patterns(inputs)
+            x = self._patterns(on, inputs)
             P = x.shape[0]
             shape = (G, P, n_out)
-            outputs = _on_device("outputs", outputs, torch.float32, shape).contiguous()
-            grad_outputs = _on_device("grad_outputs", grad_outputs, torch.float32, shape).contiguous()
+            outputs = _on_device(on, "outputs", outputs, torch.float32, shape).contiguous()
+            grad_outputs = _on_device(on, "grad_outputs", grad_outputs, torch.float32, shape).contiguous()
             b = _kept_width(P)
-            codes = _on_device("kept", kept.codes, torch.uint8,
+            codes = _on_device(on, "kept", kept.codes, torch.uint8,
                                (max(steps - 1, 0), -(-P // b), nodes, b)).contiguous()
             grad_w = torch.empty(edges, dtype=torch.float32, device=x.device)
             grad_x = torch.empty((G, P, n_in), dtype=torch.float32,
@@ -1091,7 +1091,7 @@ class Networks:
             _check(lib().emr_activate_backward(
                 self.handle, x.data_ptr(), P, steps, outputs.data_ptr(), codes.data_ptr(), codes.numel(),
                 grad_outputs.data_ptr(), grad_w.data_ptr() or x.data_ptr(),
-                None if grad_x is None else grad_x.data_ptr(), raw))
+                None if grad_x is None else grad_x.data_ptr(), on.raw))
             return grad_w, grad_x
 
 
@@ -1114,10 +1114,11 @@ class Kept:
         dtype = dtype or torch.float32
         if _score_type(dtype) is None:
             raise ValueError("dtype: float32, bfloat16 or float16 is needed")
-        with _On(stream) as raw:
+        with _On(stream) as on:
+            _on_device(on, "kept", self.codes)
             out = torch.empty((planes, nodes, self.patterns), dtype=dtype, device=self.codes.device)
             _check(lib().emr_kept_values(self.codes.data_ptr(), nodes, self.patterns, planes + 1,
-                                         _score_type(dtype), out.data_ptr(), raw))
+                                         _score_type(dtype), out.data_ptr(), on.raw))
             return out
 
 
@@ -1168,11 +1169,13 @@ def emr_build_networks(pop: Population, substrate, depth: int, theta: float, typ
 
 # ----------------------------------------------------------------------------- choices
 
-def _on_device(name, t, dtype=None, shape=None):
-    """t, checked: a device tensor of the dtype and shape asked for."""
-    import torch
-    if not torch.is_tensor(t) or not t.is_cuda:
-        raise ValueError("%s: a device tensor is needed" % name)
+def _on_device(on, name, t, dtype=None, shape=None):
+    """t, checked: a tensor on the device of the call's stream, of the dtype and shape asked for."""
+    device = t.get_device() if hasattr(t, "get_device") else -1
+    if device != on.device:
+        if device < 0:
+            raise ValueError("%s: a device tensor is needed" % name)
+        raise ValueError("%s: on device %d, the call's stream is on %d" % (name, device, on.device))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s: %s is needed, not %s" % (name, dtype, t.dtype))
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -1181,23 +1184,23 @@ def _on_device(name, t, dtype=None, shape=None):
 
 
 class _On:
-    """The stream that a call's copies and results are made on: the call's own, as `raw`."""
+    """The stream that a call's copies and results are made on, as `raw`, and its device's number."""
 
     def __init__(self, stream):
         import torch
         if stream is not None:
-            self.outer, self.raw = torch.cuda.stream(stream), stream.cuda_stream
+            self.outer, self.raw, self.device = torch.cuda.stream(stream), stream.cuda_stream, stream.device_index
             return
-        self.outer = None
+        self.outer, self.device = None, torch.cuda.current_device()
         try:  # (without a Stream object: that takes longer than most calls' launch)
-            self.raw = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+            self.raw = torch._C._cuda_getCurrentRawStream(self.device)
         except AttributeError:
             self.raw = torch.cuda.current_stream().cuda_stream
 
     def __enter__(self):
         if self.outer is not None:
             self.outer.__enter__()
-        return self.raw
+        return self
 
     def __exit__(self, *e):
         if self.outer is not None:
@@ -1235,12 +1238,12 @@ def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: 
     one for each row (float32; top_k int32). Returns index (int32 [rows, draws]) and their
     log-probabilities (float32, or None without logp), not synchronized."""
     import torch
-    if not torch.is_tensor(scores) or not scores.is_cuda:
+    if not getattr(scores, "is_cuda", False):
         raise ValueError("scores: a device tensor is needed")
-    with _On(stream) as raw:
-        st, x = _scores(scores)
+    with _On(stream) as on:
+        st, x = _scores(_on_device(on, "scores", scores))
         rows = st.rows
-        _on_device("u", u, torch.float32)
+        _on_device(on, "u", u, torch.float32)
         if u.dim() != 2 or u.shape[0] != rows:
             raise ValueError("u: shape (%d, draws) is needed, not %s" % (rows, tuple(u.shape)))
         u = u.contiguous()
@@ -1248,7 +1251,7 @@ def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: 
         for name, v, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                                ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
             if torch.is_tensor(v):
-                v = _on_device(name, v, dtype, (rows,)).contiguous()
+                v = _on_device(on, name, v, dtype, (rows,)).contiguous()
                 held.append(v)
                 rule += (0, v.data_ptr())
             else:
@@ -1257,7 +1260,7 @@ def emr_sample(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp: 
         index = torch.empty_like(u, dtype=torch.int32)
         lp = torch.empty_like(u) if logp else None
         _check(lib().emr_sample(C.byref(st), C.byref(rule), u.data_ptr(), u.shape[1], index.data_ptr(),
-                                lp.data_ptr() if logp else None, raw))
+                                lp.data_ptr() if logp else None, on.raw))
         return index, lp
 
 
@@ -1266,16 +1269,16 @@ def emr_answer_loss(scores, index, scale=None, temperature: float = 1.0, stream=
     include/emr.h. index: int32 [rows]; scale: float32 [rows] or None. Returns loss (float32 [rows]) and
     grad ([rows, n], of the scores' type), not synchronized."""
     import torch
-    if not torch.is_tensor(scores) or not scores.is_cuda:
+    if not getattr(scores, "is_cuda", False):
         raise ValueError("scores: a device tensor is needed")
-    with _On(stream) as raw:
-        st, x = _scores(scores)
+    with _On(stream) as on:
+        st, x = _scores(_on_device(on, "scores", scores))
         rows, n = x.shape
-        index = _on_device("index", index, torch.int32, (rows,)).contiguous()
+        index = _on_device(on, "index", index, torch.int32, (rows,)).contiguous()
         if scale is not None:
-            scale = _on_device("scale", scale, torch.float32, (rows,)).contiguous()
+            scale = _on_device(on, "scale", scale, torch.float32, (rows,)).contiguous()
         loss = torch.empty(rows, dtype=torch.float32, device=x.device)
         grad = torch.empty((rows, n), dtype=x.dtype, device=x.device)
         _check(lib().emr_answer_loss(C.byref(st), index.data_ptr(), None if scale is None else scale.data_ptr(),
-                                     temperature, loss.data_ptr(), grad.data_ptr(), n, raw))
+                                     temperature, loss.data_ptr(), grad.data_ptr(), n, on.raw))
         return loss, grad

@@ -80,3 +80,48 @@ def test_binding_refuses():
         emr.emr_sample(x, torch.zeros((2, 1)))
     with pytest.raises(ValueError):
         emr.emr_answer_loss(x, torch.zeros(2, dtype=torch.int32))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """A call launches on the current device (a stream's own): tensors that lie elsewhere would be read
+    across, or not at all. (Tensors without memory stand for a second device's.)"""
+    torch = pytest.importorskip("torch")
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    class On:
+        raw, device = None, 0
+
+        def __init__(self, stream):
+            pass
+
+        def __enter__(self):
+            return self
+
+        def __exit__(self, *e):
+            pass
+
+    monkeypatch.setattr(emr, "_On", On)
+    net = emr.Networks(None)
+    net._counts = (2, 8, 5, 3, 1)  # genomes, nodes, edges, inputs, outputs
+    with FakeTensorMode():
+        def new(*shape, dtype=torch.float32, device="cuda:0"):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        def each(call, *tensors):
+            for k in range(len(tensors)):
+                for device in ("cuda:1", "cpu"):
+                    args = list(tensors)
+                    args[k] = torch.empty_like(args[k], device=device)
+                    with pytest.raises(ValueError, match="device"):
+                        call(*args)
+
+        i32, u8 = torch.int32, torch.uint8
+        each(lambda x, u: emr.emr_sample(x, u), new(4, 9), new(4, 2))
+        each(lambda t, k, p, m: emr.emr_sample(new(4, 9), new(4, 2), t, k, p, m), new(4), new(4, dtype=i32), new(4),
+             new(4))
+        each(lambda x, i, s: emr.emr_answer_loss(x, i, s), new(4, 9), new(4, dtype=i32), new(4))
+        each(net.set_weights, new(5))
+        each(lambda x: net.activate_keep(x, 2), new(4, 3))
+        each(lambda x, o, c, g: net.activate_backward(x, 2, o, emr.Kept(c, 4), g), new(4, 3), new(2, 4, 1),
+             new(1, 1, 8, 4, dtype=u8), new(2, 4, 1))
+        each(lambda c: emr.Kept(c, 4).values(), new(1, 1, 8, 4, dtype=u8))
