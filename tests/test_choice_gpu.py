@@ -437,3 +437,73 @@ def test_loss_of_more_rows_than_a_launch_takes(emr, n, rows):
     emr._check(emr.lib().emr_answer_loss(C.byref(st), index.data_ptr(), None, C.c_float(0.5), loss.data_ptr(), None,
                                          0, emr._stream_ptr()))
     assert torch.equal(loss, torch.where(index < 0, 0.0, few[at]))
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n", [65529, 65530, 65533, 65534, 70001])
+def test_loss_of_rows_around_the_registers(emr, n, type):
+    """The longest rows that a workgroup's registers hold (fewer by up to a group where unaligned), and those read
+    three times."""
+    test_loss(emr, n, type)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+def test_long_losses_in_place_and_strided(emr, type):
+    import ctypes as C
+    n = 70003
+    x, _ = scores(n, 5, n, type, pad=6)
+    index = x.float().argmax(1).int()
+    loss, grad = emr.emr_answer_loss(x, index, temperature=0.7)
+    wide = torch.empty((5, n + 6), dtype=x.dtype, device="cuda")
+    y = wide[:, 3:n + 3]
+    y.copy_(x)
+    wide[:, :3], wide[:, n + 3:] = 7.0, 7.0
+    st, held = emr._scores(y)
+    assert held is y
+    out = torch.empty(5, device="cuda")
+    emr._check(emr.lib().emr_answer_loss(C.byref(st), index.data_ptr(), None, C.c_float(0.7), out.data_ptr(),
+                                         y.data_ptr(), n + 6, emr._stream_ptr()))
+    torch.cuda.synchronize()
+    assert torch.equal(y, grad) and torch.equal(out, loss)
+    assert (wide[:, :3] == 7).all() and (wide[:, n + 3:] == 7).all()
+
+
+@pytest.mark.parametrize("n", [1048573, 1048574, 1100003, 2200001])
+def test_parts_of_more_entries(emr, n):
+    """Rows of more than 4096 parts of 256 scores: parts of 512 and more, limits and draws inside them, and equal
+    scores across them."""
+    for j, rule in enumerate((dict(), dict(k=n // 3, t=3.0), dict(k=100, p=0.9), dict(p=0.97), dict(p=0.5, t=20.0),
+                              dict(min_p=0.05, t=2.0))):
+        x, u = scores(n + j, 2, n, ("f32", "bf16", "f16")[j % 3], pad=(0, 1, 3)[j % 3])
+        check(emr, x, u, **rule)
+    x = torch.zeros((2, n), device="cuda")
+    x[1] = torch.arange(n, device="cuda") % 5
+    u = torch.rand((2, 300), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    for rule in (dict(), dict(k=n // 2 + 1), dict(p=0.5), dict(k=n - 1, p=0.3), dict(k=n // 3 + 1, p=0.77, t=0.5)):
+        check(emr, x, u, **rule)
+
+
+def test_longest_rows(emr):
+    """Two rows of 2^31 - 1 scores, the second one unaligned and beyond 2^32 bytes, of which a few are not masked:
+    the draws, losses and gradients of those few alone."""
+    n, at = (1 << 31) - 1, [0, 5, 1000, 1 << 30, (1 << 31) - 300, (1 << 31) - 2]
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough free device memory")
+    few = torch.tensor([[0.5, 1.0, -2.0, 1.0, 0.25, 1.5], [-1.0, 2.0, 0.0, 2.0, 2.0, 0.5]], dtype=torch.bfloat16,
+                       device="cuda")
+    x = torch.full((2, n), -np.inf, dtype=torch.bfloat16, device="cuda")
+    place = torch.tensor(at, device="cuda")
+    x[:, place] = few
+    u = torch.rand((2, 40), device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    for rule in (dict(), dict(top_k=3), dict(top_p=0.6), dict(top_k=5, top_p=0.8, min_p=0.1, temperature=0.6),
+                 dict(temperature=0.0)):
+        want, lp = emr.emr_sample(few, u, **rule)
+        index, logp = emr.emr_sample(x, u, **rule)
+        assert torch.equal(index.long(), place[want.long()]) and torch.equal(logp, lp)
+    pick = torch.tensor([5, 3], device="cuda")
+    loss, grad = emr.emr_answer_loss(x, place[pick].int(), temperature=0.5)
+    want, g = emr.emr_answer_loss(few, pick.int(), temperature=0.5)
+    # (sums of few and of many lanes: their roundings, and the gradient's to bfloat16)
+    assert ((loss - want).abs() <= 2.0 ** -20 * (1 + want.abs())).all()
+    assert ((grad[:, place].float() - g.float()).abs() <= 2.0 ** -8 * g.float().abs() + 2.0 ** -20).all()
+    assert int((grad[:, ::4099] != 0).sum()) <= 12 and int(torch.count_nonzero(grad[1, 6:1000])) == 0

@@ -544,3 +544,17 @@ def test_many_patterns_of_large_genomes(emr):
         got = gw[g * e:(g + 1) * e].double()
         assert ((got - gm[to, own]).abs() <= eps * ga[to, own] + 1e-30).all()
         assert ((gx[g].double().t() - xs).abs() <= eps * xa + 1e-30).all()
+
+
+@pytest.mark.parametrize("hidden", [[10300], [40, 10300, 0], [10236], [10237]])
+def test_genomes_larger_than_any_layout(emr, hidden):
+    """Genomes of more than 10239 nodes (and around that), alone and beside small ones: no layout, a launch for
+    each step."""
+    a = random_nets(sum(hidden), hidden, 2, 1, 6, mixed=True)
+    net = load(emr, a)
+    rng = np.random.default_rng(4)
+    for patterns, steps in ((2, 1), (2, 3), (19, 3), (5, 4), (19, 0)):
+        check(emr, net, a, rng.uniform(-1, 1, (patterns, 2)), steps)
+    w = torch.tensor(a["w"], device="cuda")
+    net.set_weights(w * -0.5)
+    check(emr, net, dict(a, w=a["w"] * np.float32(-0.5)), rng.uniform(-1, 1, (9, 2)), 3)
