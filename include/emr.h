@@ -528,9 +528,9 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  * Learning the weights. emr_activate_keep is emr_activate with the patterns on the device (inputs,
  * [n_patterns][n_inputs], caller-owned) that also keeps every step's states in 8 bits (its sums, in fp32
  * as well, run in another order: the outputs differ from emr_activate's by their rounding);
- * emr_activate_backward takes them to the derivatives of a loss by the weights (grad_w, device, [edges]) and, where grad_inputs (device, [n_genomes][n_patterns][n_inputs]) is not
- * NULL, by each genome's copy of the patterns, from those by the outputs (grad_outputs, device,
- * [n_genomes][n_patterns][n_outputs]).
+ * emr_activate_backward takes them to the derivatives of a loss by the weights (grad_w, device, [edges]) and,
+ * where grad_inputs (device, [n_genomes][n_patterns][n_inputs]) is not NULL, by each genome's copy of the
+ * patterns, from those by the outputs (grad_outputs, device, [n_genomes][n_patterns][n_outputs]).
  *   - kept (device, caller-owned, emr_kept_bytes of it, aligned to 16 bytes): code c = rint(255 s) stands
  *     for the state c / 255, an error of at most 1 / 510 against 4 bytes for the float. Codes are
  *     [steps - 1][blocks][nodes][b], b patterns beside each other: b = 4, 8 or 16 for up to 4, up to 8 or
@@ -540,6 +540,11 @@ emr_status emr_networks_set_weights(const emr_networks* net, const float* w, voi
  *   - The gradient is the one of the activation with each state replaced by c / 255 in both places where it
  *     occurs (the product with a weight's derivative, and s (1 - s)), in fp32; every sum has a fixed
  *     order, so a handle's gradients are the same bits on every call.
+ *   - Against the gradient of unrounded states: a state above 254.5 / 255 or below 0.5 / 255 (of a sum beyond
+ *     6.2) has slope 0, and what passes through such states alone is lost. On discovered networks (populations
+ *     of 30 and 60, 2 to 32 inputs, 2 to 5 steps) a population's gradient was off by 0.24 to 1.5 % of its 2-norm
+ *     and the median network's by 0.2 to 0.8 %, but that of a network whose states all lie at the ends, itself
+ *     small, by all of it.
  *   - Memory that a handle keeps from its first call of the two on: the edges laid out four times (about 100
  *     bytes an edge, and at least 10 KB a genome); partial sums and states, 2 GiB at most beyond one copy of
  *     each genome's (about 8 bytes an edge), whatever the number of patterns; for networks too large or too few

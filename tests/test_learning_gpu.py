@@ -558,3 +558,73 @@ def test_genomes_larger_than_any_layout(emr, hidden):
     w = torch.tensor(a["w"], device="cuda")
     net.set_weights(w * -0.5)
     check(emr, net, dict(a, w=a["w"] * np.float32(-0.5)), rng.uniform(-1, 1, (9, 2)), 3)
+
+
+def unrounded(a, x, steps, outputs_grad):
+    """The weights' derivatives with no state rounded (float64), and a bound on what the states' rounding to 8
+    bits and fp32 leave of it. A state's code errs by 1 / 510 and by what fp32 moved the state (a sum's chain of
+    adds and the sigmoid's own, forward through the steps), an input not at all; s (1 - s) errs by no more than
+    s does. So, backwards, with sizes |.| and errors e: e(gz s) <= e(gz) (|s| + e(s)) + |gz| e(s), and
+    e(d s (1 - s)) <= e(d) (s (1 - s) + e(s)) + |d| e(s)."""
+    G, P = len(a["node_offset"]) - 1, len(x)
+    nodes = int(a["node_offset"][-1])
+    held = np.concatenate([o + np.nonzero(a["is_in"])[0] for o in a["node_offset"][:-1]])
+    degree = np.diff(a["in_offset"])
+    dst, src, w = np.repeat(np.arange(nodes), degree), a["src"], a["w"].astype(np.float64)
+    u = 2.0 ** -24
+
+    def sums(at, of, weight, v):
+        out = np.zeros((nodes, P))
+        np.add.at(out, at, weight[:, None] * v[of])
+        return out
+
+    states = forward64(a, x, steps)
+    fp32 = [np.zeros((nodes, P))]
+    for t in range(steps):
+        ez = sums(dst, src, np.abs(w), fp32[t]) + (degree[:, None] + 8) * u * sums(dst, src, np.abs(w), np.abs(states[t]))
+        slope = states[t + 1] * (1 - states[t + 1])
+        e = np.minimum(0.25, slope + 0.1 * ez) * ez + 4 * u  # (the sigmoid's second derivative is below 0.1)
+        e[held] = 0
+        fp32.append(e)
+    err = [np.zeros((nodes, P))] + [e + 1 / 510 for e in fp32[1:]]
+    for e in err:
+        e[held] = 0
+    at = output_nodes(a).reshape(-1)
+    g = outputs_grad.astype(np.float64).transpose(0, 2, 1).reshape(-1, P)
+    gz, ez = np.zeros((nodes, P)), np.zeros((nodes, P))
+    o = states[steps][at]
+    gz[at] = g * o * (1 - o)
+    ez[at] = np.abs(g) * (fp32[steps][at] + 4 * u)
+    gw, ew, size = np.zeros(len(src)), np.zeros(len(src)), np.zeros(len(src))
+    za = np.abs(gz) + ez
+    for t in range(steps, 0, -1):
+        s, e = states[t - 1], err[t - 1]
+        gw += (gz[dst] * s[src]).sum(1)
+        ew += (ez[dst] * (np.abs(s) + e)[src] + np.abs(gz)[dst] * e[src]).sum(1)
+        size += (za[dst] * (np.abs(s) + e)[src]).sum(1)
+        d, ed, da = sums(src, dst, w, gz), sums(src, dst, np.abs(w), ez), sums(src, dst, np.abs(w), za)
+        slope = np.abs(s * (1 - s))
+        gz, ez, za = d * s * (1 - s), ed * (slope + e) + np.abs(d) * e, da * (slope + e)
+        for v in (gz, ez, za):
+            v[held] = 0
+    terms = int(max(degree.max(), P, np.bincount(src).max()))
+    return gw, ew + unit(steps, terms) * size
+
+
+@pytest.mark.parametrize("inputs,types,iterations,steps", [(5, 15, 1, 3), (2, 1, 0, 2), (8, 15, 1, 5)])
+def test_gradient_against_unrounded_states(emr, inputs, types, iterations, steps):
+    """On discovered networks, in-degrees from none to hundreds."""
+    subs = W.tabular_sources(inputs)
+    pop = emr.emr_pack_population(W.population(3, 30, 20, 60))
+    net = emr.emr_build_networks(pop, subs, 5, 0.02, types, 0.1, iterations)
+    a = from_handle(emr, net, subs)
+    assert len(a["w"]) > 1000
+    rng = np.random.default_rng(1)
+    x = rng.uniform(-1, 1, (21, int(a["is_in"].sum()))).astype(np.float32)
+    grad_out = rng.standard_normal((30, 21, int((~a["is_in"]).sum()))).astype(np.float32)
+    xd = torch.tensor(x, device="cuda")
+    out, kept = net.activate_keep(xd, steps)
+    gw, _ = net.activate_backward(xd, steps, out, kept, torch.tensor(grad_out, device="cuda"))
+    want, bound = unrounded(a, x.astype(np.float64), steps, grad_out)
+    assert np.abs(want).max() > 0
+    assert (np.abs(gw.cpu().numpy() - want) <= bound + 1e-30).all()
