@@ -152,7 +152,8 @@ __device__ __forceinline__ uint32_t ties_of(double target, uint64_t before, uint
 // ----------------------------------------------------------------------------- short rows
 
 // Rows of up to G scores, G lanes each, a score to a lane. An entry's rank, and the weight before it by
-// rank, come from comparing it with the G others. Bound by the launch: 4000 rows of 8 take 9.6 us a call.
+// rank, come from comparing it with the G others. Bound by the launch: 4000 rows of 8 take 9.6 us a call. A row's
+// draws are its lanes' alone: 300000 draws of one row of 50 take 2.35 ms, where a row of 1000 takes 16 us.
 template <int TYPE, int G>
 __global__ void __launch_bounds__(256) k_sample_short(SampleArgs A) {
   using T = typename Score<TYPE>::T;
@@ -856,7 +857,9 @@ __device__ __forceinline__ void draw_listed(const SampleArgs& A, const RowRule& 
 // A workgroup for a row (blockIdx.x, from A.first on), and for a share of its draws (blockIdx.y). Memory: the row once
 // (J > 0); else for its maximum, for the limits' bins and for the parts' sums, and once more for each division of
 // a crowded bin. 256 rows of 131072 float scores, top-p: 109 us, 1.2 TB/s of the scores read once (each is read
-// three times); 256 rows of 2485, all filters: 15 us, latency.
+// three times, 200 MB of it from memory, and the VALU issues in 56 % of the cycles); 256 rows of 2485, all filters:
+// 15 us, latency. Draws from a short list look at all of the workgroup's: one row, top-k of up to 128, 16384
+// draws: 400 us.
 template <int TYPE, int NT, int J>
 __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
   using T = typename Score<TYPE>::T;
@@ -872,8 +875,8 @@ __global__ void __launch_bounds__(NT) k_sample_row(SampleArgs A) {
     m = capped(m);
   }
   RowRule R = row_rule(A, r, (uint64_t)key_of(m) << 32);
-  // (bounded for the least temperatures, whose bins then cover fewer scores than weigh nothing: the maximum's
-  // difference of 0 times an infinity would be in no bin)
+  // (bounded for the least temperatures, where it would be an infinity, and the maximum's difference of 0 times
+  // that in no bin: the bins then cover more scores than weigh anything)
   R.per = fmaxf(-R.inv * ((float)kBins / kSpan), -3.402823466e38f);
   if (!(m > -INFINITY) || R.greedy) {
     const bool none = !(m > -INFINITY);
@@ -1070,8 +1073,9 @@ __device__ __forceinline__ float row_max(float v, float* part) {
 // A row for NT threads (a wave: four rows to a workgroup), its scores in registers as J groups of 16 bytes to
 // a thread, or (J = 0) read for the maximum, the sum and the gradient. Groups lie where memory is aligned; the
 // row's first entry is number `lo` of its first group. The sum is taken in doubles, so that its float does
-// not depend on where the row lies. One read and one write of each row, which is what bounds it: 2047 rows of
-// 32001 bfloat16 scores in 83.5 us, 3.1 TB/s.
+// not depend on where the row lies. One read and one write of each row: 2047 rows of 32001 bfloat16 scores in
+// 83.4 us, 3.1 TB/s, bound as much by arithmetic as by memory: the VALU issues in 67 % of the cycles, three
+// waves to a SIMD (an entry is unpacked, its exponential taken, added in double, scaled and rounded).
 template <int TYPE, int NT, int J>
 __global__ void __launch_bounds__(NT == kWave ? 256 : NT) k_loss_row(LossArgs A) {
   using T = typename Score<TYPE>::T;
@@ -1208,6 +1212,10 @@ void launch_row(const SampleArgs& A, hipStream_t s) {
                        s, B);
   }
 }
+// The smallest variant that holds a row. It is the faster one up to its border, with exceptions (us of it and of the
+// next one, float scores, top-p 0.95; 4096 rows up to 8189 scores, then 1024): 64 scores: 11.9, 28.3; 1021: 33, 42;
+// 4093: 67, 93; 8189: 136, 232 (but 256 rows, one to a CU: 24, 17); 16381: 80, 94; 32765: 146, 127, since the
+// weights' registers spill there (without a filter 83, 89; with top-k 50 too 82, 92).
 template <int TYPE>
 void launch_sample(const SampleArgs& A, hipStream_t s) {
   if (A.n <= 8) launch_short<TYPE, 8>(A, s);
@@ -1236,6 +1244,9 @@ void launch_loss_row(const LossArgs& A, hipStream_t s) {
     hipLaunchKernelGGL((k_loss_row<TYPE, NT, J>), dim3((uint32_t)((rows + each - 1) / each)), dim3(threads), 0, s, B);
   }
 }
+// The smallest variant that holds a row (us of it and of the next one at its border, float scores, 4M of them up to
+// rows of 64, then 32M): 8: 14.6, 25.6; 16: 14.2, 25.7; 32: 14.4, 26.9; 64: 15.2, 30.4; 1021: 42.6, 65.1; 4093: 42.7, 50.2;
+// 16381: 40.9, 43.9; 32765: 43.3, 58.8; 65533: 50.2, 75.1 (bfloat16 rows of 65529: 40.4, 42.0).
 template <int TYPE>
 void launch_loss(const LossArgs& A, hipStream_t s) {
   constexpr uint32_t V = 16 / sizeof(typename Score<TYPE>::T);

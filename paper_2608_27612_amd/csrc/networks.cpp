@@ -1111,10 +1111,11 @@ emr_status kept_layout(int64_t nodes, int32_t n_patterns, int32_t steps, uint8_t
 }
 
 // Items of a call over all genomes, about: many times what the chip holds, so that their ends fall together (150
-// networks on 1000 patterns, gradients: 1.10 ms at 4096, 0.98 at 16384, 0.97 at 65536).
+// networks on 1000 patterns, gradients: 1139 us at 4096, 1030 at 16384, 1016 at 32768, 1010 at 65536; activation: 773,
+// 665, 646, 643).
 constexpr double kLearnItems = 32768.0;
-// Copies of a stepped genome's sums, at most. (Three of 5000 to 9000 nodes, a step: 50 us with a copy for each of
-// 16 blocks of patterns, 58 with eight, 67 with four: fewer leave longer workgroups.)
+// Copies of a stepped genome's sums, at most. (Three of 5000 to 9000 nodes, 6 steps, inputs in the caches: 279 us with a copy for each of
+// 16 blocks of patterns, 311 with eight, 442 with four: fewer leave longer workgroups.)
 constexpr uint32_t kStepGroups = 64;
 // Bytes of the items' sums and of their values outside LDS, beyond the one item that a genome has at least: where
 // more items would take more, there are fewer, longer ones. (Gradients of 150 networks of up to 773 hidden nodes on

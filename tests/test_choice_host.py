@@ -82,6 +82,7 @@ def test_binding_refuses():
         emr.emr_answer_loss(x, torch.zeros(2, dtype=torch.int32))
 
 
+@pytest.mark.filterwarnings("ignore:Accessing the data pointer of FakeTensor")
 def test_tensors_of_another_device_are_refused(monkeypatch):
     """A call launches on the current device (a stream's own): tensors that lie elsewhere would be read
     across, or not at all. (Tensors without memory stand for a second device's.)"""
